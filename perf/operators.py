@@ -254,7 +254,7 @@ def _append(s):
     most = mean.abs().amax(2)
     fine = torch.isfinite(most)
     step = torch.where(fine, most / 127, math.inf)
-    whole = (mean / step[:, :, None]).round()
+    whole = (mean / step[:, :, None]).round().clamp(-127, 127)
     kq[page] = torch.where((fine & (step > 0))[:, :, None], whole, 0.0).to(torch.int8)
     ks[page] = step
     return kc, vc, kq.float() * ks[:, :, None]
@@ -292,7 +292,7 @@ def _attend(s):
     x.sub_(top).exp_()
     total = x.sum(4, keepdim=True)
     o = (x.view(R, Hkv, -1, longest) @ V.permute(0, 2, 1, 3).contiguous()).view(R, Hkv, -1, N, D)
-    o = torch.where(total > 0, o / total, 0.0).permute(0, 3, 1, 2, 4).reshape(R, N, Hq, D)[there].to(q.dtype)
+    o = torch.where(total == 0, 0.0, o / total).permute(0, 3, 1, 2, 4).reshape(R, N, Hq, D)[there].to(q.dtype)
     if not c["lse"]:
         return o
     return o, (top + total.log())[..., 0].permute(0, 3, 1, 2).reshape(R, N, Hq)[there]
@@ -307,7 +307,7 @@ def _select(s):
     u = q.view(s["T"], Hkv, -1, D).double().sum(2).float()
     most = u.abs().amax(2, keepdim=True)
     step = most / 127
-    q8 = torch.where((step > 0) & torch.isfinite(most), (u / step).round(), 0.0)[token]  # R, N, Hkv, D
+    q8 = torch.where((step > 0) & torch.isfinite(most), (u / step).round().clamp(-127, 127), 0.0)[token]  # R, N, Hkv, D
     page = table.long().clamp(min=0)
     k8 = s["kq"][page].float().permute(0, 2, 3, 1).contiguous()  # R, Hkv, D, W
     score = q8.permute(0, 2, 1, 3) @ k8  # whole numbers below 2^24
@@ -344,7 +344,7 @@ def _sparse(s):
     x = (x - top).exp()
     total = x.sum(3, keepdim=True)
     V = torch.where(live[..., None], s["vc"][rows].view(T, Hkv, -1, D).float(), 0.0)
-    o = torch.where(total > 0, (x @ V) / total, 0.0).view(T, Hq, D).to(q.dtype)
+    o = torch.where(total == 0, 0.0, (x @ V) / total).view(T, Hq, D).to(q.dtype)
     return (o, (top + total.log()).view(T, Hq)) if c["lse"] else o
 
 
