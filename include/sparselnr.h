@@ -244,6 +244,151 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
                                          int64_t N, int64_t M, int64_t colidx_len,
                                          int64_t *nnz_out, void *stream);
 
+/* ------------------------------------------------------------------------
+ * Attention over a paged cache.
+ *
+ * A serving program keeps the keys and values of its requests in pages of a
+ * shared cache: request r's row of position j lies in page table[r][j / P] at
+ * place j % P.  That table is the structure of a sparse matrix as B is above,
+ * and attention is its SDDMM (q.k) and SpMM (p.v) with a softmax between them,
+ * computed in one pass.  (No counterpart in the paper, whose <SDDMM, SpMM> has
+ * no softmax.)
+ *
+ * Conventions, besides those above on pointers, streams, errors and
+ * determinism (results are bit-identical for the same inputs):
+ *   - Types: bf16, fp16 or fp32 values; products of 16-bit values accumulate in
+ *     fp32, and so do the softmax' maximum, sum and the weighted sum.  The
+ *     weights are rounded to the values' type for their product with V.
+ *   - New tokens are packed: request r's n_r = qptr[r+1] - qptr[r] new tokens are
+ *     the rows qptr[r] .. of q, k, v and out (as the rows of a CSR matrix); they
+ *     are the last n_r of its seq_len[r] positions, and their own rows have to be
+ *     in the cache.  n_r = 1 is a decode step; any mixture is fine.  Rows of out
+ *     and sel that belong to no request are left as they were.
+ *   - Heads: Hq is a multiple of Hkv; query head h reads KV head h / (Hq / Hkv).
+ *   - A table entry outside [0, pages) is a page that is not there (not yet
+ *     taken, or given back): its keys are not seen.  A query that sees no key
+ *     gets zeros, and -inf as its lse.  Whatever the arrays on the device hold,
+ *     no call reads or writes outside the arrays that it was given.
+ *   - Keys that a query does not see have no part in its result, whatever their
+ *     rows hold (NaN and infinities included).  NaN in what it sees gives NaN.
+ *   - dim: a multiple of 8 up to 256.  page_size: a power of two up to
+ *     SPARSELNR_MAX_PAGE.  Row, page and head strides are in values, may be any
+ *     that keep each row of dim values at a multiple of 16 bytes (so a slice of a
+ *     fused q/k/v projection and caches of either order of slots and heads
+ *     will do); the dim values of a row are adjacent.  Anything else is
+ *     SPARSELNR_ERR_UNSUPPORTED.  R < 2^24, T < 2^28, W * page_size and T * Hq < 2^31.
+ *   - R = 0 or T = 0 is a no-op.
+ *   - The two attention calls use a workspace per (device, stream) for the
+ *     results of contexts that are cut into pieces; its size depends on the
+ *     type and dim class alone (at most 68 MB), so that one call of a kind allocates it,
+ *     later ones and captured graphs find it whatever the lengths are.
+ * ---------------------------------------------------------------------- */
+
+enum sparselnr_dtype { SPARSELNR_BF16 = 0, SPARSELNR_FP16 = 1, SPARSELNR_FP32 = 2 };
+
+#define SPARSELNR_MAX_PAGE 4096
+
+/* The cache: K and V rows of dim values for every page, place and KV head. */
+typedef struct sparselnr_kv_cache {
+  void *k, *v;
+  int64_t pages, page_size, heads, dim;
+  int64_t k_page, k_slot, k_head; /* strides of K, in values */
+  int64_t v_page, v_slot, v_head; /* strides of V */
+  int32_t dtype;                  /* sparselnr_dtype, of q, k, v and out too */
+} sparselnr_kv_cache;
+
+/* The requests of a call. */
+typedef struct sparselnr_requests {
+  const int32_t *table; /* [R][W], rows table_stride apart */
+  int64_t table_stride;
+  const int32_t *seq_len; /* [R] positions, new tokens included */
+  const int32_t *qptr;    /* [R + 1] */
+  int64_t R, W, T;        /* T: rows of q */
+} sparselnr_requests;
+
+/*
+ * Block tables and slots from the request lengths: request r has ctx_len[r]
+ * cached and new_len[r] new tokens (negative lengths count as none).  Writes
+ *   qptr[r]     = sum of new_len before r          (R + 1 entries)
+ *   seq_len[r]  = ctx_len[r] + new_len[r]
+ *   table[r][j] for the pages j that the new tokens begin, handed out of
+ *               free_pages[0 .. F) in the order of requests and positions; -1 where
+ *               the list is used up.  Entries from W on do not exist.
+ *   slots[t]    = page * page_size + place of new token t, -1 if it has no page;
+ *               T >= qptr[R] entries, those from qptr[R] on -1
+ *   counts      = { qptr[R], pages wanted, tokens without a slot }
+ * counts[1] is what the free list goes forward by (if it is at most F); a
+ * counts[2] above zero tells that F or W was too small.  If T < qptr[R], tokens
+ * from T on get no slot and no table entry.  The sums have to stay below 2^31.
+ */
+SPARSELNR_API int sparselnr_page_tables(const int32_t *ctx_len, const int32_t *new_len, int32_t *table,
+                                        int64_t table_stride, const int32_t *free_pages, int32_t *qptr,
+                                        int32_t *seq_len, int64_t *slots, int32_t *counts, int64_t R,
+                                        int64_t W, int64_t F, int64_t T, int64_t page_size,
+                                        void *stream);
+
+/*
+ * Writes the new tokens' K and V rows (T x Hkv x dim, strides in values) into
+ * their slots; slots outside the cache are left out.  With kq (int8
+ * [pages][Hkv][dim]) and kscale (float [pages][Hkv]), renews the summaries of the
+ * pages written to: m = mean of the page's K rows up to the last one written (sum in
+ * 64 bits, rounded once to 32), step = max|m| * s, s = 1/127 in 32 bits, kq = m / step rounded to the nearest
+ * whole number (ties to even), kscale = step; 0 and 0 for a mean of zeros, 0 and
+ * +inf if the mean is not finite.  Slots of one page have to be adjacent in `slots` and
+ * ascending, without gaps, as sparselnr_page_tables gives them; no slot may occur twice.
+ */
+SPARSELNR_API int sparselnr_cache_append(const void *k, int64_t k_token, int64_t k_head,
+                                         const void *v, int64_t v_token, int64_t v_head,
+                                         const int64_t *slots, const sparselnr_kv_cache *cache,
+                                         int8_t *kq, float *kscale, int64_t T, void *stream);
+
+/*
+ * Attention of the new tokens over their requests' cached rows, causal: the
+ * query at position p sees the keys j <= p, and of those only j > p - window if
+ * window > 0.
+ *   out(t, h) = sum_j softmax_j(scale * q(t, h).k(j)) v(j),
+ *   lse(t, h) = log sum_j exp(scale * q(t, h).k(j))
+ * q: T x Hq x dim with strides; out: T x Hq x dim, packed; lse: float T x Hq or
+ * NULL.  scale > 0.  max_new > 0 is a hint: no request has more new tokens (0:
+ * not known); it chooses kernels, and results stay right if it is wrong.
+ */
+SPARSELNR_API int sparselnr_paged_attention(const void *q, int64_t q_token, int64_t q_head,
+                                            int64_t Hq, const sparselnr_kv_cache *cache,
+                                            const sparselnr_requests *requests, double scale,
+                                            int64_t window, int64_t max_new, void *out, float *lse,
+                                            void *stream);
+
+/*
+ * The `top` pages (at most 256) that each new token attends, per KV head, by a
+ * cheap score of the pages b <= p / page_size of its request:
+ *   u = sum of the group's query heads (in 64 bits, rounded once to 32),
+ *   q8 = u / (max|u| * s) rounded to the nearest whole number (0 if u is zero or not finite),
+ *   score(b) = float(sum_d q8(d) kq(page, d)) * kscale(page)
+ * The sum is a whole number below 2^24, so scores are exact up to one rounding
+ * and do not depend on any order.  The first `first` and the last `local` of those
+ * pages are always taken (first + local <= top); the others by score, NaN before every
+ * number, equal scores by the lower index.  Pages that are not there are never
+ * taken.  sel: int32 [T][Hkv][top], indices into the request's table row, ascending,
+ * with -1 behind them where there are fewer.
+ */
+SPARSELNR_API int sparselnr_block_select(const void *q, int64_t q_token, int64_t q_head, int64_t Hq,
+                                         int32_t dtype, const int8_t *kq, const float *kscale,
+                                         int64_t pages, int64_t page_size, int64_t Hkv, int64_t dim,
+                                         const sparselnr_requests *requests, int64_t top,
+                                         int64_t first, int64_t local, int32_t *sel, void *stream);
+
+/*
+ * Attention of each new token over its selected pages only: as
+ * sparselnr_paged_attention, with the keys j <= p of the pages sel[t][h / (Hq / Hkv)][:].
+ * Entries outside the table's row are skipped; a page that is named twice counts
+ * twice.  top * page_size < 2^29.
+ */
+SPARSELNR_API int sparselnr_block_attention(const void *q, int64_t q_token, int64_t q_head,
+                                            int64_t Hq, const sparselnr_kv_cache *cache,
+                                            const sparselnr_requests *requests, const int32_t *sel,
+                                            int64_t top, double scale, void *out, float *lse,
+                                            void *stream);
+
 /* Static text for a status code (never NULL). */
 SPARSELNR_API const char *sparselnr_status_string(int status);
 

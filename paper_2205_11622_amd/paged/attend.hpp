@@ -1,0 +1,952 @@
+// Attention over a paged cache: the SDDMM q.k, the softmax and the SpMM p v of
+// one (request, KV head) in one pass, with the running maximum and sum of the
+// softmax.  The query heads of a KV head are rows of one matrix product.
+#pragma once
+
+#include "common.hpp"
+
+namespace slnr {
+namespace paged {
+
+struct AttendArgs {
+  const void *q;         // [T][Hq][D], strides q_token, q_head
+  int64_t q_token, q_head;
+  const void *k, *v;     // [pages][P][Hkv][D]
+  int64_t k_page, k_slot, k_head, v_page, v_slot, v_head;
+  const int32_t *table;  // [R][W], row stride table_row
+  int64_t table_row;
+  const int32_t *seq;    // [R]
+  const int32_t *qptr;   // [R + 1]
+  const int32_t *sel;    // [T][Hkv][top], sparse form only
+  void *out;             // [T][Hq][D], densely packed
+  float *lse;            // [T][Hq] or null
+  float *part;           // per piece of a split tile: rows x DP values, then rows maxima and sums
+  int32_t *meta;         // per piece, what the join has to know (see Meta)
+  int32_t R, T, W, pages, shift, Hq, Hkv, G, D, top, window;
+  int32_t few;           // requests with at most this many rows belong to attend_few, the others to attend_many
+  int32_t target;        // pieces that the work is cut into, about
+  float scale2;          // scale * log2(e)
+};
+
+// meta[0]: slots that this call uses.  From kMeta * (1 + slot) on: pieces of this tile
+// if the slot is its first, else 0; the tile's first row (token * G + head of the
+// group), its rows, and the KV head.
+constexpr int kMeta = 4;
+
+__device__ __forceinline__ int imin(int a, int b) { return a < b ? a : b; }
+__device__ __forceinline__ int imax(int a, int b) { return a > b ? a : b; }
+
+struct Request {
+  int first, n, S;  // first token, tokens, visible length
+};
+
+// Whatever the arrays hold, tokens stay in [0, T) and keys in the table's row.
+__device__ __forceinline__ Request request_of(const AttendArgs &a, int r) {
+  Request q;
+  const int b = imin(imax(a.qptr[r], 0), a.T);
+  const int e = imin(imax(a.qptr[r + 1], 0), a.T);
+  q.first = b;
+  q.n = imax(e - b, 0);
+  const int64_t room = (int64_t)a.W << a.shift;
+  const int s = imax(a.seq[r], 0);
+  q.S = s < room ? s : (int)room;
+  return q;
+}
+
+// ------------------------------------------------------------- split of the work
+//
+// A tile is up to ROWS rows (token, head of the group) of one request and KV head.
+// Tiles whose keys take more than `cap` steps are cut into np equal pieces of the
+// key axis, whose results attend_join adds up; cap is such that all the work makes
+// about `target` pieces, so long contexts are cut where there are few tiles and
+// left whole where there are many.  Every block derives the split from the
+// lengths by one scan: nothing has to be planned, copied or known on the host.
+
+template <int NT>
+struct Split {
+  int begin[NT];  // pieces (of one KV head) before this thread's requests
+  int slot[NT];   // the same of split tiles only
+  long long work[NT / kWave];
+  int wave_a[NT / kWave], wave_b[NT / kWave];
+  int total, total_split, cap, per;
+};
+
+struct Piece {
+  int r, tile, part, np, slot;  // slot < 0: the tile is whole
+};
+
+// count(r, tiles, steps) gives a request's tiles and the steps of its longest one.
+template <int NT, class F>
+__device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, F count) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.R + NT - 1) / NT;
+  const int r0 = imin(tid * per, a.R), r1 = imin(r0 + per, a.R);
+  long long w = 0;
+  for (int r = r0; r < r1; ++r) {
+    int tiles, steps;
+    count(r, tiles, steps);
+    w += (long long)tiles * imax(steps, 1);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) w += __shfl_xor(w, o);
+  if (lane == 0) sh.work[wave] = w;
+  __syncthreads();
+  long long all = 0;
+#pragma unroll
+  for (int i = 0; i < NT / kWave; ++i) all += sh.work[i];
+  const long long want = (all * a.Hkv + a.target - 1) / a.target;
+  const int cap = imax(min_steps, (int)(want < (1 << 28) ? want : (1 << 28)));
+  int np = 0, ns = 0;
+  for (int r = r0; r < r1; ++r) {
+    int tiles, steps;
+    count(r, tiles, steps);
+    const int k = imax((steps + cap - 1) / cap, 1);
+    np += tiles * k;
+    ns += k > 1 ? tiles * k : 0;
+  }
+  int x = np, y = ns;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int px = __shfl_up(x, o), py = __shfl_up(y, o);
+    if (lane >= o) x += px, y += py;
+  }
+  if (lane == 63) sh.wave_a[wave] = x, sh.wave_b[wave] = y;
+  __syncthreads();
+  int bx = 0, by = 0, total = 0, total_split = 0;
+#pragma unroll
+  for (int i = 0; i < NT / kWave; ++i) {
+    if (i < wave) bx += sh.wave_a[i], by += sh.wave_b[i];
+    total += sh.wave_a[i];
+    total_split += sh.wave_b[i];
+  }
+  sh.begin[tid] = bx + x - np;
+  sh.slot[tid] = by + y - ns;
+  if (tid == 0) sh.total = total, sh.total_split = total_split, sh.cap = cap, sh.per = per;
+  __syncthreads();
+}
+
+// The piece number q of one KV head, 0 <= q < total.
+template <int NT, class F>
+__device__ Piece split_find(const Split<NT> &sh, const AttendArgs &a, int q, F count) {
+  int lo = 0, hi = NT - 1;  // the last thread that begins at or before q
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (sh.begin[mid] <= q)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  // threads without pieces begin where the next one does; the last of them with
+  // begin <= q is the one that holds q
+  int r = lo * sh.per;
+  int left = q - sh.begin[lo], slot = sh.slot[lo];
+  Piece p{};
+  for (; r < a.R; ++r) {
+    int tiles, steps;
+    count(r, tiles, steps);
+    const int np = imax((steps + sh.cap - 1) / sh.cap, 1);
+    const int here = tiles * np;
+    if (left < here) {
+      p.r = r;
+      p.np = np;
+      const int t = left / np;
+      p.tile = tiles - 1 - t;  // the longest (last) tile of a causal chunk first
+      p.part = left - t * np;
+      p.slot = np > 1 ? slot + left : -1;
+      return p;
+    }
+    left -= here;
+    if (np > 1) slot += here;
+  }
+  p.r = -1;
+  return p;
+}
+
+// ---------------------------------------------------------------- few rows
+//
+// attend_few: a block of four waves takes one piece of a tile of 16 rows (the
+// heads of one token of a decode step, or of a few tokens; the heads of one token
+// over its selected pages in the sparse form).  Each wave walks every fourth tile
+// of 32 keys.  S^T = K Q^T puts a query into a lane's column, so the softmax
+// needs two exchanges between lanes a tile, and P^T stays in the registers in
+// which O^T = V^T P^T wants it.  K goes from memory straight to the matrix cores'
+// operands; V passes through LDS to be transposed.  The waves' results are joined
+// in LDS.
+//
+// Bound by memory: a key is read once for all heads of its group.  16 KB of K and V
+// are in flight per wave while the previous tile is worked on.
+
+constexpr int kFewBlock = 256;
+constexpr int kFewWaves = kFewBlock / kWave;
+constexpr int kFewRows = 16;
+constexpr int kFewKeys = 32;                           // keys of a wave's tile
+constexpr int kFewStep = kFewKeys * kFewWaves;         // keys of a block's step
+
+template <class T, int DP>
+struct FewShared {
+  union {
+    T v[kFewWaves][kFewKeys * Tile<T, DP>::kStride];
+    float o[kFewWaves][kFewRows * DP];
+  };
+  float m[kFewWaves][kFewRows], l[kFewWaves][kFewRows];
+  Split<kFewBlock> split;
+};
+
+template <class T, int DP, bool SPARSE>
+__global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
+  typedef typename Type<T>::Vec Vec;
+  constexpr int KS = DP / 32;   // steps of the summed axis of q.k
+  constexpr int DT = DP / 16;   // tiles of output columns
+  extern __shared__ __align__(16) char raw[];
+  FewShared<T, DP> &sh = *reinterpret_cast<FewShared<T, DP> *>(raw);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 15, grp = lane >> 4;
+  const int row_tiles = (a.G + kFewRows - 1) / kFewRows;  // sparse form: of one token
+  const int P = 1 << a.shift;
+  auto count = [&](int r, int &tiles, int &steps) {
+    const Request q = request_of(a, r);
+    const long long rows = (long long)q.n * a.G;
+    tiles = rows > a.few ? 0 : (int)((rows + kFewRows - 1) / kFewRows);
+    const int lo = a.window ? imax(q.S - q.n - a.window + 1, 0) : 0;
+    steps = (q.S - lo + kFewStep - 1) / kFewStep;
+  };
+  int total, used, np_sparse = 1;
+  int steps_sparse = 0;
+  if constexpr (SPARSE) {
+    const long long keys = (long long)a.top << a.shift;
+    steps_sparse = (int)((keys + kFewStep - 1) / kFewStep);
+    const long long tiles = (long long)a.T * row_tiles * a.Hkv;
+    // all tiles are alike: cut until there are `target` pieces
+    const long long k = a.target / (tiles > 0 ? tiles : 1);
+    np_sparse = imax(1, (int)(k < steps_sparse ? k : steps_sparse));
+    total = a.T * row_tiles * np_sparse;
+    used = np_sparse > 1 ? total : 0;
+  } else {
+    split_scan<kFewBlock>(sh.split, a, 1, count);
+    total = sh.split.total;
+    used = sh.split.total_split;
+  }
+  if (blockIdx.x == 0 && tid == 0) a.meta[0] = used * a.Hkv;
+
+  for (unsigned p = blockIdx.x; p < (unsigned)total * (unsigned)a.Hkv; p += gridDim.x) {
+    const int h = (int)(p % (unsigned)a.Hkv), qn = (int)(p / (unsigned)a.Hkv);
+    // ------------------------------------------------ which rows and keys
+    int r, row0, rows, pos_first, pos_last, lo, hi, part, np, slot;
+    const int32_t *sel = nullptr;
+    Request rq;
+    if constexpr (SPARSE) {
+      part = qn % np_sparse;
+      const int t2 = qn / np_sparse;
+      const int t = t2 / row_tiles, rt = t2 % row_tiles;
+      // the request of token t: the last r with qptr[r] <= t
+      int x = 0, y = a.R - 1;
+      while (x < y) {
+        const int mid = (x + y + 1) >> 1;
+        if (a.qptr[mid] <= t)
+          x = mid;
+        else
+          y = mid - 1;
+      }
+      r = x;
+      rq = request_of(a, r);
+      np = np_sparse;
+      slot = np > 1 ? qn : -1;
+      if (t < rq.first || t >= rq.first + rq.n) {  // no request's token
+        if (slot >= 0 && tid == 0) a.meta[(1 + (int64_t)slot * a.Hkv + h) * kMeta] = 0;
+        continue;
+      }
+      row0 = t * a.G + rt * kFewRows;
+      rows = imin(a.G - rt * kFewRows, kFewRows);
+      pos_first = pos_last = rq.S - rq.n + (t - rq.first);
+      sel = a.sel + ((int64_t)t * a.Hkv + h) * a.top;
+      lo = 0;
+      hi = a.top << a.shift;
+    } else {
+      const Piece pc = split_find<kFewBlock>(sh.split, a, qn, count);
+      if (pc.r < 0) continue;
+      r = pc.r;
+      part = pc.part;
+      np = pc.np;
+      slot = pc.slot;
+      rq = request_of(a, r);
+      const int first = pc.tile * kFewRows;  // of the request's rows
+      rows = imin(rq.n * a.G - first, kFewRows);
+      row0 = rq.first * a.G + first;
+      pos_first = rq.S - rq.n + first / a.G;
+      pos_last = rq.S - rq.n + (first + rows - 1) / a.G;
+      lo = a.window ? imax(pos_first - a.window + 1, 0) : 0;
+      hi = imin(pos_last + 1, rq.S);
+    }
+    const int tiles = hi > lo ? (hi - lo + kFewKeys - 1) / kFewKeys : 0;
+    const int steps = (tiles + kFewWaves - 1) / kFewWaves;
+    const int s0 = (int)((long long)steps * part / np), s1 = (int)((long long)steps * (part + 1) / np);
+    const int32_t *table = a.table + (int64_t)r * a.table_row;
+
+    // ------------------------------------------------ the queries, as columns
+    const bool have_row = col < rows;
+    const int rho = row0 + (have_row ? col : 0);
+    const int tok = rho / a.G, head = h * a.G + rho % a.G;
+    const int pos = rq.S - rq.n + (tok - rq.first);
+    Vec q[KS];
+    {
+      const T *src = (const T *)a.q + (int64_t)tok * a.q_token + (int64_t)head * a.q_head;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const int d = i * 32 + grp * 8;
+        q[i] = load8<T>(have_row && d < a.D ? src + d : (const T *)kZeroRow);
+      }
+    }
+
+    // ------------------------------------------------ walk of the keys
+    f32x4 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
+    float m = kNegInf, l = 0.0f;
+
+    // The page of key u of the piece's axis; -1 where no row of the tile sees it.
+    auto find = [&](int u) {
+      int page = -1;
+      if (u < hi) {
+        int b = u >> a.shift, at = u;
+        if constexpr (SPARSE) {
+          b = sel[b];
+          at = (b << a.shift) | (u & (P - 1));
+        }
+        if (b >= 0 && b < a.W) page = table[b];
+        if ((unsigned)page >= (unsigned)a.pages || at > pos_last) page = -1;
+      }
+      return page;
+    };
+    int page[2], page2[2];  // of the tile to load, and of the one after it
+    Vec kr[2][KS], vr[2][KS];
+    unsigned live;  // bit: this key of the tile is there
+    auto load = [&](int base) {
+      live = 0;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const bool ok = page[s] >= 0;
+        live |= ((unsigned)__builtin_amdgcn_ballot_w64(ok) & 0xffffu) << (16 * s);
+        const int64_t in = ((base + s * 16 + col) & (P - 1));
+        const T *ks = (const T *)a.k + (int64_t)page[s] * a.k_page + in * a.k_slot + (int64_t)h * a.k_head;
+        const T *vs = (const T *)a.v + (int64_t)page[s] * a.v_page + in * a.v_slot + (int64_t)h * a.v_head;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          const int d = i * 32 + grp * 8;
+          const bool in_row = ok && d < a.D;
+          kr[s][i] = load8<T>(in_row ? ks + d : (const T *)kZeroRow);
+          vr[s][i] = load8<T>(in_row ? vs + d : (const T *)kZeroRow);
+        }
+      }
+    };
+    T *vt = sh.v[wave];
+    int base = lo + (s0 * kFewWaves + wave) * kFewKeys;
+    const int end = imin(lo + s1 * kFewStep, hi);
+    auto look = [&](int base, int out[2]) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) out[s] = base < end ? find(base + s * 16 + col) : -1;
+    };
+    look(base, page);
+    look(base + kFewStep, page2);
+    if (base < end) load(base);
+    while (base < end) {
+      const unsigned now = live;
+      const int tile = base;
+      base += kFewStep;
+      page[0] = page2[0], page[1] = page2[1];
+      look(base + kFewStep, page2);
+      // S^T = K Q^T
+      f32x4 x[2];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        x[s] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) x[s] = Type<T>::dot16(kr[s][i], q[i], x[s]);
+      }
+      // Rows of several tokens see different keys.  A key that some rows see and
+      // others do not must not reach the latter through 0 * inf: infinite and
+      // NaN values of V are taken out of the product and added on their own.
+      bool mixed = false;
+      unsigned odd = 0;
+      if constexpr (!SPARSE)
+        mixed = pos_first != pos_last && (tile + kFewKeys - 1 > pos_first || (a.window && tile <= pos_last - a.window));
+      if (mixed) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          bool bad = false;
+#pragma unroll
+          for (int i = 0; i < KS; ++i) bad |= clean8<T>(vr[s][i]);
+          unsigned long long b = __builtin_amdgcn_ballot_w64(bad);
+          b |= b >> 32;
+          b |= b >> 16;
+          odd |= ((unsigned)b & 0xffffu) << (16 * s);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+          store8<T>(vt + Tile<T, DP>::at(s * 16 + col, i * 32 + grp * 8), vr[s][i]);
+      load(base);  // the next tile's rows are on their way from here on
+
+      if (now != 0xffffffffu || mixed) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = s * 16 + grp * 4 + i;
+            bool seen = (now >> key) & 1;
+            if (mixed) seen = seen && tile + key <= pos && (!a.window || tile + key > pos - a.window);
+            x[s][i] = seen ? x[s][i] : kNegInf;
+          }
+      }
+      float top = x[0][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
+      top = max_across_16(top);
+      const float mn = fmaxf(m, top);
+      const float ms = mn == kNegInf ? 0.0f : mn * a.scale2;  // nothing seen yet: exp2(-inf - 0) = 0
+      const float fade = exp2_of(m * a.scale2 - ms);          // 0 at the first key seen
+      m = mn;
+      l *= fade;
+      Vec pv;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e = exp2_of(__builtin_fmaf(x[i >> 2][i & 3], a.scale2, -ms));
+        l += e;
+        x[i >> 2][i & 3] = e;
+        // the weights go to the matrix cores in the type of V, their sum stays in fp32
+        pv[i] = (T)e;
+      }
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= fade;
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        union {
+          Vec v;
+          T t[8];
+        } w;
+        Tile<T, DP>::read4(vt, grp * 4, i * 16, lane, w.t);
+        Tile<T, DP>::read4(vt, 16 + grp * 4, i * 16, lane, w.t + 4);
+        o[i] = Type<T>::dot16(w.v, pv, o[i]);
+      }
+      while (odd) {  // rare: a row of V with infinities or NaN at the edge of what is seen
+        const int key = __builtin_ctz(odd);
+        odd &= odd - 1;
+        float e = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (((key >> 4) << 2 | (key & 3)) == i) e = x[i >> 2][i & 3];
+        e = __shfl(e, ((key >> 2) & 3) * 16 + col);
+        const bool seen = tile + key <= pos && (!a.window || tile + key > pos - a.window);
+        const int u = tile + key;
+        const T *vs = (const T *)a.v + (int64_t)table[u >> a.shift] * a.v_page +
+                      (int64_t)(u & (P - 1)) * a.v_slot + (int64_t)h * a.v_head;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int d = i * 16 + grp * 4 + j;
+            const float v = d < a.D ? (float)vs[d] : 0.0f;
+            if (seen && !(fabsf(v) < __builtin_inff())) o[i][j] += e * v;
+          }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    // ------------------------------------------------ the four waves' results
+    l = sum_across_16(l);
+    if (l != l) m = __builtin_inff();  // NaN among the scores: the whole row is NaN
+    __syncthreads();  // every wave is done with its tile of V
+    if (grp == 0) sh.m[wave][col] = m, sh.l[wave][col] = l;
+    __syncthreads();
+    float mall = kNegInf;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) mall = fmaxf(mall, sh.m[w][col]);
+    {
+      const float f = m == kNegInf ? 0.0f : exp2_of((m - mall) * a.scale2);
+#pragma unroll
+      for (int i = 0; i < DT; ++i)
+        *reinterpret_cast<f32x4 *>(&sh.o[wave][col * DP + i * 16 + grp * 4]) = m == kNegInf ? f32x4{0, 0, 0, 0} : o[i] * f;
+    }
+    __syncthreads();
+    const int threads_row = DP / 8;
+    for (int e = tid; e < rows * threads_row; e += kFewBlock) {
+      const int i = e / threads_row, d = (e % threads_row) * 8;
+      float mx = kNegInf, sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) mx = fmaxf(mx, sh.m[w][i]);
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w)
+        sum += sh.m[w][i] == kNegInf ? 0.0f : sh.l[w][i] * exp2_of((sh.m[w][i] - mx) * a.scale2);
+      f32x4 lo4{0, 0, 0, 0}, hi4{0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        lo4 += *reinterpret_cast<const f32x4 *>(&sh.o[w][i * DP + d]);
+        hi4 += *reinterpret_cast<const f32x4 *>(&sh.o[w][i * DP + d + 4]);
+      }
+      if (slot >= 0) {
+        const int64_t s = (int64_t)slot * a.Hkv + h;
+        float *dst = a.part + s * (kFewRows * (DP + 2)) + i * DP + d;
+        *reinterpret_cast<f32x4 *>(dst) = lo4;
+        *reinterpret_cast<f32x4 *>(dst + 4) = hi4;
+        if (d == 0) {
+          float *ml = a.part + s * (kFewRows * (DP + 2)) + kFewRows * DP + i * 2;
+          ml[0] = mx;
+          ml[1] = sum;
+        }
+      } else {
+        const int rr = row0 + i, t = rr / a.G, hd = h * a.G + rr % a.G;
+        const float inv = mx == kNegInf ? 0.0f : 1.0f / sum;
+        if (d < a.D) {
+          Vec w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            w[j] = (T)(mx == kNegInf ? 0.0f : lo4[j] * inv);
+            w[4 + j] = (T)(mx == kNegInf ? 0.0f : hi4[j] * inv);
+          }
+          store8<T>((T *)a.out + ((int64_t)t * a.Hq + hd) * a.D + d, w);
+        }
+        if (d == 0 && a.lse)
+          a.lse[(int64_t)t * a.Hq + hd] = mx == kNegInf ? kNegInf : mx * (a.scale2 * kLn2) + __logf(sum);
+      }
+    }
+    if (slot >= 0 && tid == 0) {
+      int32_t *mt = a.meta + (1 + (int64_t)slot * a.Hkv + h) * kMeta;
+      mt[0] = part == 0 ? np : 0;
+      mt[1] = row0;
+      mt[2] = rows;
+      mt[3] = h;
+    }
+    __syncthreads();
+  }
+}
+
+// --------------------------------------------------------------- many rows
+//
+// attend_many: a block takes one piece of a tile of 32 * NW rows, 32 to a wave, and
+// walks it in tiles of 64 keys that all its waves share through LDS (two buffers;
+// the next tile's rows are in registers, the ones after it on their way).  As above
+// S^T = K Q^T and O^T = V^T P^T, here on the 32 x 32 x 16 products: a lane holds one
+// query and half the keys of a tile, so a row's maximum takes one exchange and P^T is
+// used where it lies.
+template <class T, int DP, int NW>
+struct ManyShared {
+  T k[2][64 * Tile<T, DP>::kStride];
+  T v[2][64 * Tile<T, DP>::kStride];
+  unsigned long long odd[2][NW];
+  Split<NW * kWave> split;
+};
+
+constexpr int kManyKeys = 64;
+constexpr int kManyMinSteps = 4;  // a piece is at least so many tiles of keys long
+
+template <class T>
+struct Pack4 {
+  typedef i16x4 V;
+};
+template <>
+struct Pack4<float> {
+  typedef f32x4 V;
+};
+
+template <class T, int DP, int NW>
+__global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
+  typedef typename Type<T>::Vec Vec;
+  typedef Tile<T, DP> L;
+  constexpr int NT = NW * kWave, ROWS = 32 * NW;
+  constexpr int KS = DP / 16;               // steps of the summed axis of q.k
+  constexpr int DT = DP / 32;               // tiles of output columns
+  constexpr int NC = DP / 8;                // chunks of eight values of a row
+  constexpr int CH = kManyKeys * NC / NT;   // chunks of K and of V that a thread carries
+  constexpr int RS = NT / NC;               // rows between two of them
+  extern __shared__ __align__(16) char raw[];
+  ManyShared<T, DP, NW> &sh = *reinterpret_cast<ManyShared<T, DP, NW> *>(raw);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 31, half = lane >> 5;
+  const int P = 1 << a.shift;
+  auto count = [&](int r, int &tiles, int &steps) {
+    const Request q = request_of(a, r);
+    const long long rows = (long long)q.n * a.G;
+    tiles = rows > a.few ? (int)((rows + ROWS - 1) / ROWS) : 0;
+    const int lo = a.window ? imax(q.S - q.n - a.window + 1, 0) : 0;
+    steps = (q.S - lo + kManyKeys - 1) / kManyKeys;
+  };
+  split_scan<NT>(sh.split, a, kManyMinSteps, count);
+  const int total = sh.split.total;
+  if (blockIdx.x == 0 && tid == 0) a.meta[0] = sh.split.total_split * a.Hkv;
+
+  for (unsigned p = blockIdx.x; p < (unsigned)total * (unsigned)a.Hkv; p += gridDim.x) {
+    const int h = (int)(p % (unsigned)a.Hkv);
+    const Piece pc = split_find<NT>(sh.split, a, (int)(p / (unsigned)a.Hkv), count);
+    if (pc.r < 0) continue;
+    const Request rq = request_of(a, pc.r);
+    const int before = rq.S - rq.n;  // position of the request's first token
+    const int first = pc.tile * ROWS, rows = imin(rq.n * a.G - first, ROWS);
+    const int pos_first = before + first / a.G, pos_last = before + (first + rows - 1) / a.G;
+    const int lo = a.window ? imax(pos_first - a.window + 1, 0) : 0;
+    const int hi = imin(pos_last + 1, rq.S);
+    const int tiles = hi > lo ? (hi - lo + kManyKeys - 1) / kManyKeys : 0;
+    const int t0 = (int)((long long)tiles * pc.part / pc.np), t1 = (int)((long long)tiles * (pc.part + 1) / pc.np);
+    const int32_t *table = a.table + (int64_t)pc.r * a.table_row;
+
+    // ------------------------------------------------ the queries, as columns
+    const int mine = first + wave * 32 + col;  // this lane's row of the request
+    const bool have_row = mine < first + rows;
+    const int rho = have_row ? mine : first;
+    const int tok = rq.first + rho / a.G, head = h * a.G + rho % a.G;
+    const int pos = before + rho / a.G;
+    const int wave_rows = imin(rows - wave * 32, 32);
+    const int wave_first = wave_rows > 0 ? before + (first + wave * 32) / a.G : 0;
+    const int wave_last = wave_rows > 0 ? before + (first + wave * 32 + wave_rows - 1) / a.G : -1;
+    Vec q[KS];
+    {
+      const T *src = (const T *)a.q + (int64_t)tok * a.q_token + (int64_t)head * a.q_head;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const int d = i * 16 + half * 8;
+        q[i] = load8<T>(have_row && d < a.D ? src + d : (const T *)kZeroRow);
+      }
+    }
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+    float m = kNegInf, l = 0.0f;
+
+    // ------------------------------------------------ K and V into LDS
+    auto find = [&](int t) {  // the page of key `lane` of tile t
+      const int u = lo + t * kManyKeys + lane;
+      int page = t < t1 && u < hi ? table[u >> a.shift] : -1;
+      return (unsigned)page < (unsigned)a.pages ? page : -1;
+    };
+    // a tile of which some of the block's rows see a part only
+    auto mixed = [&](int t) {
+      const int b = lo + t * kManyKeys;
+      return b + kManyKeys - 1 > pos_first || (a.window && b <= pos_last - a.window);
+    };
+    const int c8 = (tid % NC) * 8, row_of = tid / NC;
+    const bool in_row = c8 < a.D;
+    Vec kr[CH], vr[CH];
+    auto load = [&](int t, int page_lane) {
+      const int b = lo + t * kManyKeys;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int row = i * RS + row_of;
+        const int page = __shfl(page_lane, row);
+        const int64_t in = (b + row) & (P - 1);
+        const bool ok = page >= 0 && in_row;
+        const T *ks = (const T *)a.k + (int64_t)page * a.k_page + in * a.k_slot + (int64_t)h * a.k_head + c8;
+        const T *vs = (const T *)a.v + (int64_t)page * a.v_page + in * a.v_slot + (int64_t)h * a.v_head + c8;
+        kr[i] = load8<T>(ok ? ks : (const T *)kZeroRow);
+        vr[i] = load8<T>(ok ? vs : (const T *)kZeroRow);
+      }
+    };
+    auto store = [&](int t, int buf) {
+      if (mixed(t)) {
+        unsigned long long odd = 0;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          const unsigned long long b = __builtin_amdgcn_ballot_w64(clean8<T>(vr[i]));
+#pragma unroll
+          for (int g = 0; g < 64 / NC; ++g)
+            if ((b >> (g * NC)) & ((1ull << NC) - 1)) odd |= 1ull << (i * RS + wave * (64 / NC) + g);
+        }
+        if (lane == 0) sh.odd[buf][wave] = odd;
+      }
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const int at = L::at(i * RS + row_of, c8);
+        store8<T>(sh.k[buf] + at, kr[i]);
+        store8<T>(sh.v[buf] + at, vr[i]);
+      }
+    };
+
+    __syncthreads();  // the last piece's tiles are done with
+    int page = find(t0), page1 = find(t0 + 1), page2 = find(t0 + 2);
+    unsigned long long live = 0, live1 = __builtin_amdgcn_ballot_w64(page >= 0);
+    if (t0 < t1) {
+      load(t0, page);
+      store(t0, t0 & 1);
+      load(t0 + 1, page1);
+    }
+    __syncthreads();
+    for (int t = t0; t < t1; ++t) {
+      const int buf = t & 1;
+      live = live1;
+      live1 = __builtin_amdgcn_ballot_w64(page1 >= 0);
+      if (t + 1 < t1) {
+        store(t + 1, buf ^ 1);
+        load(t + 2, page2);
+      }
+      page1 = page2;
+      page2 = find(t + 3);
+      const int b = lo + t * kManyKeys;
+      if (b <= wave_last && (!a.window || b + kManyKeys - 1 > wave_first - a.window)) {
+        const T *kt = sh.k[buf], *vt = sh.v[buf];
+        // S^T = K Q^T
+        f32x16 x[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[s][j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+            x[s] = Type<T>::dot32(load8<T>(kt + L::at(s * 32 + col, i * 16 + half * 8)), q[i], x[s]);
+        const bool part_seen = b + kManyKeys - 1 > wave_first || (a.window && b <= wave_last - a.window);
+        if (part_seen || live != ~0ull) {
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const int key = s * 32 + 8 * (j >> 2) + 4 * half + (j & 3);
+              const bool seen = ((live >> key) & 1) && b + key <= pos && (!a.window || b + key > pos - a.window);
+              x[s][j] = seen ? x[s][j] : kNegInf;
+            }
+        }
+        float top = x[0][0];
+#pragma unroll
+        for (int j = 1; j < 32; ++j) top = fmaxf(top, x[j >> 4][j & 15]);
+        top = max_across_32(top);
+        const float mn = fmaxf(m, top);
+        const float ms = mn == kNegInf ? 0.0f : mn * a.scale2;
+        if (__builtin_amdgcn_ballot_w64(mn > m)) {
+          const float fade = exp2_of(m * a.scale2 - ms);
+          l *= fade;
+#pragma unroll
+          for (int i = 0; i < DT; ++i) o[i] *= fade;
+          m = mn;
+        }
+        Vec pv[4];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          const float e = exp2_of(__builtin_fmaf(x[j >> 4][j & 15], a.scale2, -ms));
+          l += e;
+          x[j >> 4][j & 15] = e;
+          // the weights go to the matrix cores in the type of V, their sum stays in fp32
+          pv[j >> 3][j & 7] = (T)e;
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            union {
+              Vec v;
+              T t[8];
+            } w;
+            const int row = s * 16 + half * 4, d0 = i * 32 + (lane & 16);
+            L::read4(vt, row, d0, lane, w.t);
+            L::read4(vt, row + 8, d0, lane, w.t + 4);
+            o[i] = Type<T>::dot32(w.v, pv[s], o[i]);
+          }
+        if (part_seen) {  // infinities and NaN of V, left out of the product above, to the rows that see them
+          unsigned long long odd = 0;
+#pragma unroll
+          for (int w = 0; w < NW; ++w) odd |= sh.odd[buf][w];
+          while (odd) {
+            const int key = __builtin_ctzll(odd);
+            odd &= odd - 1;
+            float e = 0.0f;
+            const int at = (key >> 5) * 16 + ((key >> 3) & 3) * 4 + (key & 3);
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (j == at) e = x[j >> 4][j & 15];
+            e = __shfl(e, ((key >> 2) & 1) * 32 + col);
+            const int u = b + key;
+            const bool seen = u <= pos && (!a.window || u > pos - a.window);
+            const T *vs = (const T *)a.v + (int64_t)table[u >> a.shift] * a.v_page +
+                          (int64_t)(u & (P - 1)) * a.v_slot + (int64_t)h * a.v_head;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const int d = i * 32 + 8 * (j >> 2) + 4 * half + (j & 3);
+                const float v = d < a.D ? (float)vs[d] : 0.0f;
+                if (seen && !(fabsf(v) < __builtin_inff())) o[i][j] += e * v;
+              }
+          }
+        }
+      }
+      __syncthreads();
+    }
+
+    // ------------------------------------------------ out, or to the join
+    l = sum_across_32(l);
+    if (l != l) m = __builtin_inff();  // NaN among the scores: the whole row is NaN
+    if (pc.slot >= 0) {
+      const int64_t s = (int64_t)pc.slot * a.Hkv + h;
+      float *dst = a.part + s * (ROWS * (DP + 2));
+      const int i = wave * 32 + col;
+      if (have_row) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<f32x4 *>(dst + (int64_t)i * DP + t * 32 + j * 8 + half * 4) =
+                f32x4{o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+        if (half == 0) {
+          dst[ROWS * DP + i * 2] = m;
+          dst[ROWS * DP + i * 2 + 1] = l;
+        }
+      }
+      if (tid == 0) {
+        int32_t *mt = a.meta + (1 + s) * kMeta;
+        mt[0] = pc.part == 0 ? pc.np : 0;
+        mt[1] = rq.first * a.G + first;
+        mt[2] = rows;
+        mt[3] = h;
+      }
+    } else if (have_row) {
+      const float inv = m == kNegInf ? 0.0f : 1.0f / l;
+      T *dst = (T *)a.out + ((int64_t)tok * a.Hq + head) * a.D;
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int d = t * 32 + j * 8 + half * 4;
+          if (d < a.D) {
+            union {
+              T t[4];
+              typename Pack4<T>::V v;
+            } w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w.t[k] = (T)(m == kNegInf ? 0.0f : o[t][4 * j + k] * inv);
+            *reinterpret_cast<typename Pack4<T>::V *>(dst + d) = w.v;
+          }
+        }
+      if (half == 0 && a.lse)
+        a.lse[(int64_t)tok * a.Hq + head] = m == kNegInf ? kNegInf : m * (a.scale2 * kLn2) + __logf(l);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ the join
+//
+// Adds the pieces of one row of a split tile: the largest of their maxima, their
+// sums and values rescaled to it, in the order of the pieces.  One block per
+// piece's slot and row (or every gridDim.y-th row); blocks whose slot is not a
+// tile's first piece leave at once.  The pieces of a tile are Hkv slots apart.
+
+constexpr int kJoinBlock = 256;
+
+template <class T, int DP>
+__global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
+  constexpr int ROWS = kFewRows;
+  constexpr int kLanes = DP / 4;                    // threads of a row
+  constexpr int kSide = kJoinBlock / kLanes;        // pieces side by side
+  __shared__ float acc[kSide][DP];
+  __shared__ float weight[kJoinBlock];
+  __shared__ float red[2][kJoinBlock / kWave];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t s = blockIdx.x;
+  if (s >= a.meta[0]) return;
+  const int32_t *mt = a.meta + (1 + s) * kMeta;
+  const int np = mt[0];
+  if (np <= 1) return;
+  constexpr int64_t kSize = (int64_t)ROWS * (DP + 2);
+  const float *part = a.part + s * kSize;
+  const int64_t next = (int64_t)a.Hkv * kSize;
+  for (int i = blockIdx.y; i < mt[2]; i += gridDim.y) {
+    const float *ml = part + ROWS * DP + i * 2;
+    float mx = kNegInf;
+    for (int j = tid; j < np; j += kJoinBlock) mx = fmaxf(mx, ml[j * next]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if (lane == 0) red[0][wave] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinBlock / kWave; ++w) mx = fmaxf(mx, red[0][w]);
+    const int c = (tid % kLanes) * 4, g = tid / kLanes;
+    f32x4 o{0, 0, 0, 0};
+    float sum = 0.0f;
+    for (int j0 = 0; j0 < np; j0 += kJoinBlock) {
+      const int j = j0 + tid;
+      float w = 0.0f;
+      if (j < np) {
+        const float mj = ml[j * next];
+        w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * a.scale2);
+        sum += w == 0.0f ? 0.0f : w * ml[j * next + 1];
+      }
+      __syncthreads();
+      weight[tid] = w;
+      __syncthreads();
+      const int n = imin(np - j0, kJoinBlock);
+#pragma unroll 8
+      for (int k = g; k < n; k += kSide) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (j0 + k) * next + i * DP + c);
+        const float f = weight[k];
+        if (f != 0.0f) o += x * f;
+      }
+    }
+#pragma unroll
+    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+    if (lane == 0) red[1][wave] = sum;
+    *reinterpret_cast<f32x4 *>(&acc[g][c]) = o;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinBlock / kWave; ++w) sum += red[1][w];
+    const int row = mt[1] + i, t = row / a.G, hd = mt[3] * a.G + row % a.G;
+    const int64_t at = (int64_t)t * a.Hq + hd;
+    if (tid < a.D) {
+      float v = 0.0f;
+#pragma unroll
+      for (int k = 0; k < kSide; ++k) v += acc[k][tid];
+      ((T *)a.out)[at * a.D + tid] = (T)(mx == kNegInf ? 0.0f : v / sum);
+    }
+    if (tid == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (a.scale2 * kLn2) + __logf(sum);
+    __syncthreads();
+  }
+}
+
+// The same for the tiles of attend_many: many rows of few pieces, a wave per row.
+constexpr int kJoinRows = 32;  // rows of a block, one after the other in its four waves
+
+template <class T, int DP, int ROWS>
+__global__ __launch_bounds__(kJoinBlock) void join_many(AttendArgs a) {
+  constexpr int C = DP / 64;  // columns of a lane
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t s = blockIdx.x;
+  if (s >= a.meta[0]) return;
+  const int32_t *mt = a.meta + (1 + s) * kMeta;
+  const int np = mt[0], rows = mt[2];
+  if (np <= 1) return;
+  constexpr int64_t kSize = (int64_t)ROWS * (DP + 2);
+  const int64_t next = (int64_t)a.Hkv * kSize;
+  for (int i = blockIdx.y * kJoinRows + wave; i < rows && i < (int)(blockIdx.y + 1) * kJoinRows;
+       i += kJoinBlock / kWave) {
+    const float *part = a.part + s * kSize + i * DP + lane * C;
+    const float *ml = a.part + s * kSize + ROWS * DP + i * 2;
+    float mx = kNegInf;
+    for (int j = lane; j < np; j += kWave) mx = fmaxf(mx, ml[j * next]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    float sum = 0.0f, o[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = 0.0f;
+#pragma unroll 4
+    for (int j = 0; j < np; ++j) {
+      const float mj = ml[j * next], lj = ml[j * next + 1];
+      const float w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * a.scale2);
+      float x[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c) x[c] = part[j * next + c];
+      if (w != 0.0f) {
+        sum += w * lj;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] += w * x[c];
+      }
+    }
+    const int row = mt[1] + i, t = row / a.G, hd = mt[3] * a.G + row % a.G;
+    const int64_t at = (int64_t)t * a.Hq + hd;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (lane * C + c < a.D) ((T *)a.out)[at * a.D + lane * C + c] = (T)(mx == kNegInf ? 0.0f : o[c] / sum);
+    if (lane == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (a.scale2 * kLn2) + __logf(sum);
+  }
+}
+
+}  // namespace paged
+}  // namespace slnr

@@ -1,0 +1,20 @@
+// What the entry points of the paged cache share with the rest of the library:
+// the record of HIP errors, the device's facts and the workspaces per (device,
+// stream, slot) that sparselnr_release() frees.  Defined in csrc/sparselnr.hip.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+
+namespace slnr {
+
+// Workspace slots of these operators (0 to 2 belong to the sparse products).
+enum WorkspaceSlot { kSlotAttend = 3 };
+
+int hip_error(hipError_t e);  // records e for the calling thread; SPARSELNR_ERR_HIP
+int this_device(int *dev);
+int device_cu_count(int dev, int *cus);
+int stream_workspace(int dev, hipStream_t stream, size_t bytes, void **out, int slot);
+
+}  // namespace slnr

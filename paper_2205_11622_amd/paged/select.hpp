@@ -1,0 +1,270 @@
+// Which pages a query attends: a cheap score of every page and an exact top-k.
+#pragma once
+
+#include "common.hpp"
+
+namespace slnr {
+namespace paged {
+
+struct SelectArgs {
+  const void *q;  // [T][Hq][D]
+  int64_t q_token, q_head;
+  const int8_t *kq;     // [pages][Hkv][D]
+  const float *kscale;  // [pages][Hkv]
+  const int32_t *table;
+  int64_t table_row;
+  const int32_t *seq, *qptr;
+  int32_t *sel;  // [T][Hkv][top]
+  int32_t R, T, W, pages, shift, Hkv, G, D, top, first, local;
+  int32_t capacity;  // entries of a row in LDS: top carried ones, then a segment of pages
+};
+
+constexpr int kSelectWaves = 16;
+constexpr int kSelectBlock = kSelectWaves * kWave;
+constexpr int kSelectMaxTop = 256;
+
+// Keys that order as the scores do, as unsigned numbers: 0 is no page, ~0 one that
+// is always taken.  NaN ranks above every number.
+__device__ __forceinline__ unsigned rank_of(float s) {
+  if (s != s) s = 3.402823466e38f;
+  s = fminf(fmaxf(s, -3.402823466e38f), 3.402823466e38f) + 0.0f;  // -0 and 0 are one score
+  const unsigned b = __float_as_uint(s);
+  return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+
+// Scores: the group's query heads are added up in 64 bits, rounded once and cut to
+// 8 bits; its product with a page's 8-bit mean key is a whole number below 2^24,
+// exact on the integer matrix cores, and the page's step makes it the score.  So a
+// score has one rounding, in no order, and equal scores are equal numbers.
+//
+// A block takes TM tokens of one request and one KV head: 16 (rows of the 16 x 16
+// x 64 products, one wave per token in the choice) or one (a decode step: all 16 waves
+// share the choice).  Scores stay in LDS as keys; a longer context is taken in
+// segments, the best so far carried in front of the next one, which keeps the
+// order of the indices.  The choice finds the k-th largest key bit by bit, a count
+// over the row per bit, and stops at the first prefix that exactly k keys reach;
+// equal keys at the end go by the lowest index.
+//
+// NR: keys of a row that a lane holds in the choice.
+template <class T, int DP, int TM, int NR>
+__global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
+  constexpr int KS = DP / 64;
+  constexpr int WPR = kSelectWaves / TM;  // waves of a row in the choice
+  static_assert(TM == 1 || TM == kSelectWaves, "one wave per token, or all for one");
+  extern __shared__ __align__(16) char raw[];
+  const int stride = a.capacity + 4;
+  unsigned *keys = reinterpret_cast<unsigned *>(raw);               // [TM][stride]
+  int *carried = reinterpret_cast<int *>(keys + TM * stride);       // [TM][top], indices
+  int8_t *q8 = reinterpret_cast<int8_t *>(carried + TM * a.top + ((-TM * a.top) & 3));  // [16][DP + 16]
+  constexpr int QS = DP + 16;
+  int *count = reinterpret_cast<int *>(q8 + 16 * QS);               // [2][16] of the waves
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int col = lane & 15, grp = lane >> 4;
+  const int h = blockIdx.y;
+
+  // ------------------------------------------------------ which tokens
+  // TM = 16: request r's tiles begin at number floor(qptr[r] / 16) + r, which leaves
+  // room for all of them and never runs back.  TM = 1: token by token.
+  const int id = blockIdx.x;
+  auto start = [&](int r) {
+    int b = a.qptr[r];
+    b = b < 0 ? 0 : b > a.T ? a.T : b;
+    return TM == 1 ? b : b / TM + r;
+  };
+  int x = 0, y = a.R - 1;
+  while (x < y) {
+    const int mid = (x + y + 1) >> 1;
+    if (start(mid) <= id)
+      x = mid;
+    else
+      y = mid - 1;
+  }
+  const int r = x;
+  int qb = a.qptr[r], qe = a.qptr[r + 1];
+  qb = qb < 0 ? 0 : qb > a.T ? a.T : qb;
+  qe = qe < 0 ? 0 : qe > a.T ? a.T : qe;
+  const int t0 = qb + (id - start(r)) * TM;
+  if (id < start(r) || t0 >= qe) return;
+  const int tokens = qe - t0 < TM ? qe - t0 : TM;
+  const int seq = a.seq[r];
+  const int pos0 = seq - (qe - qb) + (t0 - qb);  // position of the first token
+  const int pos1 = pos0 + tokens - 1;
+  const int32_t *table = a.table + (int64_t)r * a.table_row;
+  const int near1 = pos1 < 0 ? -1 : pos1 >> a.shift;
+  const int blocks = near1 + 1 < a.W ? near1 + 1 : a.W;
+
+  // ------------------------------------------------------ the queries in 8 bits
+  if (wave < TM) {  // a wave per token
+    float u[DP / 64];
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i) {
+      const int d = i * 64 + lane;
+      double s = 0;
+      if (wave < tokens && d < a.D) {
+        const T *src = (const T *)a.q + (int64_t)(t0 + wave) * a.q_token + (int64_t)h * a.G * a.q_head + d;
+        for (int g = 0; g < a.G; ++g) s += (double)(float)src[g * a.q_head];
+      }
+      u[i] = (float)s;
+      const float z = fabsf(u[i]);
+      most = z <= 3.402823466e38f ? fmaxf(most, z) : __builtin_inff();
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    const bool fine = most < __builtin_inff();
+    const float step = most * kStep127;
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i)
+      q8[wave * QS + i * 64 + lane] = fine && step > 0.0f ? whole8(u[i], step) : (int8_t)0;
+  }
+  if (TM == 1)  // the other columns of the product are not used
+    for (int i = tid; i < 15 * QS; i += kSelectBlock) q8[QS + i] = 0;
+  __syncthreads();
+  i32x4 qv[KS];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) qv[i] = *reinterpret_cast<const i32x4 *>(q8 + col * QS + i * 64 + grp * 16);
+
+  const int my_token = TM == 1 ? 0 : wave;                   // row of the choice
+  const int room = a.capacity - a.top;                       // pages of a segment
+  int held = 0;                                              // carried entries of my row
+  for (int seg = 0; seg == 0 || seg < blocks; seg += room) {
+    const int n = blocks - seg < room ? (blocks - seg > 0 ? blocks - seg : 0) : room;
+    // ---------------------------------------------------- scores of a segment
+    for (int b0 = wave * 16; b0 < n; b0 += kSelectWaves * 16) {
+      const int b = seg + b0 + col;
+      int page = b < blocks ? table[b] : -1;
+      if ((unsigned)page >= (unsigned)a.pages) page = -1;
+      const int8_t *src = a.kq + ((int64_t)(page < 0 ? 0 : page) * a.Hkv + h) * a.D;
+      i32x4 acc{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const int d = i * 64 + grp * 16;
+        union {
+          i32x4 v;
+          uint2 u[2];
+        } w;
+        w.u[0] = *reinterpret_cast<const uint2 *>(d < a.D ? src + d : (const int8_t *)kZeroRow);
+        w.u[1] = *reinterpret_cast<const uint2 *>(d + 8 < a.D ? src + d + 8 : (const int8_t *)kZeroRow);
+        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w.v, qv[i], acc, 0, 0, 0);
+      }
+      const float scale = page < 0 ? 0.0f : a.kscale[(int64_t)page * a.Hkv + h];
+      unsigned k4[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int from = grp * 4 + i;  // page of row 4 grp + i
+        const float sc = __shfl(scale, from);
+        const int pg = __shfl(page, from);
+        const int bb = seg + b0 + from;
+        const int p = pos0 + col;
+        const int near = p < 0 ? -1 : p >> a.shift;
+        unsigned key = rank_of(__fmul_rn((float)acc[i], sc));
+        if (bb < a.first || bb > near - a.local) key = ~0u;
+        if (pg < 0 || bb > near) key = 0;
+        k4[i] = key;
+      }
+      if (col < TM) {
+        unsigned *dst = keys + col * stride + a.top + b0 + grp * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (b0 + grp * 4 + i < n) dst[i] = k4[i];
+      }
+    }
+    __syncthreads();
+
+    // ---------------------------------------------------- the best of carried and new
+    // Entries: the carried ones at [top - held, top), then the segment's n.
+    unsigned *row = keys + my_token * stride;
+    int *names = carried + my_token * a.top;
+    const int first_entry = a.top - held, entries = held + n;
+    const int base = TM == 1 ? wave * (NR * kWave) : 0;  // a wave's entries are one run of them
+    unsigned v[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int e = base + i * kWave + lane;
+      v[i] = e < entries ? row[first_entry + e] : 0;
+    }
+    // Keys of the row that are at least `than`.
+    int turn = 0;
+    auto at_least = [&](unsigned than) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) c += __popcll(__builtin_amdgcn_ballot_w64(v[i] >= than));
+      if constexpr (WPR > 1) {
+        if (lane == 0) count[turn * kSelectWaves + wave] = c;
+        __syncthreads();
+        c = 0;
+#pragma unroll
+        for (int w = 0; w < kSelectWaves; ++w) c += count[turn * kSelectWaves + w];
+        turn ^= 1;
+      }
+      return c;
+    };
+    unsigned cut = 1;  // keys from here on are taken
+    int reach = at_least(1);
+    if (reach > a.top) {
+      cut = 0;
+      for (int bit = 31; bit >= 0 && reach != a.top; --bit) {
+        const unsigned next = cut | (1u << bit);
+        const int c = at_least(next);
+        if (c >= a.top) cut = next, reach = c;
+      }
+    }
+    const int over = reach > a.top ? at_least(cut + 1) : reach;  // cut < ~0: fewer than top are forced
+    const int ties = reach > a.top ? a.top - over : reach;       // keys equal to cut that are taken, lowest first
+    const bool cut_ties = reach > a.top;
+    // taken and tied entries before this wave's
+    int out = 0, tied = 0;
+    if constexpr (WPR > 1) {
+      int c = 0, e = 0;
+#pragma unroll
+      for (int i = 0; i < NR; ++i) {
+        c += __popcll(__builtin_amdgcn_ballot_w64(cut_ties ? v[i] > cut : v[i] >= cut));
+        e += __popcll(__builtin_amdgcn_ballot_w64(cut_ties && v[i] == cut));
+      }
+      __syncthreads();
+      if (lane == 0) count[wave] = c, count[kSelectWaves + wave] = e;
+      __syncthreads();
+      for (int w = 0; w < wave; ++w) out += count[w], tied += count[kSelectWaves + w];
+      out += tied < ties ? tied : ties;
+    }
+    // names of the entries, before the carried ones are written over
+    int name[NR];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int e = base + i * kWave + lane;
+      name[i] = e < held ? names[e] : seg + (e - held);
+    }
+    if constexpr (WPR > 1) __syncthreads();
+    const bool last = seg + room >= blocks;
+    int taken = out;
+    int32_t *dst = a.sel + ((int64_t)(t0 + my_token) * a.Hkv + h) * a.top;
+    const bool mine = my_token < tokens;
+    const int kept = reach > a.top ? a.top : reach;  // entries that the row keeps
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const bool eq = cut_ties && v[i] == cut;
+      const unsigned long long be = __builtin_amdgcn_ballot_w64(eq);
+      const unsigned long long below = (1ull << lane) - 1;
+      const bool take = (cut_ties ? v[i] > cut : v[i] >= cut) || (eq && tied + __popcll(be & below) < ties);
+      const unsigned long long b = __builtin_amdgcn_ballot_w64(take);
+      if (take) {
+        const int at = taken + __popcll(b & below);
+        if (last) {
+          if (mine) dst[at] = name[i];
+        } else {
+          names[at] = name[i];
+          row[a.top - kept + at] = v[i];
+        }
+      }
+      taken += __popcll(b);
+      tied += __popcll(be);
+    }
+    if (last && mine)
+      for (int e = kept + (TM == 1 ? tid : lane); e < a.top; e += TM == 1 ? kSelectBlock : kWave) dst[e] = -1;
+    held = kept;
+    __syncthreads();
+  }
+}
+
+}  // namespace paged
+}  // namespace slnr
