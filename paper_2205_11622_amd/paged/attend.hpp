@@ -36,6 +36,14 @@ constexpr int kMeta = 4;
 __device__ __forceinline__ int imin(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int imax(int a, int b) { return a > b ? a : b; }
 
+// Scores are kept as they come out of q.k and scaled inside the exponent, exp2(s c - m c),
+// except in fp32: there s c comes first, so that the largest weight is exactly one.
+// Maxima are in the same unit; this is what takes it to the exponent of two.
+template <class T>
+__device__ __forceinline__ float score_unit(const AttendArgs &a) {
+  return sizeof(T) == 4 ? 1.0f : a.scale2;
+}
+
 struct Request {
   int first, n, S;  // first token, tokens, visible length
 };
@@ -199,6 +207,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
   constexpr int DT = DP / 16;   // tiles of output columns
   extern __shared__ __align__(16) char raw[];
   FewShared<T, DP> &sh = *reinterpret_cast<FewShared<T, DP> *>(raw);
+  const float sc = score_unit<T>(a);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, grp = lane >> 4;
   const int row_tiles = (a.G + kFewRows - 1) / kFewRows;  // sparse form: of one token
@@ -361,6 +370,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
         x[s] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < KS; ++i) x[s] = Type<T>::dot16(kr[s][i], q[i], x[s]);
+        if constexpr (sizeof(T) == 4) x[s] *= a.scale2;
       }
       // Rows of several tokens see different keys.  A key that some rows see and
       // others do not must not reach the latter through 0 * inf: infinite and
@@ -404,14 +414,14 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
       for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
       top = max_across_16(top);
       const float mn = fmaxf(m, top);
-      const float ms = mn == kNegInf ? 0.0f : mn * a.scale2;  // nothing seen yet: exp2(-inf - 0) = 0
-      const float fade = exp2_of(m * a.scale2 - ms);          // 0 at the first key seen
+      const float ms = mn == kNegInf ? 0.0f : mn * sc;  // nothing seen yet: exp2(-inf - 0) = 0
+      const float fade = exp2_of(m * sc - ms);          // 0 at the first key seen
       m = mn;
       l *= fade;
       Vec pv;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float e = exp2_of(__builtin_fmaf(x[i >> 2][i & 3], a.scale2, -ms));
+        const float e = exp2_of(__builtin_fmaf(x[i >> 2][i & 3], sc, -ms));
         l += e;
         x[i >> 2][i & 3] = e;
         // the weights go to the matrix cores in the type of V, their sum stays in fp32
@@ -463,7 +473,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) mall = fmaxf(mall, sh.m[w][col]);
     {
-      const float f = m == kNegInf ? 0.0f : exp2_of((m - mall) * a.scale2);
+      const float f = m == kNegInf ? 0.0f : exp2_of((m - mall) * sc);
 #pragma unroll
       for (int i = 0; i < DT; ++i)
         *reinterpret_cast<f32x4 *>(&sh.o[wave][col * DP + i * 16 + grp * 4]) = m == kNegInf ? f32x4{0, 0, 0, 0} : o[i] * f;
@@ -477,7 +487,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
       for (int w = 0; w < kFewWaves; ++w) mx = fmaxf(mx, sh.m[w][i]);
 #pragma unroll
       for (int w = 0; w < kFewWaves; ++w)
-        sum += sh.m[w][i] == kNegInf ? 0.0f : sh.l[w][i] * exp2_of((sh.m[w][i] - mx) * a.scale2);
+        sum += sh.m[w][i] == kNegInf ? 0.0f : sh.l[w][i] * exp2_of((sh.m[w][i] - mx) * sc);
       f32x4 lo4{0, 0, 0, 0}, hi4{0, 0, 0, 0};
 #pragma unroll
       for (int w = 0; w < kFewWaves; ++w) {
@@ -507,7 +517,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
           store8<T>((T *)a.out + ((int64_t)t * a.Hq + hd) * a.D + d, w);
         }
         if (d == 0 && a.lse)
-          a.lse[(int64_t)t * a.Hq + hd] = mx == kNegInf ? kNegInf : mx * (a.scale2 * kLn2) + __logf(sum);
+          a.lse[(int64_t)t * a.Hq + hd] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
       }
     }
     if (slot >= 0 && tid == 0) {
@@ -561,6 +571,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
   constexpr int RS = NT / NC;               // rows between two of them
   extern __shared__ __align__(16) char raw[];
   ManyShared<T, DP, NW> &sh = *reinterpret_cast<ManyShared<T, DP, NW> *>(raw);
+  const float sc = score_unit<T>(a);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 31, half = lane >> 5;
   const int P = 1 << a.shift;
@@ -695,6 +706,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
 #pragma unroll
           for (int s = 0; s < 2; ++s)
             x[s] = Type<T>::dot32(load8<T>(kt + L::at(s * 32 + col, i * 16 + half * 8)), q[i], x[s]);
+        if constexpr (sizeof(T) == 4) x[0] *= a.scale2, x[1] *= a.scale2;
         const bool part_seen = b + kManyKeys - 1 > wave_first || (a.window && b <= wave_last - a.window);
         if (part_seen || live != ~0ull) {
 #pragma unroll
@@ -711,9 +723,9 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
         for (int j = 1; j < 32; ++j) top = fmaxf(top, x[j >> 4][j & 15]);
         top = max_across_32(top);
         const float mn = fmaxf(m, top);
-        const float ms = mn == kNegInf ? 0.0f : mn * a.scale2;
+        const float ms = mn == kNegInf ? 0.0f : mn * sc;
         if (__builtin_amdgcn_ballot_w64(mn > m)) {
-          const float fade = exp2_of(m * a.scale2 - ms);
+          const float fade = exp2_of(m * sc - ms);
           l *= fade;
 #pragma unroll
           for (int i = 0; i < DT; ++i) o[i] *= fade;
@@ -722,7 +734,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
         Vec pv[4];
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
-          const float e = exp2_of(__builtin_fmaf(x[j >> 4][j & 15], a.scale2, -ms));
+          const float e = exp2_of(__builtin_fmaf(x[j >> 4][j & 15], sc, -ms));
           l += e;
           x[j >> 4][j & 15] = e;
           // the weights go to the matrix cores in the type of V, their sum stays in fp32
@@ -817,7 +829,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
           }
         }
       if (half == 0 && a.lse)
-        a.lse[(int64_t)tok * a.Hq + head] = m == kNegInf ? kNegInf : m * (a.scale2 * kLn2) + __logf(l);
+        a.lse[(int64_t)tok * a.Hq + head] = m == kNegInf ? kNegInf : m * (sc * kLn2) + __logf(l);
     }
   }
 }
@@ -839,6 +851,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
   __shared__ float acc[kSide][DP];
   __shared__ float weight[kJoinBlock];
   __shared__ float red[2][kJoinBlock / kWave];
+  const float sc = score_unit<T>(a);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t s = blockIdx.x;
   if (s >= a.meta[0]) return;
@@ -866,7 +879,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
       float w = 0.0f;
       if (j < np) {
         const float mj = ml[j * next];
-        w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * a.scale2);
+        w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
         sum += w == 0.0f ? 0.0f : w * ml[j * next + 1];
       }
       __syncthreads();
@@ -896,7 +909,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
       for (int k = 0; k < kSide; ++k) v += acc[k][tid];
       ((T *)a.out)[at * a.D + tid] = (T)(mx == kNegInf ? 0.0f : v / sum);
     }
-    if (tid == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (a.scale2 * kLn2) + __logf(sum);
+    if (tid == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
     __syncthreads();
   }
 }
@@ -907,6 +920,7 @@ constexpr int kJoinRows = 32;  // rows of a block, one after the other in its fo
 template <class T, int DP, int ROWS>
 __global__ __launch_bounds__(kJoinBlock) void join_many(AttendArgs a) {
   constexpr int C = DP / 64;  // columns of a lane
+  const float sc = score_unit<T>(a);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t s = blockIdx.x;
   if (s >= a.meta[0]) return;
@@ -929,7 +943,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_many(AttendArgs a) {
 #pragma unroll 4
     for (int j = 0; j < np; ++j) {
       const float mj = ml[j * next], lj = ml[j * next + 1];
-      const float w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * a.scale2);
+      const float w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
       float x[C];
 #pragma unroll
       for (int c = 0; c < C; ++c) x[c] = part[j * next + c];
@@ -944,7 +958,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_many(AttendArgs a) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
       if (lane * C + c < a.D) ((T *)a.out)[at * a.D + lane * C + c] = (T)(mx == kNegInf ? 0.0f : o[c] / sum);
-    if (lane == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (a.scale2 * kLn2) + __logf(sum);
+    if (lane == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
   }
 }
 

@@ -1,0 +1,606 @@
+"""The paged-cache operators on the GPU against their definitions in 64 bits."""
+import math
+import random
+
+import pytest
+import torch
+
+import paper_2205_11622_amd as slnr
+from tests import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def vmax(b):
+    return float(b.vc.float().nan_to_num(0.0, 0.0, 0.0).abs().max()) if b.vc.numel() else 0.0
+
+
+def run_attention(b, gpu, window=0, max_new=0, scale=None, with_lse=True, fill=None):
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    lse = torch.full(q.shape[:2], math.nan, device=gpu) if with_lse else None
+    out = torch.full(q.shape, 0 if fill is None else fill, dtype=q.dtype, device=gpu)
+    got = slnr.sparselnr_paged_attention(q, kc, vc, table, seq, qptr, scale=scale, window=window, max_new=max_new,
+                                         out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert got is out
+    return out.cpu(), lse
+
+
+def compare(b, gpu, window=0, max_new=0, scale=None, logits=8.0):
+    out, lse = run_attention(b, gpu, window, max_new, scale)
+    D = b.q.shape[2]
+    pu.check(out, lse, b.reference(scale, window), b.dtype, max(b.seq + [1]), D, vmax(b), logits)
+    return out, lse
+
+
+# ------------------------------------------------------------- attention
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D", [8, 64, 72, 128, 136, 256])
+def test_decode_types_and_widths(gpu, dtype, D):
+    b = pu.Batch([0, 1, 15, 16, 17, 63, 200, 333], [1] * 8, 6, 2, D, 16, dtype, seed=D)
+    print(dtype, D, flush=True)
+    compare(b, gpu, max_new=1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D", [8, 64, 72, 128, 136, 256])
+def test_chunk_types_and_widths(gpu, dtype, D):
+    b = pu.Batch([0, 5, 130], [70, 1, 301], 4, 2, D, 32, dtype, seed=D + 1)
+    print(dtype, D, flush=True)
+    compare(b, gpu)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (3, 3), (5, 1), (7, 1), (12, 4), (16, 2), (17, 1), (40, 2), (64, 1)])
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_head_layouts(gpu, Hq, Hkv, new):
+    b = pu.Batch([100, 0, 37], [new, 1, new], Hq, Hkv, 64, 16, BF16, seed=Hq)
+    print(Hq, Hkv, new, flush=True)
+    compare(b, gpu, max_new=max(new, 1))
+
+
+@pytest.mark.parametrize("P", [1, 2, 8, 16, 64, 128, 1024])
+@pytest.mark.parametrize("order", ["slots", "heads", "pairs"])
+def test_page_sizes_and_orders(gpu, P, order):
+    b = pu.Batch([0, 130, 65], [1, 2, 140], 8, 2, 64, P, BF16, seed=P, order=order)
+    print(P, order, flush=True)
+    compare(b, gpu)
+
+
+@pytest.mark.parametrize("window", [1, 2, 31, 64, 100, 5000])
+@pytest.mark.parametrize("new", [1, 5, 150])
+def test_windows(gpu, window, new):
+    b = pu.Batch([0, 3, 400], [new, new, new], 4, 2, 64, 16, FP16, seed=window)
+    print(window, new, flush=True)
+    compare(b, gpu, window=window)
+
+
+def test_requests_without_tokens_and_lengths_of_none(gpu):
+    b = pu.Batch([0, 7, 0, 0, 20], [0, 0, 1, 0, 2], 4, 1, 64, 16, BF16, seed=2)
+    compare(b, gpu)
+    b = pu.Batch([4, 9], [0, 0], 4, 1, 64, 16, BF16, seed=2)
+    out, _ = run_attention(b, gpu)  # no tokens at all
+    assert out.shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("new", [1, 4, 90])
+def test_pages_that_are_not_there(gpu, new):
+    b = pu.Batch([300, 64, 10], [new] * 3, 8, 2, 64, 16, BF16, seed=5)
+    for j in (0, 3, 4, 11):
+        b.table[0][j] = -1
+    b.table[1] = [-1] * len(b.table[1])  # nothing left: empty rows
+    b.table[2][0] = b.kc.shape[0]        # past the cache
+    out, lse = compare(b, gpu)
+    a, e = b.qptr[1], b.qptr[2]
+    assert (out[a:e] == 0).all() and (lse[a:e] == -math.inf).all()
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_lengths_that_do_not_fit_stay_in_bounds(gpu, new):
+    """seq_len past the table's row ends there; more new tokens than positions: the first see nothing."""
+    b = pu.Batch([40, 40], [new, new], 4, 2, 64, 16, FP32, seed=6, extra_w=0)
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    W = table.shape[1]
+    big = torch.tensor([2 ** 31 - 1, b.seq[1]], dtype=torch.int32, device=gpu)
+    full = pu.Batch([W * 16 - new, 40], [new, new], 4, 2, 64, 16, FP32, seed=6, extra_w=0)
+    full.kc, full.vc, full.q, full.table = b.kc.nan_to_num(0), b.vc.nan_to_num(0), b.q, b.table
+    kc0, vc0 = kc.nan_to_num(0), vc.nan_to_num(0)
+    out = slnr.sparselnr_paged_attention(q, kc0, vc0, table, big, qptr).cpu()
+    pu.check(out, None, full.reference(), FP32, W * 16, 64, vmax(b))
+    # one position, `new` tokens
+    one = torch.tensor([1, 1], dtype=torch.int32, device=gpu)
+    lse = torch.empty(q.shape[:2], device=gpu)
+    out = slnr.sparselnr_paged_attention(q, kc0, vc0, table, one, qptr, lse=lse).cpu()
+    for r in range(2):
+        a, e = b.qptr[r], b.qptr[r + 1]
+        assert (out[a:e - 1] == 0).all() and (lse[a:e - 1] == -math.inf).all()
+        v = b.vc[b.table[r][0], 0].repeat_interleave(2, 0)
+        assert torch.equal(out[e - 1], v)  # one key: its value
+
+
+@pytest.mark.parametrize("what", ["tokens past T", "backwards", "negative"])
+def test_offsets_that_do_not_fit_stay_in_bounds(gpu, what):
+    b = pu.Batch([30, 30], [3, 3], 4, 2, 64, 16, BF16, seed=7)
+    q, kc, vc, table, seq, _ = b.upload(gpu)
+    qptr = {"tokens past T": [0, 3, 100], "backwards": [0, 6, 3], "negative": [-5, 3, 6]}[what]
+    out = torch.full(q.shape, 7.0, dtype=BF16, device=gpu)
+    slnr.sparselnr_paged_attention(q, kc, vc, table, seq, b.ints(qptr, gpu), out=out)
+    sel = slnr.sparselnr_block_select(q, torch.zeros(kc.shape[0], 2, 64, dtype=torch.int8, device=gpu),
+                                      torch.ones(kc.shape[0], 2, device=gpu), table, seq, b.ints(qptr, gpu), 16, 2)
+    slnr.sparselnr_block_attention(q, kc, vc, table, seq, b.ints(qptr, gpu), sel.clamp(-1, 1), out=out)
+    torch.cuda.synchronize()
+
+
+def test_rows_of_no_request_are_left(gpu):
+    b = pu.Batch([30, 5], [2, 100], 4, 2, 64, 16, BF16, seed=8)
+    b.q = torch.cat([b.q, b.q[:5]])
+    b.qkv = b.q
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    out = torch.full(q.shape, 7.0, dtype=BF16, device=gpu)
+    slnr.sparselnr_paged_attention(q, kc, vc, table, seq, qptr, out=out)
+    assert (out[102:] == 7).all() and not (out[:102] == 7).all(dim=2).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("new", [3, 9, 130])
+@pytest.mark.parametrize("window", [0, 40])
+def test_infinities_and_nan_where_a_query_does_not_look(gpu, dtype, new, window):
+    """Rows of the newest tokens that hold inf and NaN reach the tokens that see
+    them, in the columns that have them, and no other."""
+    b = pu.Batch([61, 0], [new, new], 4, 2, 64, 16, dtype, seed=9)
+    ref, _, _ = b.reference(window=window)
+    S = b.seq[0]
+    bad = [(S - 1, 3, math.nan), (S - 2, 5, math.inf), (S - 2, 6, -math.inf)]
+    for j, d, x in bad:
+        b.vc[b.table[0][j // 16], j % 16, :, d] = x
+    old = 4  # and, with a window, one that only the first tokens still see
+    if window:
+        b.vc[b.table[0][old // 16], old % 16, :, 7] = math.inf
+    b.kc[b.table[0][(S - 1) // 16], (S - 1) % 16, 1, :] = math.nan  # key of the last token, second head
+    out, _ = run_attention(b, gpu, window=window)
+    pos = torch.arange(61, S)
+    for i, p in enumerate(pos.tolist()):
+        o = out[i].float()
+        nan_head = p == S - 1
+        assert torch.isnan(o[2:, :]).all() == nan_head
+        for h in range(0, 2 if nan_head else 4):
+            assert bool(torch.isnan(o[h, 3])) == (p >= S - 1), (i, h)
+            assert bool(o[h, 5] == math.inf) == (p >= S - 2), (i, h)
+            assert bool(o[h, 6] == -math.inf) == (p >= S - 2), (i, h)
+            if window:
+                assert bool(o[h, 7] == math.inf) == (p - old < window), (i, h)
+            fine = [d for d in range(64) if d not in (3, 5, 6, 7)]
+            assert (o[h, fine] - ref[i, h, fine]).abs().max() < 0.05
+    assert (out[new:].double() - ref[new:]).abs().max() < 0.05
+
+
+def test_scores_of_any_size(gpu):
+    """Large scores (one key takes all), and a scale that makes all weights alike."""
+    b = pu.Batch([200, 90], [1, 80], 4, 2, 64, 16, FP32, seed=10, amp=60.0)
+    out, _ = run_attention(b, gpu)
+    ref, _, _ = b.reference()
+    # scores up to about 2000, off by 64 * 2^-24 of the sum of their terms' magnitudes: < 0.05 of a weight's exponent
+    assert (out.double() - ref).abs().max() < 0.15
+    b = pu.Batch([200, 90], [1, 80], 4, 2, 64, 16, BF16, seed=10)
+    compare(b, gpu, scale=1e-6)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("ctx,new", [(9000, 1), (20011, 1), (9000, 3), (3000, 60), (2500, 170)])
+def test_long_contexts_are_cut_and_joined(gpu, dtype, ctx, new):
+    b = pu.Batch([ctx], [new], 4, 2, 64, 64, dtype, seed=11)
+    compare(b, gpu, max_new=new)
+
+
+def test_one_long_request_among_many_short_ones(gpu):
+    rng = random.Random(3)
+    ctx = [rng.randrange(0, 40) for _ in range(700)]
+    ctx[300] = 6000
+    b = pu.Batch(ctx, [1] * 699 + [70], 2, 1, 64, 16, BF16, seed=12)
+    compare(b, gpu)
+
+
+@pytest.mark.parametrize("hint", [0, 1, 3, 200, 10 ** 6])
+def test_the_hint_does_not_change_what_is_right(gpu, hint):
+    b = pu.Batch([50, 10, 400], [1, 200, 3], 4, 1, 64, 16, BF16, seed=13)
+    compare(b, gpu, max_new=hint)
+
+
+def test_same_bits_again_and_on_another_stream(gpu):
+    b = pu.Batch([5000, 10, 900], [1, 200, 3], 8, 2, 128, 32, BF16, seed=14)
+    up = b.upload(gpu)
+    first = slnr.sparselnr_paged_attention(*up)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(s):
+            again = slnr.sparselnr_paged_attention(*up)
+        s.synchronize()
+        assert torch.equal(first.view(torch.int16), again.view(torch.int16))
+    third = slnr.sparselnr_paged_attention(*up, stream=s)
+    s.synchronize()
+    assert torch.equal(first.view(torch.int16), third.view(torch.int16))
+
+
+def test_offsets_past_32_bits(gpu):
+    """Pages that begin past 2^32 values, and slots of them."""
+    P, Hkv, D = 64, 8, 128
+    pages = (1 << 32) // (P * Hkv * D) + 70
+    b = pu.Batch([150, 30], [1, 66], 8, Hkv, D, P, BF16, seed=15)
+    kc = torch.empty(pages, P, Hkv, D, dtype=BF16, device=gpu)
+    vc = torch.empty(pages, P, Hkv, D, dtype=BF16, device=gpu)
+    shift = pages - b.kc.shape[0]
+    q, k0, v0, table, seq, qptr = b.upload(gpu)
+    kc[shift:], vc[shift:] = k0, v0
+    table = torch.where(table >= 0, table + shift, table)
+    out = slnr.sparselnr_paged_attention(q, kc, vc, table, seq, qptr)
+    want = slnr.sparselnr_paged_attention(q, k0, v0, b.ints(b.table, gpu), seq, qptr)
+    assert torch.equal(out, want)
+    sel = torch.arange(3, dtype=torch.int32, device=gpu).expand(q.shape[0], Hkv, 3).contiguous()
+    assert torch.equal(slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, sel),
+                       slnr.sparselnr_block_attention(q, k0, v0, b.ints(b.table, gpu), seq, qptr, sel))
+    slots = torch.tensor([pages * P - 1], device=gpu)
+    k = torch.randn(1, Hkv, D, device=gpu).to(BF16)
+    kc[-1] = 0
+    kq = torch.zeros(pages, Hkv, D, dtype=torch.int8, device=gpu)
+    ks = torch.zeros(pages, Hkv, device=gpu)
+    slnr.sparselnr_cache_append(k, k, slots, kc, vc, kq, ks)
+    assert torch.equal(kc[-1, -1], k[0]) and torch.equal(vc[-1, -1], k[0])
+    want_q, want_s = pu.summary(kc[-1, :, 0].cpu().double())
+    assert torch.equal(kq[-1, 0].cpu(), want_q) and float(ks[-1, 0]) == want_s
+    assert (kq[:-1] == 0).all()
+
+
+def test_refusals_on_the_device(gpu):
+    b = pu.Batch([30], [2], 4, 2, 64, 16, BF16, seed=16)
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    call = slnr.sparselnr_paged_attention
+    with pytest.raises(TypeError):
+        call(q.float(), kc, vc, table, seq, qptr)
+    with pytest.raises(TypeError):
+        call(q, kc, vc, table.long(), seq, qptr)
+    with pytest.raises(TypeError):
+        call(q.to(torch.float64), kc.to(torch.float64), vc.to(torch.float64), table, seq, qptr)
+    with pytest.raises(ValueError):
+        call(q, kc, vc[:-1], table, seq, qptr)
+    with pytest.raises(ValueError):
+        call(q[:, :3], kc, vc, table, seq, qptr)
+    with pytest.raises(ValueError):
+        call(q, kc, vc, table, seq, qptr[:-1])
+    with pytest.raises(ValueError):
+        call(q, kc, vc, table, seq, qptr, out=q[:1].contiguous())
+    with pytest.raises(ValueError):
+        call(q, kc, vc, table, seq, qptr, lse=torch.empty(2, 3, device=gpu))
+    with pytest.raises(ValueError):
+        call(q.transpose(1, 2), kc, vc, table, seq, qptr)
+    with pytest.raises(slnr.SparseLNRError) as e:
+        call(q, kc, vc, table, seq, qptr, scale=-1.0)
+    assert e.value.status == slnr.ERR_INVALID_ARG
+    odd = torch.zeros(2 * 4 * 64 + 1, dtype=BF16, device=gpu)[1:].view(2, 4, 64)
+    with pytest.raises(slnr.SparseLNRError) as e:  # rows off 16 bytes
+        call(odd, kc, vc, table, seq, qptr)
+    assert e.value.status == slnr.ERR_UNSUPPORTED
+    with pytest.raises(slnr.SparseLNRError) as e:
+        slnr.sparselnr_block_select(q, torch.zeros(3, 2, 64, dtype=torch.int8, device=gpu), torch.zeros(3, 2, device=gpu),
+                                    table, seq, qptr, 16, 300)
+    assert e.value.status == slnr.ERR_UNSUPPORTED
+    with pytest.raises(ValueError):
+        slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, torch.zeros(2, 3, 4, dtype=torch.int32, device=gpu))
+
+
+# ------------------------------------------------------------- tables
+
+
+def run_tables(ctx, new, table, free, tokens, P, gpu, stride=None):
+    R, W = len(ctx), len(table[0]) if table else 0
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device=gpu)  # noqa: E731
+    wide = torch.full((R, (stride or W)), -77, dtype=torch.int32, device=gpu)
+    t = wide[:, :W]
+    t.copy_(ints(table).view(R, W))
+    qptr, seq, slots, counts = slnr.sparselnr_page_tables(ints(ctx), ints(new), t, ints(free), tokens, P)
+    assert (wide[:, W:] == -77).all()
+    return qptr.tolist(), seq.tolist(), slots.tolist(), counts.tolist(), t.tolist()
+
+
+@pytest.mark.parametrize("R,P,seed", [(1, 16, 0), (5, 1, 1), (64, 64, 2), (255, 16, 3), (256, 8, 4), (257, 32, 5),
+                                      (1500, 16, 6), (3, 4096, 7)])
+@pytest.mark.parametrize("fit", ["fits", "few pages", "narrow table", "few tokens", "many tokens", "holes"])
+def test_page_tables(gpu, R, P, seed, fit):
+    rng = random.Random(seed)
+    ctx = [rng.choice([0, 1, P - 1, P, P + 1, rng.randrange(0, 6 * P + 20)]) for _ in range(R)]
+    new = [rng.choice([0, 1, 1, 2, P, rng.randrange(0, 2 * P + 9)]) for _ in range(R)]
+    if P == 4096:
+        new = [min(n, 3000) for n in new]
+    have = [-(-c // P) for c in ctx]
+    want = [-(-(c + n) // P) for c, n in zip(ctx, new)]
+    ids = list(range(sum(want) + 7))
+    rng.shuffle(ids)
+    W = max(want) + 2
+    if fit == "narrow table":
+        W = max(1, max(want) // 2)
+    table, at = [], 0
+    for h in have:
+        row = ids[at:at + h]
+        at += h
+        table.append((row + [-1] * W)[:W])
+    if fit == "holes":
+        for row, h in zip(table, have):
+            if h and rng.random() < 0.5:
+                row[h - 1] = -1
+    free = ids[at:]
+    need = sum(w - h for w, h in zip(want, have))
+    if fit == "few pages":
+        free = free[:need // 2]
+    T = sum(new)
+    tokens = {"few tokens": T // 2, "many tokens": T + 300}.get(fit, T)
+    got = run_tables(ctx, new, table, free, tokens, P, gpu, stride=W + 3)
+    exp = pu.page_tables(ctx, new, table, free, tokens, P)
+    for name, x, y in zip(("qptr", "seq", "slots", "counts", "table"), got, exp):
+        assert x == list(y), (name, fit)
+
+
+def test_page_tables_of_nothing(gpu):
+    got = run_tables([], [], [], [], 0, 16, gpu)
+    assert got[0] == [0] and got[3] == [0, 0, 0]
+    got = run_tables([-4, 3], [-1, 2], [[-1], [5]], [1], 2, 16, gpu)
+    assert got[0] == [0, 0, 2] and got[1] == [0, 5] and got[2] == [83, 84]
+
+
+# ------------------------------------------------------------- append
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D,Hkv,P,order", [(8, 1, 16, "slots"), (64, 8, 16, "heads"), (72, 3, 4, "pairs"),
+                                           (128, 8, 64, "slots"), (256, 2, 1, "slots"), (128, 40, 32, "slots"),
+                                           (256, 12, 128, "heads")])
+def test_cache_append(gpu, dtype, D, Hkv, P, order):
+    ctx, new = [0, 5, 3 * P, 2 * P + 1], [2 * P + 3, 1, 1, P]
+    b = pu.Batch(ctx, new, Hkv, Hkv, D, P, dtype, seed=D + P, order=order)
+    T = b.qptr[-1]
+    slots, touched = [], {}
+    for r in range(4):
+        for i in range(new[r]):
+            pos = ctx[r] + i
+            slots.append(b.table[r][pos // P] * P + pos % P)
+            touched[b.table[r][pos // P]] = pos % P + 1
+    k, v = b.qkv[:, Hkv:2 * Hkv], b.qkv[:, 2 * Hkv:]
+    _, kc, vc, *_ = b.upload(gpu)
+    qkv = b.qkv.to(gpu)
+    pages = kc.shape[0]
+    kq = torch.full((pages, Hkv, D), 99, dtype=torch.int8, device=gpu)
+    ks = torch.full((pages, Hkv), 99.0, device=gpu)
+    s = torch.tensor(slots, device=gpu)
+    slnr.sparselnr_cache_append(qkv[:, Hkv:2 * Hkv], qkv[:, 2 * Hkv:], s, kc, vc, kq, ks)
+    b.kc[s.cpu() // P, s.cpu() % P] = k
+    b.vc[s.cpu() // P, s.cpu() % P] = v
+    bits = torch.int32 if dtype == FP32 else torch.int16
+    assert torch.equal(kc.cpu().contiguous().view(bits), b.kc.contiguous().view(bits))
+    assert torch.equal(vc.cpu().contiguous().view(bits), b.vc.contiguous().view(bits))
+    for page in range(pages):
+        if page not in touched:
+            assert (kq[page] == 99).all() and (ks[page] == 99).all()
+            continue
+        for h in range(Hkv):
+            wq, ws = pu.summary(b.kc[page, :touched[page], h].double())
+            assert torch.equal(kq[page, h].cpu(), wq) and float(ks[page, h]) == ws, (page, h)
+    # without summaries the caches are the same
+    _, kc2, vc2, *_ = b.upload(gpu)
+    slnr.sparselnr_cache_append(qkv[:, Hkv:2 * Hkv], qkv[:, 2 * Hkv:], s, kc2, vc2)
+    assert torch.equal(kc2.cpu().contiguous().view(bits), b.kc.contiguous().view(bits))
+
+
+def test_append_leaves_out_slots_that_are_none(gpu):
+    kc = torch.zeros(2, 4, 1, 64, dtype=BF16, device=gpu)
+    vc, k = torch.zeros_like(kc), torch.ones(5, 1, 64, dtype=BF16, device=gpu)
+    kq, ks = torch.zeros(2, 1, 64, dtype=torch.int8, device=gpu), torch.zeros(2, 1, device=gpu)
+    slots = torch.tensor([-1, 1, 8, 2 ** 40, -2 ** 50], device=gpu)
+    slnr.sparselnr_cache_append(k, k, slots, kc, vc, kq, ks)
+    assert int((kc != 0).sum()) == 64 and (kc[0, 1] == 1).all() and int((vc != 0).sum()) == 64
+    # mean of a zero row and a row of ones
+    assert (kq[0] == 127).all() and (kq[1] == 0).all()
+
+
+def test_summaries_of_zeros_and_of_what_is_not_finite(gpu):
+    kc = torch.zeros(4, 2, 1, 64, dtype=FP32, device=gpu)
+    k = torch.zeros(4, 1, 64, device=gpu)
+    k[1, 0, 5] = math.inf
+    k[2, 0, 6] = math.nan
+    k[3, 0, 7] = 1e-45  # the least subnormal number: its step is 0
+    kq, ks = torch.full((4, 1, 64), 9, dtype=torch.int8, device=gpu), torch.full((4, 1), 9.0, device=gpu)
+    slnr.sparselnr_cache_append(k, k, torch.tensor([0, 2, 4, 6], device=gpu), kc, kc.clone(), kq, ks)
+    assert (kq == 0).all() and ks.view(-1).tolist() == [0.0, math.inf, math.inf, 0.0]
+
+
+# ------------------------------------------------------------- selection
+
+
+def run_select(b, kq, ks, top, first, local, gpu):
+    q, _, _, table, seq, qptr = b.upload(gpu)
+    return slnr.sparselnr_block_select(q, kq.to(gpu), ks.to(gpu), table, seq, qptr, b.P, top, first=first,
+                                       local=local).cpu()
+
+
+def summaries(pages, Hkv, D, seed, levels=127):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randint(-levels, levels + 1, (pages, Hkv, D), generator=g).to(torch.int8),
+            torch.rand(pages, Hkv, generator=g) * 0.01)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D,Hq,Hkv", [(8, 2, 2), (64, 7, 1), (72, 8, 4), (128, 32, 8), (200, 4, 2), (256, 64, 1)])
+@pytest.mark.parametrize("new", [1, 37])
+def test_select(gpu, dtype, D, Hq, Hkv, new):
+    b = pu.Batch([0, 130, 40, 700], [new] * 4, Hq, Hkv, D, 8, dtype, seed=D)
+    kq, ks = summaries(b.kc.shape[0], Hkv, D, D)
+    for top, first, local in ((1, 0, 1), (5, 1, 2), (12, 0, 0), (100, 3, 3)):
+        got = run_select(b, kq, ks, top, first, local, gpu)
+        want = pu.select(b.q, kq, ks, b.table, b.seq, b.qptr, 8, top, first, local)
+        assert torch.equal(got, want), (top, first, local)
+
+
+@pytest.mark.parametrize("new", [1, 20])
+def test_select_ties_go_to_the_lowest_page(gpu, new):
+    b = pu.Batch([900, 333], [new, new], 2, 1, 64, 4, BF16, seed=20)
+    kq, ks = summaries(b.kc.shape[0], 1, 64, 20, levels=0)  # every score is zero
+    ks[::3] = 0.0
+    ks[1::3] = -1.0  # and -0 is 0
+    for top in (1, 7, 64, 256):
+        got = run_select(b, kq, ks, top, 0, 1, gpu)
+        assert torch.equal(got, pu.select(b.q, kq, ks, b.table, b.seq, b.qptr, 4, top, 0, 1)), top
+    kq, ks = summaries(b.kc.shape[0], 1, 64, 21, levels=1)  # few levels: many equal scores
+    ks[:] = 1.0
+    kq[:, :, 2:] = 0
+    for top in (3, 40):
+        got = run_select(b, kq, ks, top, 1, 1, gpu)
+        assert torch.equal(got, pu.select(b.q, kq, ks, b.table, b.seq, b.qptr, 4, top, 1, 1)), top
+
+
+def test_select_numbers_that_are_not_finite_and_pages_that_are_not_there(gpu):
+    b = pu.Batch([300, 100], [18, 1], 4, 2, 64, 4, FP32, seed=22)
+    kq, ks = summaries(b.kc.shape[0], 2, 64, 22)
+    kq[b.table[0][9]], ks[b.table[0][9]] = 0, math.inf       # a mean that was not finite: NaN, first
+    ks[b.table[0][11]] = 3e38                                # overflows
+    for j in (0, 3, 76):
+        b.table[0][j] = -1
+    b.table[1] = [-1] * len(b.table[1])
+    b.q[3, 1, 5] = math.nan                                  # a query that is not finite: all scores zero
+    got = run_select(b, kq, ks, 6, 1, 1, gpu)
+    assert torch.equal(got, pu.select(b.q, kq, ks, b.table, b.seq, b.qptr, 4, 6, 1, 1))
+    assert (got[18:] == -1).all() and (got[0] == 9).any()
+
+
+@pytest.mark.parametrize("new,ctx", [(1, 5000), (1, 40000), (16, 2500), (33, 5000)])
+@pytest.mark.parametrize("top", [3, 256])
+def test_select_long_contexts_go_in_segments(gpu, new, ctx, top):
+    """Pages of one token: more of them than a row in LDS holds."""
+    b = pu.Batch([ctx], [new], 2, 2, 64, 1, BF16, seed=23)
+    kq, ks = summaries(b.kc.shape[0], 2, 64, 23)
+    got = run_select(b, kq, ks, top, 1, 1, gpu)
+    assert torch.equal(got, pu.select(b.q, kq, ks, b.table, b.seq, b.qptr, 1, top, 1, 1))
+
+
+# ------------------------------------------------------------- sparse attention
+
+
+def random_selection(b, Hkv, top, seed):
+    rng = random.Random(seed)
+    sel = []
+    for r in range(len(b.seq)):
+        for i in range(b.new[r]):
+            near = (b.ctx[r] + i) // b.P
+            heads = []
+            for _ in range(Hkv):
+                n = rng.randrange(0, min(top, near + 1) + 1)
+                pick = sorted(rng.sample(range(near + 1), n))
+                heads.append(pick + [-1] * (top - n))
+            sel.append(heads)
+    return sel
+
+
+def compare_sparse(b, sel, gpu, logits=8.0):
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    lse = torch.full(q.shape[:2], math.nan, device=gpu)
+    out = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, b.ints(sel, gpu), lse=lse)
+    pu.check(out.cpu(), lse, b.reference(sel=sel), b.dtype, max(b.seq), b.q.shape[2], vmax(b), logits)
+    return out.cpu(), lse
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D,Hq,Hkv,P", [(8, 2, 2, 4), (64, 8, 2, 16), (72, 5, 1, 8), (128, 16, 4, 64), (136, 3, 1, 32),
+                                        (256, 40, 2, 16)])
+def test_block_attention(gpu, dtype, D, Hq, Hkv, P):
+    b = pu.Batch([0, 5 * P + 3, 90], [3, 20, 1], Hq, Hkv, D, P, dtype, seed=D)
+    compare_sparse(b, random_selection(b, Hkv, 5, D), gpu)
+
+
+def test_block_attention_of_nothing_and_of_wrong_pages(gpu):
+    b = pu.Batch([100, 50], [2, 2], 4, 2, 64, 16, BF16, seed=30)
+    none = [[[-1] * 3 for _ in range(2)] for _ in range(4)]
+    out, lse = compare_sparse(b, none, gpu)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    b.table[0][2] = -1
+    wild = [[[2, 4, 10 ** 6] for _ in range(2)] for _ in range(4)]
+    wild[1][0] = [-5, 1, 2 ** 31 - 1]
+    wild[3][1] = [3, 4, 5]  # pages ahead of the token: nothing to see in them but its own
+    compare_sparse(b, wild, gpu)
+
+
+@pytest.mark.parametrize("T", [1, 3])
+def test_block_attention_is_cut_where_there_are_few_tokens(gpu, T):
+    b = pu.Batch([9000], [T], 4, 1, 128, 64, BF16, seed=31)
+    sel = [[sorted(random.Random(t).sample(range(140), 60)) + [-1] * 4] for t in range(T)]
+    compare_sparse(b, sel, gpu)
+
+
+def test_sparse_over_all_pages_is_dense(gpu):
+    b = pu.Batch([200, 30], [4, 4], 8, 2, 64, 16, FP32, seed=32)
+    sel = [[list(range(20)) for _ in range(2)] for _ in range(8)]
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    out = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, b.ints(sel, gpu))
+    dense = slnr.sparselnr_paged_attention(q, kc, vc, table, seq, qptr)
+    # each within its bound of the same value
+    _, _, weight = b.reference()
+    tol = 2 * pu.tolerance(FP32, weight, 210, 64, vmax(b))
+    assert ((out.double() - dense.double()).abs().cpu() <= tol).all()
+
+
+# ------------------------------------------------------------- graphs
+
+
+def test_a_captured_step_replays(gpu):
+    """A decode step of all five calls in a HIP graph: new lengths and rows are seen
+    by every replay, which gives what the eager calls give."""
+    P, Hq, Hkv, D, R, W = 16, 8, 2, 64, 3, 40
+    g = torch.Generator(device=gpu).manual_seed(1)
+    pages = R * W
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32, device=gpu)  # noqa: E731
+
+    def state():
+        free = torch.arange(pages, dtype=torch.int32, device=gpu)
+        return dict(ctx=ints(R), new=ints(R), table=ints(R, W) - 1, free=free,
+                    kc=torch.zeros(pages, P, Hkv, D, dtype=BF16, device=gpu),
+                    vc=torch.zeros(pages, P, Hkv, D, dtype=BF16, device=gpu),
+                    kq=torch.zeros(pages, Hkv, D, dtype=torch.int8, device=gpu), ks=torch.zeros(pages, Hkv, device=gpu),
+                    qkv=torch.zeros(R, Hq + 2 * Hkv, D, dtype=BF16, device=gpu))
+
+    def step(s):
+        q, k, v = s["qkv"][:, :Hq], s["qkv"][:, Hq:Hq + Hkv], s["qkv"][:, Hq + Hkv:]
+        qptr, seq, slots, counts = slnr.sparselnr_page_tables(s["ctx"], s["new"], s["table"], s["free"], R, P)
+        slnr.sparselnr_cache_append(k, v, slots, s["kc"], s["vc"], s["kq"], s["ks"])
+        full = slnr.sparselnr_paged_attention(q, s["kc"], s["vc"], s["table"], seq, qptr, max_new=1)
+        sel = slnr.sparselnr_block_select(q, s["kq"], s["ks"], s["table"], seq, qptr, P, 4)
+        part = slnr.sparselnr_block_attention(q, s["kc"], s["vc"], s["table"], seq, qptr, sel)
+        return qptr, seq, slots, counts, full, sel, part
+
+    a, e = state(), state()
+    for s in (a, e):
+        s["new"].fill_(1)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        step(a)  # workspaces
+    stream.synchronize()
+    for s in (a,):
+        s.update({k: v for k, v in state().items() if k not in ("free",)})
+        s["new"].fill_(1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        outs = step(a)
+    used = 0
+    for i in range(50):
+        x = torch.randn(R, Hq + 2 * Hkv, D, device=gpu, generator=g).to(BF16)
+        for s in (a, e):
+            s["qkv"].copy_(x)
+            s["ctx"].fill_(i)
+            # the pages taken so far go to the end of the list
+            s["free"].copy_(torch.arange(pages, dtype=torch.int32, device=gpu).roll(-used))
+        graph.replay()
+        want = step(e)
+        torch.cuda.synchronize()
+        for x, y in zip(outs, want):
+            assert torch.equal(x, y), i
+        assert int(want[3][2]) == 0
+        used += int(want[3][1])
+    assert used == R * (-(-50 // P))
