@@ -44,6 +44,34 @@ __device__ __forceinline__ float score_unit(const AttendArgs &a) {
   return sizeof(T) == 4 ? 1.0f : a.scale2;
 }
 
+template <class T>
+struct Pack4 {
+  typedef i16x4 V;
+};
+template <>
+struct Pack4<float> {
+  typedef f32x4 V;
+};
+
+// Adds weight * v to four columns of a query that sees the key, for those of the
+// values v[d .. d + 3] that are infinite or NaN.
+template <class T, class F>
+__device__ __forceinline__ void add_odd(const T *v, int d, int D, float weight, bool seen, F add) {
+  if (d < D) {
+    union {
+      typename Pack4<T>::V v;
+      T t[4];
+    } w;
+    w.v = *(const __attribute__((address_space(1))) typename Pack4<T>::V *)(v + d);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float x = (float)w.t[c];
+      add(c, seen && !(fabsf(x) < __builtin_inff()) ? weight * x : 0.0f);
+    }
+  }
+  asm volatile("" ::: "memory");  // one load at a time: this is rare, registers are not
+}
+
 struct Request {
   int first, n, S;  // first token, tokens, visible length
 };
@@ -302,7 +330,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
         const int d = i * 32 + grp * 8;
-        q[i] = load8<T>(have_row && d < a.D ? src + d : (const T *)kZeroRow);
+        q[i] = load8_global<T>(have_row && d < a.D ? src + d : (const T *)kZeroRow);
       }
     }
 
@@ -342,8 +370,8 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
         for (int i = 0; i < KS; ++i) {
           const int d = i * 32 + grp * 8;
           const bool in_row = ok && d < a.D;
-          kr[s][i] = load8<T>(in_row ? ks + d : (const T *)kZeroRow);
-          vr[s][i] = load8<T>(in_row ? vs + d : (const T *)kZeroRow);
+          kr[s][i] = load8_global<T>(in_row ? ks + d : (const T *)kZeroRow);
+          vr[s][i] = load8_global<T>(in_row ? vs + d : (const T *)kZeroRow);
         }
       }
     };
@@ -454,12 +482,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
                       (int64_t)(u & (P - 1)) * a.v_slot + (int64_t)h * a.v_head;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int d = i * 16 + grp * 4 + j;
-            const float v = d < a.D ? (float)vs[d] : 0.0f;
-            if (seen && !(fabsf(v) < __builtin_inff())) o[i][j] += e * v;
-          }
+          add_odd<T>(vs, i * 16 + grp * 4, a.D, e, seen, [&](int c, float x) { o[i][c] += x; });
       }
       __builtin_amdgcn_wave_barrier();
     }
@@ -550,15 +573,6 @@ struct ManyShared {
 constexpr int kManyKeys = 64;
 constexpr int kManyMinSteps = 4;  // a piece is at least so many tiles of keys long
 
-template <class T>
-struct Pack4 {
-  typedef i16x4 V;
-};
-template <>
-struct Pack4<float> {
-  typedef f32x4 V;
-};
-
 template <class T, int DP, int NW>
 __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
   typedef typename Type<T>::Vec Vec;
@@ -615,7 +629,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
         const int d = i * 16 + half * 8;
-        q[i] = load8<T>(have_row && d < a.D ? src + d : (const T *)kZeroRow);
+        q[i] = load8_global<T>(have_row && d < a.D ? src + d : (const T *)kZeroRow);
       }
     }
     f32x16 o[DT];
@@ -649,8 +663,8 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
         const bool ok = page >= 0 && in_row;
         const T *ks = (const T *)a.k + (int64_t)page * a.k_page + in * a.k_slot + (int64_t)h * a.k_head + c8;
         const T *vs = (const T *)a.v + (int64_t)page * a.v_page + in * a.v_slot + (int64_t)h * a.v_head + c8;
-        kr[i] = load8<T>(ok ? ks : (const T *)kZeroRow);
-        vr[i] = load8<T>(ok ? vs : (const T *)kZeroRow);
+        kr[i] = load8_global<T>(ok ? ks : (const T *)kZeroRow);
+        vr[i] = load8_global<T>(ok ? vs : (const T *)kZeroRow);
       }
     };
     auto store = [&](int t, int buf) {
@@ -673,6 +687,8 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
       }
     };
 
+    const unsigned k_at = lds_address(sh.k[0]) + L::k_first(col, half);
+    const unsigned v_at = lds_address(sh.v[0]) + L::v_first(lane);
     __syncthreads();  // the last piece's tiles are done with
     int page = find(t0), page1 = find(t0 + 1), page2 = find(t0 + 2);
     unsigned long long live = 0, live1 = __builtin_amdgcn_ballot_w64(page >= 0);
@@ -694,7 +710,6 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
       page2 = find(t + 3);
       const int b = lo + t * kManyKeys;
       if (b <= wave_last && (!a.window || b + kManyKeys - 1 > wave_first - a.window)) {
-        const T *kt = sh.k[buf], *vt = sh.v[buf];
         // S^T = K Q^T
         f32x16 x[2];
 #pragma unroll
@@ -704,19 +719,30 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
 #pragma unroll
         for (int i = 0; i < KS; ++i)
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
-            x[s] = Type<T>::dot32(load8<T>(kt + L::at(s * 32 + col, i * 16 + half * 8)), q[i], x[s]);
+          for (int s = 0; s < 2; ++s) {
+            Vec k;
+            if constexpr (sizeof(T) == 2)
+              k = lds_read<Vec>((k_at ^ (i << 5)) + buf * (int)sizeof(sh.k[0]) + s * 32 * L::kRowBytes);
+            else
+              k = load8<T>(sh.k[buf] + L::at(s * 32 + col, i * 16 + half * 8));
+            x[s] = Type<T>::dot32(k, q[i], x[s]);
+          }
         if constexpr (sizeof(T) == 4) x[0] *= a.scale2, x[1] *= a.scale2;
         const bool part_seen = b + kManyKeys - 1 > wave_first || (a.window && b <= wave_last - a.window);
         if (part_seen || live != ~0ull) {
+          // bit: this lane's query sees the key; the lane's keys begin at 4 half
+          const int most = pos - b, least = a.window ? most - a.window : -1;
+          unsigned long long seen = live;
+          seen &= most < 0 ? 0 : most >= 63 ? ~0ull : (2ull << most) - 1;
+          seen &= least < 0 ? ~0ull : least >= 63 ? 0 : ~0ull << (least + 1);
+          seen >>= 4 * half;
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
+          for (int s = 0; s < 2; ++s) {
+            const unsigned bits = (unsigned)(seen >> (32 * s));
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const int key = s * 32 + 8 * (j >> 2) + 4 * half + (j & 3);
-              const bool seen = ((live >> key) & 1) && b + key <= pos && (!a.window || b + key > pos - a.window);
-              x[s][j] = seen ? x[s][j] : kNegInf;
-            }
+            for (int j = 0; j < 16; ++j)
+              x[s][j] = bits & (1u << (8 * (j >> 2) + (j & 3))) ? x[s][j] : kNegInf;
+          }
         }
         float top = x[0][0];
 #pragma unroll
@@ -746,11 +772,18 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
           for (int i = 0; i < DT; ++i) {
             union {
               Vec v;
+              i16x4 h[sizeof(T)];
               T t[8];
             } w;
-            const int row = s * 16 + half * 4, d0 = i * 32 + (lane & 16);
-            L::read4(vt, row, d0, lane, w.t);
-            L::read4(vt, row + 8, d0, lane, w.t + 4);
+            if constexpr (sizeof(T) == 2) {
+              const unsigned at = (v_at ^ (i << 6)) + buf * (int)sizeof(sh.v[0]) + s * 16 * L::kRowBytes;
+              w.h[0] = lds_read_transposed(at);
+              w.h[1] = lds_read_transposed((at ^ L::kEight) + 8 * L::kRowBytes);
+            } else {
+              const int row = s * 16 + half * 4, d0 = i * 32 + (lane & 16);
+              L::read4(sh.v[buf], row, d0, lane, w.t);
+              L::read4(sh.v[buf], row + 8, d0, lane, w.t + 4);
+            }
             o[i] = Type<T>::dot32(w.v, pv[s], o[i]);
           }
         if (part_seen) {  // infinities and NaN of V, left out of the product above, to the rows that see them
@@ -773,10 +806,9 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
 #pragma unroll
             for (int i = 0; i < DT; ++i)
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const int d = i * 32 + 8 * (j >> 2) + 4 * half + (j & 3);
-                const float v = d < a.D ? (float)vs[d] : 0.0f;
-                if (seen && !(fabsf(v) < __builtin_inff())) o[i][j] += e * v;
+              for (int j = 0; j < 16; j += 4) {
+                const int d = i * 32 + 2 * j + 4 * half;
+                add_odd<T>(vs, d, a.D, e, seen, [&](int c, float x) { o[i][j + c] += x; });
               }
           }
         }

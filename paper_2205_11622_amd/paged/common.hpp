@@ -97,6 +97,21 @@ __device__ __forceinline__ typename Type<T>::Vec load8(const T *p) {
   return v;
 }
 
+// The same from device memory: the pointer may be one of two objects, which would
+// otherwise make the load a flat one, and that waits for LDS too.
+template <class T>
+__device__ __forceinline__ typename Type<T>::Vec load8_global(const T *p) {
+  typedef const __attribute__((address_space(1))) u32x4 *G;
+  union {
+    u32x4 u[sizeof(T) / 2];
+    typename Type<T>::Vec v;
+  } w;
+  const G g = (G)p;
+  w.u[0] = g[0];
+  if constexpr (sizeof(T) == 4) w.u[1] = g[1];
+  return w.v;
+}
+
 template <class T>
 __device__ __forceinline__ void store8(T *p, typename Type<T>::Vec v) {
   if constexpr (sizeof(T) == 2) {
@@ -132,6 +147,19 @@ struct Tile {
     else
       return row * kStride + column;
   }
+  // Operands of a 32 x 32 product in 16 bits.  The permutation is an exclusive or, so
+  // a lane's address for step i differs from its first one in single bits:
+  // K, row `row + 32 s` (row < 32), values 16 i + 8 half ..:  k_first ^ (i << 5), + 32 s rows;
+  // V, keys 16 s + 4 half + 8 p .., column 32 i + (lane & 31): v_first ^ (i << 6) ^ p * kEight, + 16 s + 8 p rows.
+  static constexpr int kRowBytes = kStride * (int)sizeof(T);
+  static constexpr unsigned kEight = DP >= 128 ? 32 : 16;  // chunk(row + 8) ^ chunk(row), in bytes
+  static __device__ __forceinline__ unsigned k_first(int row, int half) {
+    return row * kRowBytes + ((half ^ chunk(row)) << 4);
+  }
+  static __device__ __forceinline__ unsigned v_first(int lane) {
+    const int row = (lane >> 5) * 4 + ((lane >> 2) & 3);
+    return at(row, (lane & 16) + (lane & 3) * 4) * (int)sizeof(T);
+  }
   // Keys row .. row + 3 of column `column + (lane & 15)`; row and column are the
   // same in all 16 lanes of a group, multiples of 4 and 16.
   static __device__ __forceinline__ void read4(const T *tile, int row, int column, int lane, T out[4]) {
@@ -150,6 +178,19 @@ struct Tile {
     }
   }
 };
+
+// Reads at a byte address of LDS.
+template <class V>
+__device__ __forceinline__ V lds_read(unsigned address) {
+  return *(const __attribute__((address_space(3))) V *)(uintptr_t)address;
+}
+__device__ __forceinline__ i16x4 lds_read_transposed(unsigned address) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(uintptr_t)address);
+}
+template <class T>
+__device__ __forceinline__ unsigned lds_address(const T *p) {
+  return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) T *)p;
+}
 
 // ------------------------------------------------------------------ lanes
 
