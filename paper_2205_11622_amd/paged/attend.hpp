@@ -571,6 +571,9 @@ struct ManyShared {
 };
 
 constexpr int kManyKeys = 64;
+constexpr float kLag = 8.0f;      // the maximum that weights are taken at may be so many powers of two low
+// Instruction classes of sched_group_barrier.
+constexpr int kMfma = 0x008, kDsRead = 0x100;
 constexpr int kManyMinSteps = 4;  // a piece is at least so many tiles of keys long
 
 template <class T, int DP, int NW>
@@ -593,7 +596,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     const Request q = request_of(a, r);
     const long long rows = (long long)q.n * a.G;
     tiles = rows > a.few ? (int)((rows + ROWS - 1) / ROWS) : 0;
-    const int lo = a.window ? imax(q.S - q.n - a.window + 1, 0) : 0;
+    const int lo = (a.window ? imax(q.S - q.n - a.window + 1, 0) : 0) & -kManyKeys;
     steps = (q.S - lo + kManyKeys - 1) / kManyKeys;
   };
   split_scan<NT>(sh.split, a, kManyMinSteps, count);
@@ -608,7 +611,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     const int before = rq.S - rq.n;  // position of the request's first token
     const int first = pc.tile * ROWS, rows = imin(rq.n * a.G - first, ROWS);
     const int pos_first = before + first / a.G, pos_last = before + (first + rows - 1) / a.G;
-    const int lo = a.window ? imax(pos_first - a.window + 1, 0) : 0;
+    const int lo = (a.window ? imax(pos_first - a.window + 1, 0) : 0) & -kManyKeys;
     const int hi = imin(pos_last + 1, rq.S);
     const int tiles = hi > lo ? (hi - lo + kManyKeys - 1) / kManyKeys : 0;
     const int t0 = (int)((long long)tiles * pc.part / pc.np), t1 = (int)((long long)tiles * (pc.part + 1) / pc.np);
@@ -640,180 +643,305 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     float m = kNegInf, l = 0.0f;
 
     // ------------------------------------------------ K and V into LDS
-    auto find = [&](int t) {  // the page of key `lane` of tile t
-      const int u = lo + t * kManyKeys + lane;
-      int page = t < t1 && u < hi ? table[u >> a.shift] : -1;
-      return (unsigned)page < (unsigned)a.pages ? page : -1;
+    const int n = t1 - t0;          // tiles of this piece
+    const int k0 = lo + t0 * kManyKeys;
+    // The table's entry for key `lane` of tile i, or of the last key there is (there is
+    // one wherever this is called), and the page that it stands for.
+    auto find = [&](int i) { return table[imin(k0 + i * kManyKeys + lane, hi - 1) >> a.shift]; };
+    auto valid = [&](int i, int page) {
+      return k0 + i * kManyKeys + lane < hi && (unsigned)page < (unsigned)a.pages ? page : -1;
     };
     // a tile of which some of the block's rows see a part only
-    auto mixed = [&](int t) {
-      const int b = lo + t * kManyKeys;
+    auto mixed = [&](int i) {
+      const int b = k0 + i * kManyKeys;
       return b + kManyKeys - 1 > pos_first || (a.window && b <= pos_last - a.window);
+    };
+    // a tile of which some row of this wave sees something
+    auto active = [&](int i) {
+      const int b = k0 + i * kManyKeys;
+      return i < n && b <= wave_last && (!a.window || b + kManyKeys - 1 > wave_first - a.window);
     };
     const int c8 = (tid % NC) * 8, row_of = tid / NC;
     const bool in_row = c8 < a.D;
+    // Rows that are not there are read from a page that is, and zeroed on their way to
+    // LDS: a load then has no condition.
+    const T *k_head = (a.pages ? (const T *)a.k : (const T *)kZeroRow) + (a.pages ? (int64_t)h * a.k_head : 0);
+    const T *v_head = (a.pages ? (const T *)a.v : (const T *)kZeroRow) + (a.pages ? (int64_t)h * a.v_head : 0);
+    const int64_t k_page = a.pages ? a.k_page : 0, k_slot = a.pages ? a.k_slot : 0;
+    const int64_t v_page = a.pages ? a.v_page : 0, v_slot = a.pages ? a.v_slot : 0;
+    // A tile within one page (they begin at multiples of 64): its address is a scalar,
+    // a lane adds 32 bits to it.
+    const bool one_page = P >= kManyKeys && k_slot < (1 << 23) && v_slot < (1 << 23);
+    const unsigned k_lane = (unsigned)(row_of * (int)k_slot + (in_row ? c8 : 0)) * (unsigned)sizeof(T);
+    const unsigned v_lane = (unsigned)(row_of * (int)v_slot + (in_row ? c8 : 0)) * (unsigned)sizeof(T);
     Vec kr[CH], vr[CH];
-    auto load = [&](int t, int page_lane) {
-      const int b = lo + t * kManyKeys;
+    auto load = [&](Vec r[CH], int i, int page_lane, const T *base, int64_t page_stride, int64_t slot_stride,
+                    unsigned lane_bytes) {
+      if (one_page) {
+        const int page = imax(__builtin_amdgcn_readfirstlane(page_lane), 0);
+        const int in = (k0 + i * kManyKeys) & (P - 1);
+        const char *src = (const char *)(base + page * page_stride + in * slot_stride);
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        const int row = i * RS + row_of;
-        const int page = __shfl(page_lane, row);
-        const int64_t in = (b + row) & (P - 1);
-        const bool ok = page >= 0 && in_row;
-        const T *ks = (const T *)a.k + (int64_t)page * a.k_page + in * a.k_slot + (int64_t)h * a.k_head + c8;
-        const T *vs = (const T *)a.v + (int64_t)page * a.v_page + in * a.v_slot + (int64_t)h * a.v_head + c8;
-        kr[i] = load8_global<T>(ok ? ks : (const T *)kZeroRow);
-        vr[i] = load8_global<T>(ok ? vs : (const T *)kZeroRow);
+        for (int c = 0; c < CH; ++c) {
+          r[c] = load8_global<T>((const T *)(src + lane_bytes));
+          src += RS * slot_stride * (int64_t)sizeof(T);
+        }
+      } else {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const int row = c * RS + row_of;
+          const int page = imax(__shfl(page_lane, row), 0);
+          const int in = (k0 + i * kManyKeys + row) & (P - 1);
+          r[c] = load8_global<T>(base + page * page_stride + in * slot_stride + (in_row ? c8 : 0));
+        }
       }
     };
-    auto store = [&](int t, int buf) {
-      if (mixed(t)) {
+    auto load_k = [&](int i, int page_lane) { load(kr, i, page_lane, k_head, k_page, k_slot, k_lane); };
+    auto load_v = [&](int i, int page_lane) { load(vr, i, page_lane, v_head, v_page, v_slot, v_lane); };
+    auto zero = [&](Vec r[CH], unsigned long long live) {
+      if (live != ~0ull || a.D != DP) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const bool keep = in_row && ((live >> (c * RS + row_of)) & 1);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) r[c][j] = keep ? r[c][j] : (T)0.0f;
+        }
+      }
+    };
+    auto store_k = [&](int i, unsigned long long live) {
+      zero(kr, live);
+      T *dst = sh.k[i & 1];
+#pragma unroll
+      for (int c = 0; c < CH; ++c) store8<T>(dst + L::at(c * RS + row_of, c8), kr[c]);
+    };
+    auto store_v = [&](int i, unsigned long long live) {
+      zero(vr, live);
+      if (mixed(i)) {
         unsigned long long odd = 0;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-          const unsigned long long b = __builtin_amdgcn_ballot_w64(clean8<T>(vr[i]));
+        for (int c = 0; c < CH; ++c) {
+          const unsigned long long b = __builtin_amdgcn_ballot_w64(clean8<T>(vr[c]));
 #pragma unroll
           for (int g = 0; g < 64 / NC; ++g)
-            if ((b >> (g * NC)) & ((1ull << NC) - 1)) odd |= 1ull << (i * RS + wave * (64 / NC) + g);
+            if ((b >> (g * NC)) & ((1ull << NC) - 1)) odd |= 1ull << (c * RS + wave * (64 / NC) + g);
         }
-        if (lane == 0) sh.odd[buf][wave] = odd;
+        if (lane == 0) sh.odd[i & 1][wave] = odd;
       }
+      T *dst = sh.v[i & 1];
 #pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        const int at = L::at(i * RS + row_of, c8);
-        store8<T>(sh.k[buf] + at, kr[i]);
-        store8<T>(sh.v[buf] + at, vr[i]);
-      }
+      for (int c = 0; c < CH; ++c) store8<T>(dst + L::at(c * RS + row_of, c8), vr[c]);
+    };
+    // A barrier that waits for LDS only: loads on their way stay there.
+    auto sync = [&]() {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     };
 
     const unsigned k_at = lds_address(sh.k[0]) + L::k_first(col, half);
     const unsigned v_at = lds_address(sh.v[0]) + L::v_first(lane);
-    __syncthreads();  // the last piece's tiles are done with
-    int page = find(t0), page1 = find(t0 + 1), page2 = find(t0 + 2);
-    unsigned long long live = 0, live1 = __builtin_amdgcn_ballot_w64(page >= 0);
-    if (t0 < t1) {
-      load(t0, page);
-      store(t0, t0 & 1);
-      load(t0 + 1, page1);
-    }
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-      const int buf = t & 1;
-      live = live1;
-      live1 = __builtin_amdgcn_ballot_w64(page1 >= 0);
-      if (t + 1 < t1) {
-        store(t + 1, buf ^ 1);
-        load(t + 2, page2);
-      }
-      page1 = page2;
-      page2 = find(t + 3);
-      const int b = lo + t * kManyKeys;
-      if (b <= wave_last && (!a.window || b + kManyKeys - 1 > wave_first - a.window)) {
-        // S^T = K Q^T
-        f32x16 x[2];
+    f32x16 x[2];
+    Vec pv[4];
+
+    // S^T = K Q^T of tile i
+    auto scores = [&](int i) {
+      if constexpr (sizeof(T) == 2) {
+        const unsigned at = k_at + (i & 1) * (int)sizeof(sh.k[0]);
+        Vec k[KS][2];
+#pragma unroll
+        for (int c = 0; c < KS; ++c)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) k[c][s] = lds_read<Vec>((at ^ (c << 5)) + s * 32 * L::kRowBytes);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int j = 0; j < 16; ++j) x[s][j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < KS; ++i)
+        for (int c = 0; c < KS; ++c)
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            Vec k;
-            if constexpr (sizeof(T) == 2)
-              k = lds_read<Vec>((k_at ^ (i << 5)) + buf * (int)sizeof(sh.k[0]) + s * 32 * L::kRowBytes);
-            else
-              k = load8<T>(sh.k[buf] + L::at(s * 32 + col, i * 16 + half * 8));
-            x[s] = Type<T>::dot32(k, q[i], x[s]);
-          }
-        if constexpr (sizeof(T) == 4) x[0] *= a.scale2, x[1] *= a.scale2;
-        const bool part_seen = b + kManyKeys - 1 > wave_first || (a.window && b <= wave_last - a.window);
-        if (part_seen || live != ~0ull) {
-          // bit: this lane's query sees the key; the lane's keys begin at 4 half
-          const int most = pos - b, least = a.window ? most - a.window : -1;
-          unsigned long long seen = live;
-          seen &= most < 0 ? 0 : most >= 63 ? ~0ull : (2ull << most) - 1;
-          seen &= least < 0 ? ~0ull : least >= 63 ? 0 : ~0ull << (least + 1);
-          seen >>= 4 * half;
+          for (int s = 0; s < 2; ++s) x[s] = Type<T>::dot32(k[c][s], q[c], x[s]);
+        // four operands ahead of the products
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 4, 0);
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const unsigned bits = (unsigned)(seen >> (32 * s));
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-              x[s][j] = bits & (1u << (8 * (j >> 2) + (j & 3))) ? x[s][j] : kNegInf;
-          }
+        for (int c = 0; c < 2 * KS - 4; ++c) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
         }
-        float top = x[0][0];
+        __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+      } else {
 #pragma unroll
-        for (int j = 1; j < 32; ++j) top = fmaxf(top, x[j >> 4][j & 15]);
-        top = max_across_32(top);
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[s][j] = 0.0f;
+#pragma unroll
+          for (int c = 0; c < KS; ++c)
+            x[s] = Type<T>::dot32(load8<T>(sh.k[i & 1] + L::at(s * 32 + col, c * 16 + half * 8)), q[c], x[s]);
+          x[s] *= a.scale2;
+        }
+      }
+    };
+
+    // P^T of tile i out of S^T, and what was summed so far brought to its maximum
+    auto weights = [&](int i, unsigned long long live) {
+      const int b = k0 + i * kManyKeys;
+      if (live != ~0ull || b + kManyKeys - 1 > wave_first || (a.window && b <= wave_last - a.window)) {
+        // bit: this lane's query sees the key; the lane's keys begin at 4 half
+        const int most = pos - b, least = a.window ? most - a.window : -1;
+        unsigned long long seen = live;
+        seen &= most < 0 ? 0 : most >= 63 ? ~0ull : (2ull << most) - 1;
+        seen &= least < 0 ? ~0ull : least >= 63 ? 0 : ~0ull << (least + 1);
+        seen >>= 4 * half;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const unsigned bits = (unsigned)(seen >> (32 * s));
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[s][j] = bits & (1u << (8 * (j >> 2) + (j & 3))) ? x[s][j] : kNegInf;
+        }
+      }
+      float top = x[0][0];
+#pragma unroll
+      for (int j = 1; j < 32; ++j) top = fmaxf(top, x[j >> 4][j & 15]);
+      top = max_across_32(top);
+      // The maximum may lag: weights up to 2^kLag are as good as weights up to 1 (their
+      // sums are in 32 bits, the type's rounding is relative), and O is seldom rescaled.
+      if (__builtin_amdgcn_ballot_w64((top - m) * sc > (sizeof(T) == 4 ? 0.0f : kLag))) {
         const float mn = fmaxf(m, top);
-        const float ms = mn == kNegInf ? 0.0f : mn * sc;
-        if (__builtin_amdgcn_ballot_w64(mn > m)) {
-          const float fade = exp2_of(m * sc - ms);
-          l *= fade;
+        const float fade = mn == kNegInf ? 1.0f : exp2_of((m - mn) * sc);
+        l *= fade;
 #pragma unroll
-          for (int i = 0; i < DT; ++i) o[i] *= fade;
-          m = mn;
-        }
-        Vec pv[4];
+        for (int c = 0; c < DT; ++c) o[c] *= fade;
+        m = mn;
+      }
+      const float ms = m == kNegInf ? 0.0f : m * sc;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-          const float e = exp2_of(__builtin_fmaf(x[j >> 4][j & 15], sc, -ms));
-          l += e;
-          x[j >> 4][j & 15] = e;
-          // the weights go to the matrix cores in the type of V, their sum stays in fp32
-          pv[j >> 3][j & 7] = (T)e;
-        }
+      for (int j = 0; j < 32; ++j) {
+        const float e = exp2_of(__builtin_fmaf(x[j >> 4][j & 15], sc, -ms));
+        l += e;
+        // the weights go to the matrix cores in the type of V, their sum stays in fp32
+        pv[j >> 3][j & 7] = (T)e;
+      }
+    };
+
+    // O^T += V^T P^T of tile i
+    auto values = [&](int i) {
+      if constexpr (sizeof(T) == 2) {
+        const unsigned at = v_at + (i & 1) * (int)sizeof(sh.v[0]);
+        union Operand {
+          i16x4 h[2];
+          Vec v;
+        } v[4][DT];
 #pragma unroll
         for (int s = 0; s < 4; ++s)
 #pragma unroll
-          for (int i = 0; i < DT; ++i) {
+          for (int c = 0; c < DT; ++c) {
+            const unsigned to = (at ^ (c << 6)) + s * 16 * L::kRowBytes;
+            v[s][c].h[0] = lds_read_transposed(to);
+            v[s][c].h[1] = lds_read_transposed((to ^ L::kEight) + 8 * L::kRowBytes);
+          }
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int c = 0; c < DT; ++c) o[c] = Type<T>::dot32(v[s][c].v, pv[s], o[c]);
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 8, 1);
+#pragma unroll
+        for (int c = 0; c < 4 * DT - 4; ++c) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, 1, 1);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(kMfma, 4, 1);
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int c = 0; c < DT; ++c) {
             union {
               Vec v;
-              i16x4 h[sizeof(T)];
               T t[8];
             } w;
-            if constexpr (sizeof(T) == 2) {
-              const unsigned at = (v_at ^ (i << 6)) + buf * (int)sizeof(sh.v[0]) + s * 16 * L::kRowBytes;
-              w.h[0] = lds_read_transposed(at);
-              w.h[1] = lds_read_transposed((at ^ L::kEight) + 8 * L::kRowBytes);
-            } else {
-              const int row = s * 16 + half * 4, d0 = i * 32 + (lane & 16);
-              L::read4(sh.v[buf], row, d0, lane, w.t);
-              L::read4(sh.v[buf], row + 8, d0, lane, w.t + 4);
-            }
-            o[i] = Type<T>::dot32(w.v, pv[s], o[i]);
+            const int row = s * 16 + half * 4, d0 = c * 32 + (lane & 16);
+            L::read4(sh.v[i & 1], row, d0, lane, w.t);
+            L::read4(sh.v[i & 1], row + 8, d0, lane, w.t + 4);
+            o[c] = Type<T>::dot32(w.v, pv[s], o[c]);
           }
-        if (part_seen) {  // infinities and NaN of V, left out of the product above, to the rows that see them
-          unsigned long long odd = 0;
+      }
+      if (mixed(i)) {  // infinities and NaN of V, left out of the product above, to the rows that see them
+        const int b = k0 + i * kManyKeys;
+        unsigned long long odd = 0;
 #pragma unroll
-          for (int w = 0; w < NW; ++w) odd |= sh.odd[buf][w];
-          while (odd) {
-            const int key = __builtin_ctzll(odd);
-            odd &= odd - 1;
-            float e = 0.0f;
-            const int at = (key >> 5) * 16 + ((key >> 3) & 3) * 4 + (key & 3);
+        for (int w = 0; w < NW; ++w) odd |= sh.odd[i & 1][w];
+        while (odd) {
+          const int key = __builtin_ctzll(odd);
+          odd &= odd - 1;
+          float e = 0.0f;
+          const int at = (key >> 5) * 16 + ((key >> 3) & 3) * 4 + (key & 3);
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-              if (j == at) e = x[j >> 4][j & 15];
-            e = __shfl(e, ((key >> 2) & 1) * 32 + col);
-            const int u = b + key;
-            const bool seen = u <= pos && (!a.window || u > pos - a.window);
-            const T *vs = (const T *)a.v + (int64_t)table[u >> a.shift] * a.v_page +
-                          (int64_t)(u & (P - 1)) * a.v_slot + (int64_t)h * a.v_head;
+          for (int j = 0; j < 32; ++j)
+            if (j == at) e = (float)pv[j >> 3][j & 7];
+          e = __shfl(e, ((key >> 2) & 1) * 32 + col);
+          const int u = b + key;
+          const bool seen = u <= pos && (!a.window || u > pos - a.window);
+          const T *vs = (const T *)a.v + (int64_t)table[u >> a.shift] * a.v_page + (int64_t)(u & (P - 1)) * a.v_slot +
+                        (int64_t)h * a.v_head;
 #pragma unroll
-            for (int i = 0; i < DT; ++i)
+          for (int c = 0; c < DT; ++c)
 #pragma unroll
-              for (int j = 0; j < 16; j += 4) {
-                const int d = i * 32 + 2 * j + 4 * half;
-                add_odd<T>(vs, d, a.D, e, seen, [&](int c, float x) { o[i][j + c] += x; });
-              }
-          }
+            for (int j = 0; j < 16; j += 4)
+              add_odd<T>(vs, c * 32 + 2 * j + 4 * half, a.D, e, seen, [&](int k, float y) { o[c][j + k] += y; });
         }
       }
-      __syncthreads();
+    };
+
+    // ------------------------------------------------ the walk, in two phases a tile
+    // Products of a phase (O += P V of the tile before, S = K Q of this one) and the
+    // softmax after them alternate behind barriers.  Half of the waves, one of the
+    // two on each SIMD, run a phase behind, so that one wave's products go beside
+    // the other's softmax.  Stage s is K of tile s + 1 and V of tile s, which must be in
+    // LDS before the products of tile s + 1: a wave stores its share and loads the next
+    // stage's in its softmax phases, late waves a stage further.
+    const int late = NW == 8 && wave >= NW / 2 ? 1 : 0;
+    sync();  // the last piece's tiles are done with
+    if (n > 0) {
+      const int page0 = valid(0, find(0)), page1 = valid(1, find(1)), page2 = valid(2, find(2)),
+                page3 = valid(3, find(3));
+      int pv_page = late ? page2 : page1, pk_page = late ? page3 : page2;
+      int next_page = find(late + 3);  // not looked at before its time: that would wait for the loads before it
+      // keys of this tile and the next two that are there
+      unsigned long long live0 = __builtin_amdgcn_ballot_w64(page0 >= 0),
+                         live1 = __builtin_amdgcn_ballot_w64(page1 >= 0),
+                         live2 = __builtin_amdgcn_ballot_w64(page2 >= 0);
+      load_k(0, page0);
+      store_k(0, live0);
+      load_k(1, page1);
+      load_v(0, page0);
+      sync();
+      if (late) {
+        store_k(1, live1);
+        store_v(0, live0);
+        load_k(2, page2);
+        load_v(1, page1);
+        sync();
+      }
+      for (int i = 0; i < n; ++i) {
+        if (active(i)) scores(i);
+        if (i > 0 && active(i - 1)) values(i - 1);
+        sync();
+        if (active(i)) weights(i, live0);
+        // past the piece's last tile these store what nobody reads
+        store_k(i + late + 1, late ? live2 : live1);
+        store_v(i + late, late ? live1 : live0);
+        load_k(i + late + 2, pk_page);
+        load_v(i + late + 1, pv_page);
+        const unsigned long long live = __builtin_amdgcn_ballot_w64(pk_page >= 0);
+        live0 = live1;
+        live1 = late ? live2 : live;
+        live2 = live;
+        pv_page = pk_page;
+        pk_page = valid(i + late + 3, next_page);
+        next_page = find(i + late + 4);
+        sync();
+      }
+      if (active(n - 1)) values(n - 1);
+      if (!late) sync();
     }
 
     // ------------------------------------------------ out, or to the join
