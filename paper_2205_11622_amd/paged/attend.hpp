@@ -72,6 +72,30 @@ __device__ __forceinline__ void add_odd(const T *v, int d, int D, float weight, 
   asm volatile("" ::: "memory");  // one load at a time: this is rare, registers are not
 }
 
+// Whether a row of V has infinities or NaN; the same in all lanes.
+template <class T>
+__device__ __forceinline__ bool has_odd(const T *v, int D, int lane) {
+  bool bad = false;
+  if (lane * 8 < D) {
+    typename Type<T>::Vec x = load8_global<T>(v + lane * 8);
+    bad = clean8<T>(x);
+  }
+  return __builtin_amdgcn_ballot_w64(bad) != 0;
+}
+
+// Eight terms of q.k.
+template <class T>
+__device__ __forceinline__ float dot8(typename Type<T>::Vec q, const T *k, int d, int D) {
+  float s = 0.0f;
+  if (d < D) {
+    const typename Type<T>::Vec x = load8_global<T>(k + d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = __builtin_fmaf((float)q[i], (float)x[i], s);
+  }
+  asm volatile("" ::: "memory");
+  return s;
+}
+
 struct Request {
   int first, n, S;  // first token, tokens, visible length
 };
@@ -375,6 +399,12 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
         }
       }
     };
+    // Rows of several tokens see different keys.
+    auto is_mixed = [&](int tile) {
+      return !SPARSE && pos_first != pos_last &&
+             (tile + kFewKeys - 1 > pos_first || (a.window && tile <= pos_last - a.window));
+    };
+    bool odd = false;
     T *vt = sh.v[wave];
     int base = lo + (s0 * kFewWaves + wave) * kFewKeys;
     const int end = imin(lo + s1 * kFewStep, hi);
@@ -400,24 +430,16 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
         for (int i = 0; i < KS; ++i) x[s] = Type<T>::dot16(kr[s][i], q[i], x[s]);
         if constexpr (sizeof(T) == 4) x[s] *= a.scale2;
       }
-      // Rows of several tokens see different keys.  A key that some rows see and
-      // others do not must not reach the latter through 0 * inf: infinite and
-      // NaN values of V are taken out of the product and added on their own.
-      bool mixed = false;
-      unsigned odd = 0;
-      if constexpr (!SPARSE)
-        mixed = pos_first != pos_last && (tile + kFewKeys - 1 > pos_first || (a.window && tile <= pos_last - a.window));
+      // A key that some rows see and others do not must not reach the latter through 0 *
+      // inf: infinities and NaN of V are taken out of the product and added at the end.
+      const bool mixed = is_mixed(tile);
       if (mixed) {
+        bool bad = false;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          bool bad = false;
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int i = 0; i < KS; ++i) bad |= clean8<T>(vr[s][i]);
-          unsigned long long b = __builtin_amdgcn_ballot_w64(bad);
-          b |= b >> 32;
-          b |= b >> 16;
-          odd |= ((unsigned)b & 0xffffu) << (16 * s);
-        }
+        if (__builtin_amdgcn_ballot_w64(bad)) odd = true;
       }
 #pragma unroll
       for (int s = 0; s < 2; ++s)
@@ -468,24 +490,30 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
         Tile<T, DP>::read4(vt, 16 + grp * 4, i * 16, lane, w.t + 4);
         o[i] = Type<T>::dot16(w.v, pv, o[i]);
       }
-      while (odd) {  // rare: a row of V with infinities or NaN at the edge of what is seen
-        const int key = __builtin_ctz(odd);
-        odd &= odd - 1;
-        float e = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (((key >> 4) << 2 | (key & 3)) == i) e = x[i >> 2][i & 3];
-        e = __shfl(e, ((key >> 2) & 3) * 16 + col);
-        const bool seen = tile + key <= pos && (!a.window || tile + key > pos - a.window);
-        const int u = tile + key;
-        const T *vs = (const T *)a.v + (int64_t)table[u >> a.shift] * a.v_page +
-                      (int64_t)(u & (P - 1)) * a.v_slot + (int64_t)h * a.v_head;
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-          add_odd<T>(vs, i * 16 + grp * 4, a.D, e, seen, [&](int c, float x) { o[i][c] += x; });
-      }
       __builtin_amdgcn_wave_barrier();
     }
+    if (odd) {  // rare
+      for (int tile = lo + (s0 * kFewWaves + wave) * kFewKeys; tile < end; tile += kFewStep)
+        if (is_mixed(tile))
+          for (int u = tile; u < tile + kFewKeys; ++u) {
+            const int pg = find(u);
+            if (pg < 0) continue;
+            const T *vs = (const T *)a.v + pg * a.v_page + (u & (P - 1)) * a.v_slot + (int64_t)h * a.v_head;
+            if (!has_odd<T>(vs, a.D, lane)) continue;
+            const T *ks = (const T *)a.k + pg * a.k_page + (u & (P - 1)) * a.k_slot + (int64_t)h * a.k_head;
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) s += dot8<T>(q[i], ks, i * 32 + grp * 8, a.D);
+            s = sum_across_16(s);
+            if constexpr (sizeof(T) == 4) s *= a.scale2;
+            const float e = exp2_of((s - m) * sc);
+            const bool seen = u <= pos && (!a.window || u > pos - a.window);
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+              add_odd<T>(vs, i * 16 + grp * 4, a.D, e, seen, [&](int c, float y) { o[i][c] += y; });
+          }
+    }
+
     // ------------------------------------------------ the four waves' results
     l = sum_across_16(l);
     if (l != l) m = __builtin_inff();  // NaN among the scores: the whole row is NaN
@@ -566,7 +594,7 @@ template <class T, int DP, int NW>
 struct ManyShared {
   T k[2][64 * Tile<T, DP>::kStride];
   T v[2][64 * Tile<T, DP>::kStride];
-  unsigned long long odd[2][NW];
+  int odd;  // infinities or NaN were taken out of V
   Split<NW * kWave> split;
 };
 
@@ -576,7 +604,10 @@ constexpr float kLag = 8.0f;      // the maximum that weights are taken at may b
 constexpr int kMfma = 0x008, kDsRead = 0x100;
 constexpr int kManyMinSteps = 4;  // a piece is at least so many tiles of keys long
 
-template <class T, int DP, int NW>
+//
+// ONE_PAGE: every tile of 64 keys lies in one page (64 positions and more, which begin
+// at multiples of 64), so its address is a scalar to which a lane adds 32 bits.
+template <class T, int DP, int NW, bool ONE_PAGE>
 __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
   typedef typename Type<T>::Vec Vec;
   typedef Tile<T, DP> L;
@@ -645,21 +676,28 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     // ------------------------------------------------ K and V into LDS
     const int n = t1 - t0;          // tiles of this piece
     const int k0 = lo + t0 * kManyKeys;
-    // The table's entry for key `lane` of tile i, or of the last key there is (there is
-    // one wherever this is called), and the page that it stands for.
-    auto find = [&](int i) { return table[imin(k0 + i * kManyKeys + lane, hi - 1) >> a.shift]; };
+    // The table's entry for key `lane` of tile i (ONE_PAGE: for all of them), or of the
+    // last key there is (there is one wherever this is called), and the page it stands for.
+    auto find = [&](int i) {
+      return table[imin(k0 + i * kManyKeys + (ONE_PAGE ? 0 : lane), hi - 1) >> a.shift];
+    };
     auto valid = [&](int i, int page) {
-      return k0 + i * kManyKeys + lane < hi && (unsigned)page < (unsigned)a.pages ? page : -1;
+      if constexpr (ONE_PAGE) page = __builtin_amdgcn_readfirstlane(page);
+      const bool in = k0 + i * kManyKeys + (ONE_PAGE ? 0 : lane) < hi;
+      return in && (unsigned)page < (unsigned)a.pages ? page : -1;
+    };
+    auto live_of = [&](int i, int page) -> unsigned long long {  // bit: this key is there
+      if constexpr (ONE_PAGE) {
+        const int keys = hi - (k0 + i * kManyKeys);
+        return page < 0 ? 0 : keys >= kManyKeys ? ~0ull : (1ull << keys) - 1;
+      } else {
+        return __builtin_amdgcn_ballot_w64(page >= 0);
+      }
     };
     // a tile of which some of the block's rows see a part only
     auto mixed = [&](int i) {
       const int b = k0 + i * kManyKeys;
       return b + kManyKeys - 1 > pos_first || (a.window && b <= pos_last - a.window);
-    };
-    // a tile of which some row of this wave sees something
-    auto active = [&](int i) {
-      const int b = k0 + i * kManyKeys;
-      return i < n && b <= wave_last && (!a.window || b + kManyKeys - 1 > wave_first - a.window);
     };
     const int c8 = (tid % NC) * 8, row_of = tid / NC;
     const bool in_row = c8 < a.D;
@@ -669,18 +707,14 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     const T *v_head = (a.pages ? (const T *)a.v : (const T *)kZeroRow) + (a.pages ? (int64_t)h * a.v_head : 0);
     const int64_t k_page = a.pages ? a.k_page : 0, k_slot = a.pages ? a.k_slot : 0;
     const int64_t v_page = a.pages ? a.v_page : 0, v_slot = a.pages ? a.v_slot : 0;
-    // A tile within one page (they begin at multiples of 64): its address is a scalar,
-    // a lane adds 32 bits to it.
-    const bool one_page = P >= kManyKeys && k_slot < (1 << 23) && v_slot < (1 << 23);
     const unsigned k_lane = (unsigned)(row_of * (int)k_slot + (in_row ? c8 : 0)) * (unsigned)sizeof(T);
     const unsigned v_lane = (unsigned)(row_of * (int)v_slot + (in_row ? c8 : 0)) * (unsigned)sizeof(T);
     Vec kr[CH], vr[CH];
-    auto load = [&](Vec r[CH], int i, int page_lane, const T *base, int64_t page_stride, int64_t slot_stride,
+    auto load = [&](Vec r[CH], int i, int page, const T *base, int64_t page_stride, int64_t slot_stride,
                     unsigned lane_bytes) {
-      if (one_page) {
-        const int page = imax(__builtin_amdgcn_readfirstlane(page_lane), 0);
+      if constexpr (ONE_PAGE) {
         const int in = (k0 + i * kManyKeys) & (P - 1);
-        const char *src = (const char *)(base + page * page_stride + in * slot_stride);
+        const char *src = (const char *)(base + imax(page, 0) * page_stride + in * slot_stride);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
           r[c] = load8_global<T>((const T *)(src + lane_bytes));
@@ -690,15 +724,17 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
           const int row = c * RS + row_of;
-          const int page = imax(__shfl(page_lane, row), 0);
+          const int pg = imax(__shfl(page, row), 0);
           const int in = (k0 + i * kManyKeys + row) & (P - 1);
-          r[c] = load8_global<T>(base + page * page_stride + in * slot_stride + (in_row ? c8 : 0));
+          r[c] = load8_global<T>(base + pg * page_stride + in * slot_stride + (in_row ? c8 : 0));
         }
       }
     };
-    auto load_k = [&](int i, int page_lane) { load(kr, i, page_lane, k_head, k_page, k_slot, k_lane); };
-    auto load_v = [&](int i, int page_lane) { load(vr, i, page_lane, v_head, v_page, v_slot, v_lane); };
-    auto zero = [&](Vec r[CH], unsigned long long live) {
+    auto load_k = [&](int i, int page) { load(kr, i, page, k_head, k_page, k_slot, k_lane); };
+    auto load_v = [&](int i, int page) { load(vr, i, page, v_head, v_page, v_slot, v_lane); };
+    // Rows that are not there become zeros, and V of a tile of which some rows see a part
+    // only loses its infinities and NaN (kept for those who see them: see `values`).
+    auto clean = [&](Vec r[CH], unsigned long long live) {
       if (live != ~0ull || a.D != DP) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
@@ -708,28 +744,19 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
         }
       }
     };
-    auto store_k = [&](int i, unsigned long long live) {
-      zero(kr, live);
-      T *dst = sh.k[i & 1];
-#pragma unroll
-      for (int c = 0; c < CH; ++c) store8<T>(dst + L::at(c * RS + row_of, c8), kr[c]);
-    };
-    auto store_v = [&](int i, unsigned long long live) {
-      zero(vr, live);
+    auto clean_v = [&](int i, unsigned long long live) {
+      clean(vr, live);
       if (mixed(i)) {
-        unsigned long long odd = 0;
+        bool bad = false;
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const unsigned long long b = __builtin_amdgcn_ballot_w64(clean8<T>(vr[c]));
-#pragma unroll
-          for (int g = 0; g < 64 / NC; ++g)
-            if ((b >> (g * NC)) & ((1ull << NC) - 1)) odd |= 1ull << (c * RS + wave * (64 / NC) + g);
-        }
-        if (lane == 0) sh.odd[i & 1][wave] = odd;
+        for (int c = 0; c < CH; ++c) bad |= clean8<T>(vr[c]);
+        if (__builtin_amdgcn_ballot_w64(bad)) sh.odd = 1;
       }
-      T *dst = sh.v[i & 1];
+    };
+    auto store = [&](T *dst, Vec r[CH]) {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) store8<T>(dst + L::at(c * RS + row_of, c8), vr[c]);
+      for (int c = 0; c < CH; ++c)  // 16 rows on, a row's chunks are permuted alike
+        store8<T>(dst + L::at((c * RS) % 16 + row_of, c8) + (c * RS) / 16 * 16 * L::kStride, r[c]);
     };
     // A barrier that waits for LDS only: loads on their way stay there.
     auto sync = [&]() {
@@ -746,7 +773,8 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     // S^T = K Q^T of tile i
     auto scores = [&](int i) {
       if constexpr (sizeof(T) == 2) {
-        const unsigned at = k_at + (i & 1) * (int)sizeof(sh.k[0]);
+        unsigned at = k_at + (i & 1) * (int)sizeof(sh.k[0]);
+        asm("" : "+v"(at));  // the addresses made of it here take an instruction each, kept ones a register
         Vec k[KS][2];
 #pragma unroll
         for (int c = 0; c < KS; ++c)
@@ -768,6 +796,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
           __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(kMfma, 4, 0);
+        __builtin_amdgcn_sched_barrier(0);
       } else {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -825,7 +854,8 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     // O^T += V^T P^T of tile i
     auto values = [&](int i) {
       if constexpr (sizeof(T) == 2) {
-        const unsigned at = v_at + (i & 1) * (int)sizeof(sh.v[0]);
+        unsigned at = v_at + (i & 1) * (int)sizeof(sh.v[0]);
+        asm("" : "+v"(at));
         union Operand {
           i16x4 h[2];
           Vec v;
@@ -849,6 +879,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
           __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
         }
         __builtin_amdgcn_sched_group_barrier(kMfma, 4, 1);
+        __builtin_amdgcn_sched_barrier(0);
       } else {
 #pragma unroll
         for (int s = 0; s < 4; ++s)
@@ -864,84 +895,81 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
             o[c] = Type<T>::dot32(w.v, pv[s], o[c]);
           }
       }
-      if (mixed(i)) {  // infinities and NaN of V, left out of the product above, to the rows that see them
-        const int b = k0 + i * kManyKeys;
-        unsigned long long odd = 0;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) odd |= sh.odd[i & 1][w];
-        while (odd) {
-          const int key = __builtin_ctzll(odd);
-          odd &= odd - 1;
-          float e = 0.0f;
-          const int at = (key >> 5) * 16 + ((key >> 3) & 3) * 4 + (key & 3);
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (j == at) e = (float)pv[j >> 3][j & 7];
-          e = __shfl(e, ((key >> 2) & 1) * 32 + col);
-          const int u = b + key;
-          const bool seen = u <= pos && (!a.window || u > pos - a.window);
-          const T *vs = (const T *)a.v + (int64_t)table[u >> a.shift] * a.v_page + (int64_t)(u & (P - 1)) * a.v_slot +
-                        (int64_t)h * a.v_head;
-#pragma unroll
-          for (int c = 0; c < DT; ++c)
-#pragma unroll
-            for (int j = 0; j < 16; j += 4)
-              add_odd<T>(vs, c * 32 + 2 * j + 4 * half, a.D, e, seen, [&](int k, float y) { o[c][j + k] += y; });
-        }
-      }
     };
 
     // ------------------------------------------------ the walk, in two phases a tile
-    // Products of a phase (O += P V of the tile before, S = K Q of this one) and the
-    // softmax after them alternate behind barriers.  Half of the waves, one of the
-    // two on each SIMD, run a phase behind, so that one wave's products go beside
-    // the other's softmax.  Stage s is K of tile s + 1 and V of tile s, which must be in
-    // LDS before the products of tile s + 1: a wave stores its share and loads the next
-    // stage's in its softmax phases, late waves a stage further.
+    // Products (O += P V of the tile before, S = K Q of this one) and the softmax after
+    // them alternate behind barriers.  Half of the waves, one of the two on each
+    // SIMD, run a phase behind, so that one wave's products go beside the other's
+    // softmax.  Stage i is K of tile i + 1 and V of tile i, which must be in LDS before
+    // the products of tile i + 1; a wave stores its share of it among the products of
+    // tile i, when both buffers are free, and sets off the next stage's loads.  Where a
+    // wave has no more to see, its weights are zeros.
     const int late = NW == 8 && wave >= NW / 2 ? 1 : 0;
     sync();  // the last piece's tiles are done with
+    if (tid == 0) sh.odd = 0;
+    sync();
     if (n > 0) {
-      const int page0 = valid(0, find(0)), page1 = valid(1, find(1)), page2 = valid(2, find(2)),
-                page3 = valid(3, find(3));
-      int pv_page = late ? page2 : page1, pk_page = late ? page3 : page2;
-      int next_page = find(late + 3);  // not looked at before its time: that would wait for the loads before it
-      // keys of this tile and the next two that are there
-      unsigned long long live0 = __builtin_amdgcn_ballot_w64(page0 >= 0),
-                         live1 = __builtin_amdgcn_ballot_w64(page1 >= 0),
-                         live2 = __builtin_amdgcn_ballot_w64(page2 >= 0);
+      const int page0 = valid(0, find(0));
+      int v_pg = valid(1, find(1)), k_pg = valid(2, find(2));  // pages of stage i + 1 (V, K), while stage i is at hand
+      int next_pg = find(3);  // not looked at before its time: that would wait for the loads before it
+      unsigned long long live = live_of(0, page0), live1 = live_of(1, v_pg), live2 = live_of(2, k_pg);
       load_k(0, page0);
-      store_k(0, live0);
-      load_k(1, page1);
+      clean(kr, live);
+      store(sh.k[0], kr);
+      load_k(1, v_pg);
       load_v(0, page0);
+      clean(kr, live1);
+      clean_v(0, live);
       sync();
-      if (late) {
-        store_k(1, live1);
-        store_v(0, live0);
-        load_k(2, page2);
-        load_v(1, page1);
-        sync();
-      }
+      if (late) sync();
       for (int i = 0; i < n; ++i) {
-        if (active(i)) scores(i);
-        if (i > 0 && active(i - 1)) values(i - 1);
+        scores(i);
+        // stage i: K of tile i + 1, V of tile i
+        store(sh.k[(i + 1) & 1], kr);
+        store(sh.v[i & 1], vr);
+        load_k(i + 2, k_pg);
+        load_v(i + 1, v_pg);
+        __builtin_amdgcn_sched_barrier(0);
+        if (i > 0) values(i - 1);
         sync();
-        if (active(i)) weights(i, live0);
-        // past the piece's last tile these store what nobody reads
-        store_k(i + late + 1, late ? live2 : live1);
-        store_v(i + late, late ? live1 : live0);
-        load_k(i + late + 2, pk_page);
-        load_v(i + late + 1, pv_page);
-        const unsigned long long live = __builtin_amdgcn_ballot_w64(pk_page >= 0);
-        live0 = live1;
-        live1 = late ? live2 : live;
-        live2 = live;
-        pv_page = pk_page;
-        pk_page = valid(i + late + 3, next_page);
-        next_page = find(i + late + 4);
+        // among the softmax: what the stage on its way needs before it goes to LDS, and the next one's pages
+        weights(i, live);
+        if (live2 != ~0ull || a.D != DP) clean(kr, live2);
+        if (live1 != ~0ull || a.D != DP || mixed(i + 1)) clean_v(i + 1, live1);
+        v_pg = k_pg;
+        k_pg = valid(i + 3, next_pg);
+        live = live1, live1 = live2, live2 = live_of(i + 3, k_pg);
+        next_pg = find(i + 4);
         sync();
       }
-      if (active(n - 1)) values(n - 1);
+      values(n - 1);
       if (!late) sync();
+      sync();
+      if (sh.odd) {  // rare
+        for (int i = 0; i < n; ++i)
+          if (mixed(i))
+            for (int key = 0; key < kManyKeys; ++key) {
+              const int u = k0 + i * kManyKeys + key;
+              const int page = u < hi ? table[u >> a.shift] : -1;
+              if ((unsigned)page >= (unsigned)a.pages) continue;
+              const T *vs = (const T *)a.v + page * a.v_page + (u & (P - 1)) * a.v_slot + (int64_t)h * a.v_head;
+              if (!has_odd<T>(vs, a.D, lane)) continue;
+              const T *ks = (const T *)a.k + page * a.k_page + (u & (P - 1)) * a.k_slot + (int64_t)h * a.k_head;
+              float s = 0.0f;
+#pragma unroll
+              for (int c = 0; c < KS; ++c) s += dot8<T>(q[c], ks, c * 16 + half * 8, a.D);
+              s = sum_across_32(s);
+              if constexpr (sizeof(T) == 4) s *= a.scale2;
+              const float e = exp2_of((s - m) * sc);
+              const bool seen = u <= pos && (!a.window || u > pos - a.window);
+#pragma unroll
+              for (int c = 0; c < DT; ++c)
+#pragma unroll
+                for (int j = 0; j < 16; j += 4)
+                  add_odd<T>(vs, c * 32 + 2 * j + 4 * half, a.D, e, seen, [&](int k, float y) { o[c][j + k] += y; });
+            }
+      }
     }
 
     // ------------------------------------------------ out, or to the join

@@ -58,7 +58,7 @@ int run_few(const Launch &l, AttendArgs a, int most_rows) {
                 a);
 }
 
-template <class T, int DP, int NW>
+template <class T, int DP, int NW, bool ONE_PAGE>
 int run_many(const Launch &l, AttendArgs a) {
   constexpr int ROWS = 32 * NW;
   a.target = l.cus * kManyPerCu;
@@ -68,7 +68,7 @@ int run_many(const Launch &l, AttendArgs a) {
   const int64_t slots = 2 * (int64_t)a.target;
   int rc = partials<ROWS, DP>(l, slots, a);
   if (rc != SPARSELNR_OK) return rc;
-  rc = launch(attend_many<T, DP, NW>, dim3((unsigned)pieces), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
+  rc = launch(attend_many<T, DP, NW, ONE_PAGE>, dim3((unsigned)pieces), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
   if (rc != SPARSELNR_OK) return rc;
   return launch(join_many<T, DP, ROWS>, dim3((unsigned)slots, ROWS / kJoinRows), kJoinBlock, 0, l, a);
 }
@@ -83,7 +83,9 @@ int run_attend(const Launch &l, AttendArgs a, int64_t max_new) {
     if (rows > kFewMostRows) {
       constexpr int NW = sizeof(T) == 4 || DP > 128 ? 4 : 8;
       a.few = kFewMostRows;
-      const int rc = run_many<T, DP, NW>(l, a);
+      // a tile of keys within one page, 64 rows of it within 32 bits of bytes
+      const bool one_page = a.shift >= 6 && a.k_slot < (1 << 23) && a.v_slot < (1 << 23);
+      const int rc = one_page ? run_many<T, DP, NW, true>(l, a) : run_many<T, DP, NW, false>(l, a);
       if (rc != SPARSELNR_OK) return rc;
     }
   }
