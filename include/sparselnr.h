@@ -280,7 +280,7 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *   - R = 0 or T = 0 is a no-op.
  *   - The two attention calls use a workspace per (device, stream) for the
  *     results of contexts that are cut into pieces; its size depends on the
- *     type and dim class alone (at most 68 MB), so that one call of a kind allocates it,
+ *     type and dim class alone (at most 140 MB), so that one call of a kind allocates it,
  *     later ones and captured graphs find it whatever the lengths are.
  * ---------------------------------------------------------------------- */
 

@@ -117,27 +117,51 @@ __device__ __forceinline__ Request request_of(const AttendArgs &a, int r) {
 //
 // A tile is up to ROWS rows (token, head of the group) of one request and KV head.
 // Tiles whose keys take more than `cap` steps are cut into np equal pieces of the
-// key axis, whose results attend_join adds up; cap is such that all the work makes
+// key axis, whose results the join adds up; cap is such that all the work makes
 // about `target` pieces, so long contexts are cut where there are few tiles and
-// left whole where there are many.  Every block derives the split from the
-// lengths by one scan: nothing has to be planned, copied or known on the host.
+// left whole where there are many.  With a tail, the tiles behind the first 70% of the
+// work are cut kTailCuts times finer: the blocks that are done early find something
+// to fill the time with until the longest one is done (520 tiles on 256 compute
+// units: three rounds, the last with 8 tiles, become little more than two).
+// Every block derives the split from the lengths by one scan: nothing has to be
+// planned, copied or known on the host.
+
+constexpr int kTailCuts = 3;
 
 template <int NT>
 struct Split {
-  int begin[NT];  // pieces (of one KV head) before this thread's requests
-  int slot[NT];   // the same of split tiles only
+  int begin[NT];         // pieces (of one KV head) before this thread's requests
+  int slot[NT];          // the same of split tiles only
+  long long before[NT];  // steps before them
   long long work[NT / kWave];
   int wave_a[NT / kWave], wave_b[NT / kWave];
-  int total, total_split, cap, per;
+  long long whole;       // steps up to which tiles are cut by cap, behind them by cap_tail
+  int total, total_split, cap, cap_tail, per;
 };
 
 struct Piece {
   int r, tile, part, np, slot;  // slot < 0: the tile is whole
 };
 
+// A request's tiles before the tail, and the pieces of a tile before and in it.
+struct Cut {
+  int front, np, np_tail;
+};
+
+template <int NT>
+__device__ __forceinline__ Cut cut_of(const Split<NT> &sh, long long before, int tiles, int steps) {
+  Cut c;
+  const int s = imax(steps, 1);
+  const long long left = sh.whole - before;
+  c.front = left <= 0 ? 0 : left >= (long long)tiles * s ? tiles : (int)((left + s - 1) / s);
+  c.np = (s + sh.cap - 1) / sh.cap;
+  c.np_tail = (s + sh.cap_tail - 1) / sh.cap_tail;
+  return c;
+}
+
 // count(r, tiles, steps) gives a request's tiles and the steps of its longest one.
 template <int NT, class F>
-__device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, F count) {
+__device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, bool tail, F count) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.R + NT - 1) / NT;
   const int r0 = imin(tid * per, a.R), r1 = imin(r0 + per, a.R);
@@ -147,22 +171,39 @@ __device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, F 
     count(r, tiles, steps);
     w += (long long)tiles * imax(steps, 1);
   }
+  long long upto = w;
 #pragma unroll
-  for (int o = 32; o; o >>= 1) w += __shfl_xor(w, o);
-  if (lane == 0) sh.work[wave] = w;
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 63) sh.work[wave] = upto;
   __syncthreads();
   long long all = 0;
 #pragma unroll
-  for (int i = 0; i < NT / kWave; ++i) all += sh.work[i];
-  const long long want = (all * a.Hkv + a.target - 1) / a.target;
-  const int cap = imax(min_steps, (int)(want < (1 << 28) ? want : (1 << 28)));
+  for (int i = 0; i < NT / kWave; ++i) {
+    if (i < wave) upto += sh.work[i];
+    all += sh.work[i];
+  }
+  if (tid == 0) {
+    const long long want = (all * a.Hkv + a.target - 1) / a.target;
+    sh.cap = imax(min_steps, (int)(want < (1 << 28) ? want : (1 << 28)));
+    sh.cap_tail = tail ? imax(min_steps, (sh.cap + kTailCuts - 1) / kTailCuts) : sh.cap;
+    sh.whole = tail ? all - all * 3 / 10 : all;
+    sh.per = per;
+  }
+  __syncthreads();
   int np = 0, ns = 0;
+  long long before = upto - w;
+  sh.before[tid] = before;
   for (int r = r0; r < r1; ++r) {
     int tiles, steps;
     count(r, tiles, steps);
-    const int k = imax((steps + cap - 1) / cap, 1);
-    np += tiles * k;
-    ns += k > 1 ? tiles * k : 0;
+    const Cut c = cut_of(sh, before, tiles, steps);
+    before += (long long)tiles * imax(steps, 1);
+    const int x = c.front * c.np, y = (tiles - c.front) * c.np_tail;
+    np += x + y;
+    ns += (c.np > 1 ? x : 0) + (c.np_tail > 1 ? y : 0);
   }
   int x = np, y = ns;
 #pragma unroll
@@ -181,14 +222,16 @@ __device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, F 
   }
   sh.begin[tid] = bx + x - np;
   sh.slot[tid] = by + y - ns;
-  if (tid == 0) sh.total = total, sh.total_split = total_split, sh.cap = cap, sh.per = per;
+  if (tid == 0) sh.total = total, sh.total_split = total_split;
   __syncthreads();
 }
 
 // The piece number q of one KV head, 0 <= q < total.
 template <int NT, class F>
 __device__ Piece split_find(const Split<NT> &sh, const AttendArgs &a, int q, F count) {
-  int lo = 0, hi = NT - 1;  // the last thread that begins at or before q
+  // the last thread that begins at or before q (those without pieces begin where the
+  // next one does)
+  int lo = 0, hi = NT - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (sh.begin[mid] <= q)
@@ -196,27 +239,31 @@ __device__ Piece split_find(const Split<NT> &sh, const AttendArgs &a, int q, F c
     else
       hi = mid - 1;
   }
-  // threads without pieces begin where the next one does; the last of them with
-  // begin <= q is the one that holds q
-  int r = lo * sh.per;
   int left = q - sh.begin[lo], slot = sh.slot[lo];
+  long long before = sh.before[lo];
   Piece p{};
-  for (; r < a.R; ++r) {
+  for (int r = lo * sh.per; r < a.R; ++r) {
     int tiles, steps;
     count(r, tiles, steps);
-    const int np = imax((steps + sh.cap - 1) / sh.cap, 1);
-    const int here = tiles * np;
-    if (left < here) {
+    const Cut c = cut_of(sh, before, tiles, steps);
+    before += (long long)tiles * imax(steps, 1);
+    const int x = c.front * c.np, y = (tiles - c.front) * c.np_tail;
+    if (left < x + y) {
+      const bool in_tail = left >= x;
+      if (in_tail) {
+        left -= x;
+        if (c.np > 1) slot += x;
+      }
       p.r = r;
-      p.np = np;
-      const int t = left / np;
-      p.tile = tiles - 1 - t;  // the longest (last) tile of a causal chunk first
-      p.part = left - t * np;
-      p.slot = np > 1 ? slot + left : -1;
+      p.np = in_tail ? c.np_tail : c.np;
+      const int t = left / p.np;
+      p.tile = tiles - 1 - (in_tail ? c.front + t : t);  // the longest (last) tile of a causal chunk first
+      p.part = left - t * p.np;
+      p.slot = p.np > 1 ? slot + left : -1;
       return p;
     }
-    left -= here;
-    if (np > 1) slot += here;
+    left -= x + y;
+    slot += (c.np > 1 ? x : 0) + (c.np_tail > 1 ? y : 0);
   }
   p.r = -1;
   return p;
@@ -283,7 +330,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
     total = a.T * row_tiles * np_sparse;
     used = np_sparse > 1 ? total : 0;
   } else {
-    split_scan<kFewBlock>(sh.split, a, 1, count);
+    split_scan<kFewBlock>(sh.split, a, 1, false, count);
     total = sh.split.total;
     used = sh.split.total_split;
   }
@@ -602,7 +649,7 @@ constexpr int kManyKeys = 64;
 constexpr float kLag = 8.0f;      // the maximum that weights are taken at may be so many powers of two low
 // Instruction classes of sched_group_barrier.
 constexpr int kMfma = 0x008, kDsRead = 0x100;
-constexpr int kManyMinSteps = 4;  // a piece is at least so many tiles of keys long
+constexpr int kManyMinSteps = 8;  // a piece is at least so many tiles of keys long
 
 //
 // ONE_PAGE: every tile of 64 keys lies in one page (64 positions and more, which begin
@@ -630,7 +677,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     const int lo = (a.window ? imax(q.S - q.n - a.window + 1, 0) : 0) & -kManyKeys;
     steps = (q.S - lo + kManyKeys - 1) / kManyKeys;
   };
-  split_scan<NT>(sh.split, a, kManyMinSteps, count);
+  split_scan<NT>(sh.split, a, kManyMinSteps, true, count);
   const int total = sh.split.total;
   if (blockIdx.x == 0 && tid == 0) a.meta[0] = sh.split.total_split * a.Hkv;
 

@@ -62,10 +62,13 @@ template <class T, int DP, int NW, bool ONE_PAGE>
 int run_many(const Launch &l, AttendArgs a) {
   constexpr int ROWS = 32 * NW;
   a.target = l.cus * kManyPerCu;
-  const int64_t tiles = (int64_t)a.T * a.G / ROWS + a.R;
-  const int64_t pieces = tiles * a.Hkv + a.target;
+  const int64_t tiles = ((int64_t)a.T * a.G / ROWS + a.R) * a.Hkv;
+  // Of split_scan: a tile of x caps makes at most x + 1 and, if it is cut, at most 2 x pieces;
+  // the work is `target` caps, three tenths of it (and what a tile reaches over) of a kTailCuts-th.
+  const int64_t caps = (int64_t)a.target + (int64_t)a.target * kTailCuts * 3 / 10 + kTailCuts;
+  const int64_t pieces = tiles + caps;
   if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
-  const int64_t slots = 2 * (int64_t)a.target;
+  const int64_t slots = 2 * caps;
   int rc = partials<ROWS, DP>(l, slots, a);
   if (rc != SPARSELNR_OK) return rc;
   rc = launch(attend_many<T, DP, NW, ONE_PAGE>, dim3((unsigned)pieces), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
