@@ -158,9 +158,15 @@ def sparselnr_release() -> None:
 
 # ------------------------------------------------------------ marshalling
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _check(t, name, dtype, device, ndim=None):
@@ -433,8 +439,25 @@ def sparselnr_validate_csr(rowptr, colidx, M, stream=None) -> int:
 
 
 # ------------------------------------------------------------ paged cache
+#
+# These calls run once per layer and decode step, where the GPU is done in a few
+# microseconds: arguments are looked at in one expression first, and one by one, for the
+# message, only if that fails.
 
 _DTYPES = {}
+_raw_stream = None
+
+
+def _launch_stream(stream, index):
+    """The raw stream: the one given, or the current one of GPU `index`."""
+    global _raw_stream
+    if stream is not None:
+        return getattr(stream, "cuda_stream", stream)
+    if _raw_stream is None:
+        torch = _torch()
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _raw_stream(index)
 
 
 def _dtype_code(t, name):
@@ -447,62 +470,75 @@ def _dtype_code(t, name):
     return code
 
 
-def _rows(t, name, dims, dtype, device):
-    """t of rows of adjacent values, any other strides."""
-    if not isinstance(t, _torch().Tensor):
-        raise TypeError("%s must be a torch.Tensor" % name)
+def _gpu(t, name):
+    """Index of the GPU that tensor t is on."""
+    try:
+        index = t.get_device()
+    except AttributeError:
+        raise TypeError("%s must be a torch.Tensor" % name) from None
+    if index < 0 or not t.is_cuda:
+        raise ValueError("inputs must be on a GPU device")
+    return index
+
+
+def _rows(t, name, dims, dtype, index):
+    """Strides of t, whose rows (the last dimension) are adjacent values."""
+    try:
+        s = t.stride()
+        if len(s) == dims and t.dtype is dtype and t.get_device() == index and (s[-1] == 1 or t.shape[-1] <= 1):
+            return s
+    except AttributeError:
+        raise TypeError("%s must be a torch.Tensor" % name) from None
     if t.dim() != dims:
         raise ValueError("%s must have %d dimensions" % (name, dims))
-    if t.device != device:
-        raise ValueError("%s is on %s, expected %s" % (name, t.device, device))
+    if t.get_device() != index:
+        raise ValueError("%s is on %s, expected GPU %d" % (name, t.device, index))
     if t.dtype != dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    s = t.stride()
-    if s[-1] != 1 and t.shape[-1] > 1:
-        raise ValueError("the last dimension of %s must be contiguous" % name)
-    return s
+    raise ValueError("the last dimension of %s must be contiguous" % name)
 
 
-def _gpu(t, name):
-    if not isinstance(t, _torch().Tensor):
-        raise TypeError("%s must be a torch.Tensor" % name)
-    if t.device.type != "cuda":
-        raise ValueError("inputs must be on a GPU device")
-    return t.device
+def _packed(t, name, dtype, index, shape):
+    """Address of t, densely packed and of that shape."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError("%s must be a torch.Tensor" % name) from None
+    if t.get_device() != index:
+        raise ValueError("%s is on %s, expected GPU %d" % (name, t.device, index))
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must be %s, got %s" % (name, " x ".join(map(str, shape)), tuple(t.shape)))
+    raise ValueError("%s must be contiguous" % name)
 
 
-def _table(table, device):
-    """Row stride and width of a block table; its rows need not be adjacent."""
-    stride, _ = _rows(table, "table", 2, _torch().int32, device)
+def _table(table, index):
+    """Row stride, rows and width of a block table; its rows need not be adjacent."""
+    stride = _rows(table, "table", 2, _torch().int32, index)[0]
     R, W = table.shape
     return (stride if R > 1 else max(stride, W)), R, W
 
 
 def _cache(kcache, vcache):
-    device = _gpu(kcache, "kcache")
+    index = _gpu(kcache, "kcache")
     code = _dtype_code(kcache, "kcache")
-    ks = _rows(kcache, "kcache", 4, kcache.dtype, device)
-    vs = _rows(vcache, "vcache", 4, kcache.dtype, device)
+    dtype = kcache.dtype
+    ks = _rows(kcache, "kcache", 4, dtype, index)
+    vs = _rows(vcache, "vcache", 4, dtype, index)
     shape = kcache.shape
     if vcache.shape != shape:
         raise ValueError("kcache and vcache differ in shape")
-    return device, shape, _KvCache(kcache.data_ptr(), vcache.data_ptr(), *shape, *ks[:3], *vs[:3], code)
+    return index, shape, _KvCache(kcache.data_ptr(), vcache.data_ptr(), *shape, ks[0], ks[1], ks[2], vs[0], vs[1],
+                                  vs[2], code)
 
 
-def _requests(table, seq_len, qptr, T, device):
-    torch = _torch()
-    stride, R, W = _table(table, device)
-    _check(seq_len, "seq_len", torch.int32, device, 1)
-    _check(qptr, "qptr", torch.int32, device, 1)
-    if seq_len.numel() != R or qptr.numel() != R + 1:
-        raise ValueError("seq_len and qptr must have R and R + 1 entries for R = %d rows of table" % R)
-    return _Requests(table.data_ptr(), stride, seq_len.data_ptr(), qptr.data_ptr(), R, W, T)
-
-
-def _page_size(page_size):
-    if not isinstance(page_size, int) or page_size < 1:
-        raise ValueError("page_size must be a positive integer")
-    return page_size
+def _requests(table, seq_len, qptr, T, index):
+    int32 = _torch().int32
+    stride, R, W = _table(table, index)
+    return _Requests(table.data_ptr(), stride, _packed(seq_len, "seq_len", int32, index, (R,)),
+                     _packed(qptr, "qptr", int32, index, (R + 1,)), R, W, T)
 
 
 def sparselnr_page_tables(ctx_len, new_len, table, free_pages, tokens, page_size, qptr=None, seq_len=None,
@@ -513,49 +549,29 @@ def sparselnr_page_tables(ctx_len, new_len, table, free_pages, tokens, page_size
     free_pages: int32[F].  Returns (qptr int32[R + 1], seq_len int32[R], slots
     int64[tokens], counts int32[3]), in the tensors given for them if any."""
     torch = _torch()
-    device = _gpu(ctx_len, "ctx_len")
-    _check(ctx_len, "ctx_len", torch.int32, device, 1)
-    _check(new_len, "new_len", torch.int32, device, 1)
-    _check(free_pages, "free_pages", torch.int32, device, 1)
-    stride, R, W = _table(table, device)
-    if ctx_len.numel() != R or new_len.numel() != R:
-        raise ValueError("ctx_len and new_len must have one entry per row of table")
+    int32 = torch.int32
+    index = _gpu(ctx_len, "ctx_len")
+    stride, R, W = _table(table, index)
+    F = free_pages.numel() if isinstance(free_pages, torch.Tensor) else 0
+    args = (_packed(ctx_len, "ctx_len", int32, index, (R,)), _packed(new_len, "new_len", int32, index, (R,)),
+            table.data_ptr(), stride, _packed(free_pages, "free_pages", int32, index, (F,)))
     if tokens < 0:
         raise ValueError("tokens must not be negative")
+    device = ctx_len.device
     if qptr is None and seq_len is None and counts is None:
         # one allocation for the three
-        ints = torch.empty(2 * R + 4, dtype=torch.int32, device=device)
-        qptr, seq_len, counts = ints[:R + 1], ints[R + 1:2 * R + 1], ints[2 * R + 1:]
-    else:
-        qptr = _given(qptr, "qptr", R + 1, torch.int32, device)
-        seq_len = _given(seq_len, "seq_len", R, torch.int32, device)
-        counts = _given(counts, "counts", 3, torch.int32, device)
-    slots = _given(slots, "slots", tokens, torch.int64, device)
+        qptr, seq_len, counts = torch.empty(2 * R + 4, dtype=int32, device=device).split_with_sizes((R + 1, R, 3))
+    qptr = torch.empty(R + 1, dtype=int32, device=device) if qptr is None else qptr
+    seq_len = torch.empty(R, dtype=int32, device=device) if seq_len is None else seq_len
+    counts = torch.empty(3, dtype=int32, device=device) if counts is None else counts
+    slots = torch.empty(tokens, dtype=torch.int64, device=device) if slots is None else slots
     rc = lib().sparselnr_page_tables(
-        ctx_len.data_ptr(), new_len.data_ptr(), table.data_ptr(), stride, free_pages.data_ptr(), qptr.data_ptr(),
-        seq_len.data_ptr(), slots.data_ptr(), counts.data_ptr(), R, W, free_pages.numel(), tokens,
-        _page_size(page_size), _stream(stream, device))
+        *args, _packed(qptr, "qptr", int32, index, (R + 1,)), _packed(seq_len, "seq_len", int32, index, (R,)),
+        _packed(slots, "slots", torch.int64, index, (tokens,)), _packed(counts, "counts", int32, index, (3,)), R, W, F,
+        tokens, page_size, _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_page_tables")
     return qptr, seq_len, slots, counts
-
-
-def _given(t, name, n, dtype, device):
-    if t is None:
-        return _torch().empty(n, dtype=dtype, device=device)
-    _check(t, name, dtype, device, 1)
-    if t.numel() != n:
-        raise ValueError("%s must have %d entries" % (name, n))
-    return t
-
-
-def _summaries(kq, kscale, device):
-    torch = _torch()
-    _check(kq, "kq", torch.int8, device, 3)
-    _check(kscale, "kscale", torch.float32, device, 2)
-    if kscale.shape != kq.shape[:2]:
-        raise ValueError("kscale must be pages x Hkv, as kq")
-    return kq.shape
 
 
 def sparselnr_cache_append(k, v, slots, kcache, vcache, kq=None, kscale=None, stream=None):
@@ -563,51 +579,43 @@ def sparselnr_cache_append(k, v, slots, kcache, vcache, kq=None, kscale=None, st
     kcache and vcache (pages x page_size x Hkv x D, any order of memory), and renews
     the written pages' summaries kq (int8 pages x Hkv x D), kscale (float32 pages x Hkv)."""
     torch = _torch()
-    device, shape, cache = _cache(kcache, vcache)
-    ks = _rows(k, "k", 3, kcache.dtype, device)
-    vs = _rows(v, "v", 3, kcache.dtype, device)
+    index, shape, cache = _cache(kcache, vcache)
+    ks = _rows(k, "k", 3, kcache.dtype, index)
+    vs = _rows(v, "v", 3, kcache.dtype, index)
     T = k.shape[0]
     if k.shape != v.shape or k.shape[1:] != shape[2:]:
         raise ValueError("k and v must be T x Hkv x D, as the cache's rows")
-    _check(slots, "slots", torch.int64, device, 1)
-    if slots.numel() != T:
-        raise ValueError("slots must have one entry per token")
     if (kq is None) != (kscale is None):
         raise ValueError("kq and kscale go together")
-    if kq is not None and _summaries(kq, kscale, device) != (shape[0], shape[2], shape[3]):
-        raise ValueError("kq must be pages x Hkv x D")
-    rc = lib().sparselnr_cache_append(
-        k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], slots.data_ptr(), cache,
-        kq.data_ptr() if kq is not None else None, kscale.data_ptr() if kq is not None else None, T,
-        _stream(stream, device))
+    kq_at = ks_at = None
+    if kq is not None:
+        kq_at = _packed(kq, "kq", torch.int8, index, (shape[0], shape[2], shape[3]))
+        ks_at = _packed(kscale, "kscale", torch.float32, index, (shape[0], shape[2]))
+    rc = lib().sparselnr_cache_append(k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                                      _packed(slots, "slots", torch.int64, index, (T,)), cache, kq_at, ks_at, T,
+                                      _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_cache_append")
 
 
 def _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse):
     torch = _torch()
-    device, shape, cache = _cache(kcache, vcache)
-    qs = _rows(q, "q", 3, kcache.dtype, device)
+    index, shape, cache = _cache(kcache, vcache)
+    dtype = kcache.dtype
+    qs = _rows(q, "q", 3, dtype, index)
     T, Hq, D = q.shape
     if D != shape[3]:
         raise ValueError("q and the cache differ in head dimension")
     if shape[2] == 0 or Hq % shape[2]:
         raise ValueError("query heads must be a multiple of the cache's heads")
-    requests = _requests(table, seq_len, qptr, T, device)
+    requests = _requests(table, seq_len, qptr, T, index)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=q.dtype, device=device)
+        out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
     else:
-        _check(out, "out", q.dtype, device, 3)
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
-    if lse is not None:
-        _check(lse, "lse", torch.float32, device, 2)
-        if lse.shape != q.shape[:2]:
-            raise ValueError("lse must be T x Hq")
-    if scale is None:
-        scale = D ** -0.5
-    return (device, out, (q.data_ptr(), qs[0], qs[1], Hq, cache, requests), scale,
-            lse.data_ptr() if lse is not None else None)
+        _packed(out, "out", dtype, index, (T, Hq, D))
+    lse_at = None if lse is None else _packed(lse, "lse", torch.float32, index, (T, Hq))
+    return (index, out, (q.data_ptr(), qs[0], qs[1], Hq, cache, requests), D ** -0.5 if scale is None else scale,
+            lse_at)
 
 
 def sparselnr_paged_attention(q, kcache, vcache, table, seq_len, qptr, scale=None, window=0, max_new=0, out=None,
@@ -616,9 +624,9 @@ def sparselnr_paged_attention(q, kcache, vcache, table, seq_len, qptr, scale=Non
     cached rows of their requests.  scale defaults to D ** -0.5; window > 0 bounds
     how far back a token sees; max_new > 0 says that no request has more new
     tokens.  lse (float32 T x Hq), if given, is filled.  Returns out (T x Hq x D)."""
-    device, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse)
+    index, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse)
     rc = lib().sparselnr_paged_attention(*head, scale, window, max_new, out.data_ptr(), lse,
-                                         _stream(stream, device))
+                                         _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_paged_attention")
     return out
@@ -630,25 +638,26 @@ def sparselnr_block_select(q, kq, kscale, table, seq_len, qptr, page_size, top, 
     and last `local` ones and the best by the 8-bit score.  Returns sel (int32
     T x Hkv x top): indices into the table row, ascending, -1 behind them."""
     torch = _torch()
-    device = _gpu(q, "q")
+    index = _gpu(q, "q")
     code = _dtype_code(q, "q")
-    qs = _rows(q, "q", 3, q.dtype, device)
+    qs = _rows(q, "q", 3, q.dtype, index)
     T, Hq, D = q.shape
-    pages, Hkv, Dk = _summaries(kq, kscale, device)
+    if not isinstance(kq, torch.Tensor) or kq.dim() != 3:
+        raise ValueError("kq must have 3 dimensions")
+    pages, Hkv, Dk = kq.shape
     if Dk != D:
         raise ValueError("q and kq differ in head dimension")
     if Hkv == 0 or Hq % Hkv:
         raise ValueError("query heads must be a multiple of the summaries' heads")
-    requests = _requests(table, seq_len, qptr, T, device)
+    kq_at = _packed(kq, "kq", torch.int8, index, (pages, Hkv, D))
+    ks_at = _packed(kscale, "kscale", torch.float32, index, (pages, Hkv))
+    requests = _requests(table, seq_len, qptr, T, index)
     if sel is None:
-        sel = torch.empty((T, Hkv, top), dtype=torch.int32, device=device)
+        sel = torch.empty((T, Hkv, max(top, 0)), dtype=torch.int32, device=q.device)
     else:
-        _check(sel, "sel", torch.int32, device, 3)
-        if sel.shape != (T, Hkv, top):
-            raise ValueError("sel must be T x Hkv x top")
-    rc = lib().sparselnr_block_select(
-        q.data_ptr(), qs[0], qs[1], Hq, code, kq.data_ptr(), kscale.data_ptr(), pages, _page_size(page_size), Hkv,
-        D, requests, top, first, local, sel.data_ptr(), _stream(stream, device))
+        _packed(sel, "sel", torch.int32, index, (T, Hkv, top))
+    rc = lib().sparselnr_block_select(q.data_ptr(), qs[0], qs[1], Hq, code, kq_at, ks_at, pages, page_size, Hkv, D,
+                                      requests, top, first, local, sel.data_ptr(), _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_block_select")
     return sel
@@ -658,13 +667,12 @@ def sparselnr_block_attention(q, kcache, vcache, table, seq_len, qptr, sel, scal
                               stream=None):
     """As sparselnr_paged_attention, over the pages sel (int32 T x Hkv x top) of each
     token and KV head only.  Returns out (T x Hq x D)."""
-    device, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse)
-    _check(sel, "sel", _torch().int32, device, 3)
-    T, Hkv, top = sel.shape
-    if T != q.shape[0] or Hkv != kcache.shape[2]:
-        raise ValueError("sel must be T x Hkv x top")
-    rc = lib().sparselnr_block_attention(*head, sel.data_ptr(), top, scale, out.data_ptr(), lse,
-                                         _stream(stream, device))
+    index, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse)
+    if not isinstance(sel, _torch().Tensor) or sel.dim() != 3:
+        raise ValueError("sel must have 3 dimensions")
+    top = sel.shape[2]
+    sel_at = _packed(sel, "sel", _torch().int32, index, (q.shape[0], kcache.shape[2], top))
+    rc = lib().sparselnr_block_attention(*head, sel_at, top, scale, out.data_ptr(), lse, _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_block_attention")
     return out
