@@ -32,6 +32,74 @@ __device__ __forceinline__ unsigned rank_of(float s) {
   return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
 }
 
+// The largest `cut` that at least `top` of the wave's values reach (there are more than
+// `top` values above 0), found bit by bit; `reach` is how many do.
+__device__ __forceinline__ unsigned kth_largest(unsigned v, int top, int &reach) {
+  unsigned cut = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const unsigned next = cut | (1u << bit);
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(v >= next));
+    if (c >= top) {
+      cut = next;
+      reach = c;
+      if (c == top) break;
+    }
+  }
+  return cut;
+}
+
+constexpr int kSelectFew = 64;  // as many pages as a wave has lanes
+
+// The `top` <= 64 largest of a wave's values above 0, v[i] in lane l being number 64 i + l,
+// equal ones by the lowest number: lane e < kept gets the e-th of them in the order of
+// the numbers.  The top-th largest of the lanes' maxima bounds the answer from
+// below, and few values are above it; they are put one to a lane through `room` (128
+// words), where the search goes on.  False, if there are more than 64 of them.
+template <int NR>
+__device__ __forceinline__ bool choose_few(const unsigned (&v)[NR], int top, unsigned *room, int lane, int &kept,
+                                           unsigned &key, int &number) {
+  unsigned most = v[0];
+#pragma unroll
+  for (int i = 1; i < NR; ++i) most = most > v[i] ? most : v[i];
+  unsigned low = 1;
+  int reach = 0;
+  if (__popcll(__builtin_amdgcn_ballot_w64(most > 0)) > top) low = kth_largest(most, top, reach);
+  int n = 0;
+  const unsigned long long below = (1ull << lane) - 1;
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    const unsigned long long b = __builtin_amdgcn_ballot_w64(v[i] >= low);
+    if (b) {
+      const int at = n + __popcll(b & below);
+      if (v[i] >= low && at < kWave) {
+        room[at] = v[i];
+        room[kWave + at] = i * kWave + lane;
+      }
+      n += __popcll(b);
+    }
+  }
+  if (n > kWave) return false;
+  key = lane < n ? room[lane] : 0;
+  number = lane < n ? (int)room[kWave + lane] : 0;
+  kept = n;
+  if (n > top) {
+    reach = n;
+    const unsigned c = kth_largest(key, top, reach);
+    const unsigned long long over = __builtin_amdgcn_ballot_w64(key > c), tied = __builtin_amdgcn_ballot_w64(key == c);
+    const int ties = top - __popcll(over);
+    const bool take = key > c || (key == c && __popcll(tied & below) < ties);
+    const unsigned long long b = __builtin_amdgcn_ballot_w64(take);
+    if (take) {
+      room[__popcll(b & below)] = key;
+      room[kWave + __popcll(b & below)] = number;
+    }
+    kept = top;
+    key = lane < kept ? room[lane] : 0;
+    number = lane < kept ? (int)room[kWave + lane] : 0;
+  }
+  return true;
+}
+
 // Scores: the group's query heads are added up in 64 bits, rounded once and cut to
 // 8 bits; its product with a page's 8-bit mean key is a whole number below 2^24,
 // exact on the integer matrix cores, and the page's step makes it the score.  So a
@@ -41,9 +109,11 @@ __device__ __forceinline__ unsigned rank_of(float s) {
 // x 64 products, one wave per token in the choice) or one (a decode step: all 16 waves
 // share the choice).  Scores stay in LDS as keys; a longer context is taken in
 // segments, the best so far carried in front of the next one, which keeps the
-// order of the indices.  The choice finds the k-th largest key bit by bit, a count
-// over the row per bit, and stops at the first prefix that exactly k keys reach;
-// equal keys at the end go by the lowest index.
+// order of the indices.  Up to 64 pages are chosen as choose_few says (one token: by every
+// wave among its pages, then by the first wave among those).  More of them, or
+// too many equal scores: the k-th largest key is found bit by bit, with a count over
+// the row per bit, up to the first prefix that exactly k keys reach; equal keys
+// at the end go by the lowest index.
 //
 // NR: keys of a row that a lane holds in the choice.
 template <class T, int DP, int TM, int NR>
@@ -58,6 +128,7 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
   int8_t *q8 = reinterpret_cast<int8_t *>(carried + TM * a.top + ((-TM * a.top) & 3));  // [16][DP + 16]
   constexpr int QS = DP + 16;
   int *count = reinterpret_cast<int *>(q8 + 16 * QS);               // [2][16] of the waves
+  unsigned *room = reinterpret_cast<unsigned *>(count + 2 * kSelectWaves) + (threadIdx.x >> 6) * 2 * kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, grp = lane >> 4;
   const int h = blockIdx.y;
@@ -124,49 +195,67 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
 #pragma unroll
   for (int i = 0; i < KS; ++i) qv[i] = *reinterpret_cast<const i32x4 *>(q8 + col * QS + i * 64 + grp * 16);
 
+  auto table_entry = [&](int b) { return b < blocks ? table[b] : -1; };
   const int my_token = TM == 1 ? 0 : wave;                   // row of the choice
-  const int room = a.capacity - a.top;                       // pages of a segment
+  const int room_of_segment = a.capacity - a.top;
   int held = 0;                                              // carried entries of my row
-  for (int seg = 0; seg == 0 || seg < blocks; seg += room) {
-    const int n = blocks - seg < room ? (blocks - seg > 0 ? blocks - seg : 0) : room;
+  for (int seg = 0; seg == 0 || seg < blocks; seg += room_of_segment) {
+    const int n = blocks - seg < room_of_segment ? (blocks - seg > 0 ? blocks - seg : 0) : room_of_segment;
     // ---------------------------------------------------- scores of a segment
-    for (int b0 = wave * 16; b0 < n; b0 += kSelectWaves * 16) {
-      const int b = seg + b0 + col;
-      int page = b < blocks ? table[b] : -1;
-      if ((unsigned)page >= (unsigned)a.pages) page = -1;
-      const int8_t *src = a.kq + ((int64_t)(page < 0 ? 0 : page) * a.Hkv + h) * a.D;
-      i32x4 acc{0, 0, 0, 0};
+    // Four groups of 16 pages at once: their entries, then their summaries are on
+    // their way together.
+    constexpr int U = 4;
+    for (int g0 = wave * 16; g0 < n; g0 += U * kSelectWaves * 16) {
+      int page[U];
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        const int d = i * 64 + grp * 16;
-        union {
-          i32x4 v;
-          uint2 u[2];
-        } w;
-        w.u[0] = *reinterpret_cast<const uint2 *>(d < a.D ? src + d : (const int8_t *)kZeroRow);
-        w.u[1] = *reinterpret_cast<const uint2 *>(d + 8 < a.D ? src + d + 8 : (const int8_t *)kZeroRow);
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w.v, qv[i], acc, 0, 0, 0);
+      for (int u = 0; u < U; ++u) {
+        const int b = seg + g0 + u * kSelectWaves * 16 + col;
+        page[u] = table_entry(b);
       }
-      const float scale = page < 0 ? 0.0f : a.kscale[(int64_t)page * a.Hkv + h];
-      unsigned k4[4];
+      i32x4 kv[U][KS];
+      float scale[U];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int from = grp * 4 + i;  // page of row 4 grp + i
-        const float sc = __shfl(scale, from);
-        const int pg = __shfl(page, from);
-        const int bb = seg + b0 + from;
+      for (int u = 0; u < U; ++u) {
+        if ((unsigned)page[u] >= (unsigned)a.pages) page[u] = -1;
+        const int64_t row = (int64_t)(page[u] < 0 ? 0 : page[u]) * a.Hkv + h;
+        const int8_t *src = page[u] < 0 ? (const int8_t *)kZeroRow : a.kq + row * a.D;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          const int d = i * 64 + grp * 16;
+          typedef const __attribute__((address_space(1))) uint2 *G;
+          union {
+            i32x4 v;
+            uint2 u[2];
+          } w;
+          const G g = (G)(d < a.D ? src + d : (const int8_t *)kZeroRow);
+          const G g8 = (G)(d + 8 < a.D ? src + d + 8 : (const int8_t *)kZeroRow);
+          w.u[0].x = g->x, w.u[0].y = g->y;
+          w.u[1].x = g8->x, w.u[1].y = g8->y;
+          kv[u][i] = w.v;
+        }
+        scale[u] = page[u] < 0 ? 0.0f : a.kscale[row];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int b0 = g0 + u * kSelectWaves * 16;
+        if (b0 >= n) break;
+        i32x4 acc{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(kv[u][i], qv[i], acc, 0, 0, 0);
+        const unsigned there = (unsigned)__builtin_amdgcn_ballot_w64(page[u] >= 0);
         const int p = pos0 + col;
         const int near = p < 0 ? -1 : p >> a.shift;
-        unsigned key = rank_of(__fmul_rn((float)acc[i], sc));
-        if (bb < a.first || bb > near - a.local) key = ~0u;
-        if (pg < 0 || bb > near) key = 0;
-        k4[i] = key;
-      }
-      if (col < TM) {
-        unsigned *dst = keys + col * stride + a.top + b0 + grp * 4;
+        unsigned *dst = keys + (col < TM ? col : 0) * stride + a.top + b0 + grp * 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (b0 + grp * 4 + i < n) dst[i] = k4[i];
+        for (int i = 0; i < 4; ++i) {
+          const int from = grp * 4 + i;  // page of row 4 grp + i
+          const float sc = __shfl(scale[u], from);
+          const int bb = seg + b0 + from;
+          unsigned key = rank_of(__fmul_rn((float)acc[i], sc));
+          if (bb < a.first || bb > near - a.local) key = ~0u;
+          if (!((there >> from) & 1) || bb > near) key = 0;
+          if (col < TM && b0 + from < n) dst[i] = key;
+        }
       }
     }
     __syncthreads();
@@ -182,6 +271,71 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
     for (int i = 0; i < NR; ++i) {
       const int e = base + i * kWave + lane;
       v[i] = e < entries ? row[first_entry + e] : 0;
+    }
+    const bool last = seg + room_of_segment >= blocks;
+    int32_t *dst = a.sel + ((int64_t)(t0 + my_token) * a.Hkv + h) * a.top;
+    const bool mine = my_token < tokens;
+    bool done = false;
+    if (a.top <= kSelectFew) {
+      int kept;
+      unsigned key;
+      int number;
+      done = choose_few(v, a.top, room, lane, kept, key, number);
+      if constexpr (WPR > 1) {
+        // every wave's choice behind the one of the wave before, then once more among them
+        if (lane == 0) count[wave] = done ? kept : kWave + 1;
+        __syncthreads();
+        int before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < kSelectWaves; ++w) {
+          const int c = count[w];
+          done = done && c <= kWave;
+          if (w < wave) before += c;
+          all += c;
+        }
+        if (done) {  // in all waves or in none
+          number = base + number;
+          const int name = number < held ? names[number] : seg + (number - held);
+          unsigned *list = room - wave * 2 * kWave + kSelectWaves * 2 * kWave;
+          if (lane < kept) list[before + lane] = key, list[kSelectWaves * kWave + before + lane] = (unsigned)name;
+          __syncthreads();
+          if (wave == 0) {
+            unsigned c[kSelectWaves];
+#pragma unroll
+            for (int i = 0; i < kSelectWaves; ++i) c[i] = i * kWave + lane < all ? list[i * kWave + lane] : 0;
+            done = choose_few(c, a.top, room, lane, kept, key, number);
+            if (done && lane < kept) {
+              const int chosen = (int)list[kSelectWaves * kWave + number];
+              if (last) {
+                dst[lane] = chosen;
+              } else {
+                names[lane] = chosen;
+                row[a.top - kept + lane] = key;
+              }
+            }
+            if (done && last && lane >= kept && lane < a.top) dst[lane] = -1;
+            if (lane == 0) count[kSelectWaves] = done ? kept : -1;
+          }
+          __syncthreads();
+          held = count[kSelectWaves] < 0 ? held : count[kSelectWaves];
+          done = count[kSelectWaves] >= 0;
+        }
+        __syncthreads();
+      } else if (done) {
+        int name = 0;
+        if (lane < kept) name = number < held ? names[number] : seg + (number - held);
+        if (last) {
+          if (mine && lane < a.top) dst[lane] = lane < kept ? name : -1;
+        } else if (lane < kept) {
+          names[lane] = name;
+          row[a.top - kept + lane] = key;
+        }
+        held = kept;
+      }
+    }
+    if (done) {
+      __syncthreads();
+      continue;
     }
     // Keys of the row that are at least `than`.
     int turn = 0;
@@ -235,10 +389,7 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
       name[i] = e < held ? names[e] : seg + (e - held);
     }
     if constexpr (WPR > 1) __syncthreads();
-    const bool last = seg + room >= blocks;
     int taken = out;
-    int32_t *dst = a.sel + ((int64_t)(t0 + my_token) * a.Hkv + h) * a.top;
-    const bool mine = my_token < tokens;
     const int kept = reach > a.top ? a.top : reach;  // entries that the row keeps
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
