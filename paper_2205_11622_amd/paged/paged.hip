@@ -144,10 +144,11 @@ template <class T, int DP, int TM, int NR>
 int run_select(const Launch &l, SelectArgs a, int64_t Hkv) {
   constexpr int most = NR * kWave * (kSelectWaves / TM);
   // pages of the longest request, and the carried entries in front, if they fit
-  const int64_t want = ((int64_t)a.W + 15) / 16 * 16 + a.top;
+  const int64_t pages = ((int64_t)a.W + 15) / 16 * 16;
+  const int64_t want = (pages < 2 * kWave ? 2 * kWave : pages) + a.top;
   a.capacity = (int32_t)(want < most ? want : most);
   const size_t lds = (size_t)TM * (a.capacity + 4) * 4 + ((size_t)TM * a.top + 3) / 4 * 16 + 16 * (DP + 16) +
-                     2 * kSelectWaves * 4 + kSelectWaves * 2 * kWave * 4 * (TM == 1 ? 2 : 1);
+                     2 * kSelectWaves * 4 + (TM == 1 ? kSelectWaves * 4 * kWave * 4 : 0);
   const int64_t tiles = TM == 1 ? (int64_t)a.T : (int64_t)a.T / TM + a.R;
   hipLaunchKernelGGL((block_select<T, DP, TM, NR>), dim3((unsigned)tiles, (unsigned)Hkv), dim3(kSelectBlock), lds,
                      l.stream, a);

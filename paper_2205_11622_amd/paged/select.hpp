@@ -24,12 +24,12 @@ constexpr int kSelectBlock = kSelectWaves * kWave;
 constexpr int kSelectMaxTop = 256;
 
 // Keys that order as the scores do, as unsigned numbers: 0 is no page, ~0 one that
-// is always taken.  NaN ranks above every number.
+// is always taken.  NaN ranks above every number (the minimum of NaN and a number is the
+// number), and -0 and 0 are one score.
 __device__ __forceinline__ unsigned rank_of(float s) {
-  if (s != s) s = 3.402823466e38f;
-  s = fminf(fmaxf(s, -3.402823466e38f), 3.402823466e38f) + 0.0f;  // -0 and 0 are one score
-  const unsigned b = __float_as_uint(s);
-  return b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+  const float big = 3.402823466e38f;
+  const unsigned b = __float_as_uint(fmaxf(fminf(s, big), -big) + 0.0f);
+  return b ^ (unsigned)((int)b >> 31 | (int)0x80000000);
 }
 
 // The largest `cut` that at least `top` of the wave's values reach (there are more than
@@ -117,7 +117,7 @@ __device__ __forceinline__ bool choose_few(const unsigned (&v)[NR], int top, uns
 //
 // NR: keys of a row that a lane holds in the choice.
 template <class T, int DP, int TM, int NR>
-__global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
+__global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 : 4) void block_select(SelectArgs a) {
   constexpr int KS = DP / 64;
   constexpr int WPR = kSelectWaves / TM;  // waves of a row in the choice
   static_assert(TM == 1 || TM == kSelectWaves, "one wave per token, or all for one");
@@ -128,7 +128,6 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
   int8_t *q8 = reinterpret_cast<int8_t *>(carried + TM * a.top + ((-TM * a.top) & 3));  // [16][DP + 16]
   constexpr int QS = DP + 16;
   int *count = reinterpret_cast<int *>(q8 + 16 * QS);               // [2][16] of the waves
-  unsigned *room = reinterpret_cast<unsigned *>(count + 2 * kSelectWaves) + (threadIdx.x >> 6) * 2 * kWave;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 15, grp = lane >> 4;
   const int h = blockIdx.y;
@@ -195,6 +194,7 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
 #pragma unroll
   for (int i = 0; i < KS; ++i) qv[i] = *reinterpret_cast<const i32x4 *>(q8 + col * QS + i * 64 + grp * 16);
 
+  const int near0 = pos0 < 0 ? -1 : pos0 >> a.shift;  // page of the first token
   auto table_entry = [&](int b) { return b < blocks ? table[b] : -1; };
   const int my_token = TM == 1 ? 0 : wave;                   // row of the choice
   const int room_of_segment = a.capacity - a.top;
@@ -202,16 +202,14 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
   for (int seg = 0; seg == 0 || seg < blocks; seg += room_of_segment) {
     const int n = blocks - seg < room_of_segment ? (blocks - seg > 0 ? blocks - seg : 0) : room_of_segment;
     // ---------------------------------------------------- scores of a segment
-    // Four groups of 16 pages at once: their entries, then their summaries are on
-    // their way together.
-    constexpr int U = 4;
+    // Rows of the product are the tokens, columns 16 pages, so a lane has one page for
+    // four tokens.  U groups at once: their entries, then their summaries are on their
+    // way together.
+    constexpr int U = TM == 1 ? 4 : 2;
     for (int g0 = wave * 16; g0 < n; g0 += U * kSelectWaves * 16) {
       int page[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int b = seg + g0 + u * kSelectWaves * 16 + col;
-        page[u] = table_entry(b);
-      }
+      for (int u = 0; u < U; ++u) page[u] = table_entry(seg + g0 + u * kSelectWaves * 16 + col);
       i32x4 kv[U][KS];
       float scale[U];
 #pragma unroll
@@ -241,20 +239,26 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
         if (b0 >= n) break;
         i32x4 acc{0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < KS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(kv[u][i], qv[i], acc, 0, 0, 0);
-        const unsigned there = (unsigned)__builtin_amdgcn_ballot_w64(page[u] >= 0);
-        const int p = pos0 + col;
-        const int near = p < 0 ? -1 : p >> a.shift;
-        unsigned *dst = keys + (col < TM ? col : 0) * stride + a.top + b0 + grp * 4;
+        for (int i = 0; i < KS; ++i) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qv[i], kv[u][i], acc, 0, 0, 0);
+        unsigned key[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int from = grp * 4 + i;  // page of row 4 grp + i
-          const float sc = __shfl(scale[u], from);
-          const int bb = seg + b0 + from;
-          unsigned key = rank_of(__fmul_rn((float)acc[i], sc));
-          if (bb < a.first || bb > near - a.local) key = ~0u;
-          if (!((there >> from) & 1) || bb > near) key = 0;
-          if (col < TM && b0 + from < n) dst[i] = key;
+        for (int i = 0; i < 4; ++i) key[i] = rank_of(__fmul_rn((float)acc[i], scale[u]));
+        const int bb = seg + b0 + col;
+        // all pages there, seen by all tokens and chosen by score alone, as most are
+        if (seg + b0 < a.first || seg + b0 + 15 > near0 - a.local || b0 + 15 >= n ||
+            __builtin_amdgcn_ballot_w64(page[u] < 0)) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int p = pos0 + grp * 4 + i;
+            const int near = p < 0 ? -1 : p >> a.shift;
+            if (bb < a.first || bb > near - a.local) key[i] = ~0u;
+            if (page[u] < 0 || bb > near) key[i] = 0;
+          }
+        }
+        if (b0 + col < n && (TM > 1 || grp == 0)) {
+          unsigned *dst = keys + grp * 4 * stride + a.top + b0 + col;
+#pragma unroll
+          for (int i = 0; i < (TM == 1 ? 1 : 4); ++i) dst[i * stride] = key[i];
         }
       }
     }
@@ -276,6 +280,9 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
     int32_t *dst = a.sel + ((int64_t)(t0 + my_token) * a.Hkv + h) * a.top;
     const bool mine = my_token < tokens;
     bool done = false;
+    // Two numbers a lane of LDS for a wave: the row that is now in registers, or (one
+    // token) the words behind the counts.
+    unsigned *room = TM == 1 ? reinterpret_cast<unsigned *>(count + 2 * kSelectWaves) + wave * 2 * kWave : row + a.top;
     if (a.top <= kSelectFew) {
       int kept;
       unsigned key;
@@ -381,14 +388,18 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
       for (int w = 0; w < wave; ++w) out += count[w], tied += count[kSelectWaves + w];
       out += tied < ties ? tied : ties;
     }
-    // names of the entries, before the carried ones are written over
-    int name[NR];
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
+    // Names of the entries: read before the carried ones are written over, by other
+    // waves (one token) or by this one, which writes behind where it reads.
+    auto name_of = [&](int i) {
       const int e = base + i * kWave + lane;
-      name[i] = e < held ? names[e] : seg + (e - held);
+      return e < held ? names[e] : seg + (e - held);
+    };
+    int name[WPR > 1 ? NR : 1];
+    if constexpr (WPR > 1) {
+#pragma unroll
+      for (int i = 0; i < NR; ++i) name[i] = name_of(i);
+      __syncthreads();
     }
-    if constexpr (WPR > 1) __syncthreads();
     int taken = out;
     const int kept = reach > a.top ? a.top : reach;  // entries that the row keeps
 #pragma unroll
@@ -398,12 +409,18 @@ __global__ __launch_bounds__(kSelectBlock) void block_select(SelectArgs a) {
       const unsigned long long below = (1ull << lane) - 1;
       const bool take = (cut_ties ? v[i] > cut : v[i] >= cut) || (eq && tied + __popcll(be & below) < ties);
       const unsigned long long b = __builtin_amdgcn_ballot_w64(take);
+      int its = 0;
+      if constexpr (WPR > 1)
+        its = name[i];
+      else
+        its = name_of(i);
+      __builtin_amdgcn_wave_barrier();
       if (take) {
         const int at = taken + __popcll(b & below);
         if (last) {
-          if (mine) dst[at] = name[i];
+          if (mine) dst[at] = its;
         } else {
-          names[at] = name[i];
+          names[at] = its;
           row[a.top - kept + at] = v[i];
         }
       }
