@@ -138,6 +138,18 @@ int attend(const void *q, int64_t q_token, int64_t q_head, int64_t Hq, const spa
   }
 }
 
+// Few tokens: the heads are shared out until there are about four blocks a compute unit.
+// Many: as many tokens a block as leave eight blocks to a unit, at most 8.
+template <class T>
+int run_append(const Launch &l, const AppendArgs &a) {
+  int64_t shares = 4 * (int64_t)l.cus / a.T, per = a.T / ((int64_t)l.cus * 8);
+  shares = shares < 1 ? 1 : shares > a.Hkv ? a.Hkv : shares;
+  per = per < 1 ? 1 : per > 8 ? 8 : per;
+  hipLaunchKernelGGL(cache_append<T>, dim3((unsigned)((a.T + per - 1) / per), (unsigned)shares), dim3(kAppendBlock), 0,
+                     l.stream, a, (int)per);
+  return launched();
+}
+
 // ------------------------------------------------------------ selection
 
 template <class T, int DP, int TM, int NR>
@@ -231,14 +243,13 @@ int sparselnr_cache_append(const void *k, int64_t k_token, int64_t k_head, const
   a.kq = kq, a.kscale = kscale;
   a.T = (int32_t)T, a.pages = (int32_t)cache->pages, a.shift = page_shift(cache->page_size);
   a.Hkv = (int32_t)cache->heads, a.D = (int32_t)cache->dim;
-  const dim3 grid((unsigned)T), block(kAppendBlock);
-  hipStream_t s = (hipStream_t)stream;
+  Launch l;
+  if ((rc = current(&l, stream)) != SPARSELNR_OK) return rc;
   switch (cache->dtype) {
-    case SPARSELNR_BF16: hipLaunchKernelGGL(cache_append<__bf16>, grid, block, 0, s, a); break;
-    case SPARSELNR_FP16: hipLaunchKernelGGL(cache_append<_Float16>, grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL(cache_append<float>, grid, block, 0, s, a); break;
+    case SPARSELNR_BF16: return run_append<__bf16>(l, a);
+    case SPARSELNR_FP16: return run_append<_Float16>(l, a);
+    default: return run_append<float>(l, a);
   }
-  return launched();
 }
 
 int sparselnr_paged_attention(const void *q, int64_t q_token, int64_t q_head, int64_t Hq,

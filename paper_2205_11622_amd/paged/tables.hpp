@@ -154,92 +154,117 @@ struct AppendArgs {
   int32_t T, pages, shift, Hkv, D;
 };
 
+// A block copies the rows of `per` adjacent new tokens, of a share of the heads.  It also
+// renews the summary of every page whose last new token is among them: the mean of the
+// page's K rows (sum in 64 bits, rounded once, so that it does not depend on the
+// order), in 8 bits with one step per head.  Rows written in this call are taken from
+// the call's input, since their blocks may not have run yet, older ones from the
+// cache.
+//
+// Latency for a decode step (the slot, a look for the page's other new rows, then all its
+// rows at once), so the heads go to different blocks there; memory for a chunk, where
+// more tokens a block keep the number of blocks, which start at about 3 ns each, down.
 constexpr int kAppendBlock = 256;
 
-// One block per new token copies its rows.  The block of a page's last new token
-// also renews the page's summary: the mean of its K rows (sum in 64 bits, rounded
-// once, so that it does not depend on the order), in 8 bits with one step per head.
-// Rows written in this call are taken from the call's input, since their blocks
-// may not have run yet, older ones from the cache.
 template <class T>
-__global__ __launch_bounds__(kAppendBlock) void cache_append(AppendArgs a) {
+__global__ __launch_bounds__(kAppendBlock) void cache_append(AppendArgs a, int per) {
   typedef typename Type<T>::Vec Vec;
   constexpr int NT = kAppendBlock;
-  __shared__ double sums[NT][8];
-  __shared__ float most[NT];
+  __shared__ double sums[8][NT];
+  __shared__ unsigned most[NT];
+  __shared__ int fresh_rows;
   const int tid = threadIdx.x;
-  const int t = blockIdx.x;
+  const int t0 = blockIdx.x * per, t1 = t0 + per < a.T ? t0 + per : a.T;
+  const int share = (a.Hkv + gridDim.y - 1) / gridDim.y;
+  const int first = blockIdx.y * share, last = first + share < a.Hkv ? first + share : a.Hkv;
+  if (first >= last) return;
   const int P = 1 << a.shift;
-  const int64_t slot = a.slots[t];
-  const int64_t page = slot >> a.shift;
-  if (slot < 0 || page >= a.pages) return;
-  const int row = (int)(slot & (P - 1));
-  const int nc = a.D / 8, chunks = a.Hkv * nc;
-  for (int i = tid; i < 2 * chunks; i += NT) {
-    const bool is_v = i >= chunks;
-    const int c = is_v ? i - chunks : i;
-    const int h = c / nc, d = (c - h * nc) * 8;
+  const int nc = a.D / 8, chunks = (last - first) * nc;
+  for (int i = tid; i < (t1 - t0) * 2 * chunks; i += NT) {
+    const int t = t0 + i / (2 * chunks), e = i % (2 * chunks);
+    const int64_t slot = a.slots[t], page = slot >> a.shift;
+    if (slot < 0 || page >= a.pages) continue;
+    const int row = (int)(slot & (P - 1));
+    const bool is_v = e >= chunks;
+    const int c = is_v ? e - chunks : e;
+    const int h = first + c / nc, d = (c % nc) * 8;
     const T *src = is_v ? (const T *)a.v + t * a.v_token + h * a.v_head_in + d
                         : (const T *)a.k + t * a.k_token + h * a.k_head_in + d;
     T *dst = is_v ? (T *)a.vc + page * a.v_page + row * a.v_slot + h * a.v_head + d
                   : (T *)a.kc + page * a.k_page + row * a.k_slot + h * a.k_head + d;
-    store8<T>(dst, load8<T>(src));
+    store8<T>(dst, load8_global<T>(src));
   }
   if (!a.kq) return;
-  if (row != P - 1 && t + 1 < a.T && a.slots[t + 1] == slot + 1) return;  // not the page's last new row
 
-  const int heads = NT / nc;                 // of one pass; D <= 256: at least 8
-  for (int h0 = 0; h0 < a.Hkv; h0 += heads) {
-    const int hn = a.Hkv - h0 < heads ? a.Hkv - h0 : heads;
-    const int n = hn * nc, sides = NT / n;   // threads of a row, rows side by side
-    const int c = tid % n, side = tid / n;
-    const int h = h0 + c / nc, d = (c % nc) * 8;
-    double s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (side < sides) {
-#pragma unroll 4
-      for (int i = side; i <= row; i += sides) {
-        const int back = row - i;
-        const bool fresh = t >= back && a.slots[t - back] == slot - back;
-        const T *src = fresh ? (const T *)a.k + (t - back) * a.k_token + h * a.k_head_in + d
-                             : (const T *)a.kc + page * a.k_page + i * a.k_slot + h * a.k_head + d;
-        const Vec x = load8<T>(src);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] += (double)(float)x[j];
+  for (int t = t0; t < t1; ++t) {
+    const int64_t slot = a.slots[t], page = slot >> a.shift;
+    if (slot < 0 || page >= a.pages) continue;
+    const int row = (int)(slot & (P - 1));
+    if (row != P - 1 && t + 1 < a.T && a.slots[t + 1] == slot + 1) continue;  // not the page's last new row
+    // the page's rows up to this one that are new: the tokens before with the slots before
+    if (tid == 0) fresh_rows = row + 1;
+    __syncthreads();
+    for (int back = 1 + tid; back <= row; back += NT)
+      if (back > t || a.slots[t - back] != slot - back) {
+        atomicMin(&fresh_rows, back);
+        break;
       }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) sums[tid][j] = s[j];
     __syncthreads();
-    float mean[8], top = 0.0f;
-    if (side == 0) {
+    const int fresh = fresh_rows;
+    const int heads = NT / nc;  // of one pass; D <= 256: at least 8
+    for (int h0 = first; h0 < last; h0 += heads) {
+      const int hn = last - h0 < heads ? last - h0 : heads;
+      const int n = hn * nc, sides = NT / n;  // threads of a row, rows side by side
+      const int c = tid % n, side = tid / n;
+      const int h = h0 + c / nc, d = (c % nc) * 8;
+      double s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      if (side < sides) {
+        const T *old = (const T *)a.kc + page * a.k_page + h * a.k_head + d;
+        const T *now = (const T *)a.k + (int64_t)(t - row) * a.k_token + h * a.k_head_in + d;  // row 0, were it new
+#pragma unroll 8
+        for (int i = side; i <= row; i += sides) {
+          const Vec x = load8_global<T>(row - i < fresh ? now + i * a.k_token : old + i * a.k_slot);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        double x = s[j];
-        for (int k = 1; k < sides; ++k) x += sums[k * n + c][j];
-        mean[j] = (float)(x / (double)(row + 1));
-        const float y = fabsf(mean[j]);
-        top = y <= 3.402823466e38f ? fmaxf(top, y) : __builtin_inff();
+          for (int j = 0; j < 8; ++j) s[j] += (double)(float)x[j];
+        }
       }
-      most[c] = top;
-    }
-    __syncthreads();
-    if (side == 0) {
-      const int at = c - c % nc;
-      for (int k = 0; k < nc; ++k) top = fmaxf(top, most[at + k]);
-      // a page with infinities or NaN gets the step inf: its score is NaN, which ranks first
-      const bool fine = top < __builtin_inff();
-      const float step = fine ? top * kStep127 : __builtin_inff();
-      union {
-        int8_t b[8];
-        uint2 u;
-      } w;
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        w.b[j] = fine && step > 0.0f ? whole8(mean[j], step) : (int8_t)0;
-      *reinterpret_cast<uint2 *>(a.kq + (page * a.Hkv + h) * a.D + d) = w.u;
-      if (d == 0) a.kscale[page * a.Hkv + h] = step;
+      for (int j = 0; j < 8; ++j) sums[j][tid] = s[j];
+      if (tid < hn) most[tid] = 0;
+      __syncthreads();
+      // a value a thread from here on: thread e, e + NT, ... have value e of the pass
+      constexpr int E = 8;  // n * 8 values, n <= NT
+      float mean[E];
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        const int e = tid + k * NT;
+        if (e < n * 8) {
+          const int at = e >> 3, j = e & 7;
+          double x = 0;
+          for (int i = 0; i < sides; ++i) x += sums[j][i * n + at];
+          mean[k] = (float)(x / (double)(row + 1));
+          const float y = fabsf(mean[k]);
+          atomicMax(&most[at / nc], y <= 3.402823466e38f ? __float_as_uint(y) : 0x7f800000u);
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < E; ++k) {
+        const int e = tid + k * NT;
+        if (e < n * 8) {
+          const int hh = (e >> 3) / nc;
+          const float top = __uint_as_float(most[hh]);
+          // a page with infinities or NaN gets the step inf: its score is NaN, which ranks first
+          const bool fine = top < __builtin_inff();
+          const float step = fine ? top * kStep127 : __builtin_inff();
+          const int64_t out = page * a.Hkv + h0 + hh;
+          const int d = e - hh * a.D;
+          a.kq[out * a.D + d] = fine && step > 0.0f ? whole8(mean[k], step) : (int8_t)0;
+          if (d == 0) a.kscale[out] = step;
+        }
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
