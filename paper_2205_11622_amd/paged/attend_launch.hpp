@@ -3,6 +3,7 @@
 #pragma once
 
 #include "attend.hpp"
+#include "pages.hpp"
 #include "runtime.hpp"
 #include "sparselnr.h"
 
@@ -76,9 +77,77 @@ int run_many(const Launch &l, AttendArgs a) {
   return launch(join_many<T, DP, ROWS>, dim3((unsigned)slots, ROWS / kJoinRows), kJoinBlock, 0, l, a);
 }
 
+constexpr int64_t kPagesWorkspace = (int64_t)640 << 20;  // of partial results, at most
+
+// By pages (pages.hpp) rather than by queries: where a page is selected by four queries and
+// more on average, its keys are at least four times the heads of a group (the results
+// of a page are then at most half of what is gathered by queries), and 256 MB and more are
+// gathered, which take longer than the four small launches before and the join.
+inline bool by_pages(const AttendArgs &a, int64_t bytes) {
+  const int64_t picks = (int64_t)a.T * a.top;
+  return a.W > 0 && picks >= 4 * (int64_t)a.R * a.W && ((int64_t)1 << a.shift) >= 4 * (int64_t)a.G &&
+         ((picks * a.Hkv) << a.shift) * a.D * 2 * bytes >= (int64_t)256 << 20 &&
+         (int64_t)a.R * a.W * a.Hkv < ((int64_t)1 << 30) && a.G <= kPagesRows;
+}
+
+template <class T, int DP>
+int run_pages(const Launch &l, const AttendArgs &a) {
+  PagesArgs p{};
+  const int64_t per_token = (int64_t)a.Hkv * a.top;  // selected pages
+  int64_t most = kPagesWorkspace / (per_token * a.G * (DP + 2) * (int64_t)sizeof(float));
+  most = most < 1 ? 1 : most > a.T ? a.T : most;
+  if (most * per_token >= ((int64_t)1 << 30)) most = (((int64_t)1 << 30) - 1) / per_token;
+  p.buckets = a.Hkv * a.R * a.W;
+  p.per_tile = kPagesRows / a.G;
+  const int64_t picks = most * per_token, tiles = picks / p.per_tile + p.buckets;
+  size_t size = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = size;
+    size += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  const size_t count = take((size_t)p.buckets * 4), begin = take((size_t)p.buckets * 4),
+               tile_begin = take((size_t)p.buckets * 4), total = take(4), rank = take((size_t)picks * 4),
+               list = take((size_t)picks * 4), tile = take((size_t)tiles * 4),
+               part = take((size_t)picks * a.G * DP * 4), ml = take((size_t)picks * a.G * 8);
+  void *ws = nullptr;
+  int rc = stream_workspace(l.dev, l.stream, size, &ws, kSlotAttend);
+  if (rc != SPARSELNR_OK) return rc;
+  auto at = [&](size_t offset) { return (int32_t *)((char *)ws + offset); };
+  p.count = at(count), p.begin = at(begin), p.tile_begin = at(tile_begin), p.total = at(total), p.rank = at(rank);
+  p.list = at(list), p.tile = at(tile), p.part = (float *)at(part), p.ml = (float *)at(ml);
+  auto done = [&]() {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SPARSELNR_OK : hip_error(e);
+  };
+  for (int64_t t0 = 0; t0 < a.T; t0 += most) {
+    p.t0 = (int32_t)t0;
+    p.tokens = (int32_t)(a.T - t0 < most ? a.T - t0 : most);
+    const int64_t n = p.tokens * per_token;
+    const dim3 block(kPagesBlock), each((unsigned)((n + kPagesBlock - 1) / kPagesBlock));
+    hipLaunchKernelGGL(pages_clear, dim3((unsigned)((p.buckets + kPagesBlock - 1) / kPagesBlock)), block, 0, l.stream, p);
+    hipLaunchKernelGGL(pages_count, each, block, 0, l.stream, a, p);
+    hipLaunchKernelGGL(pages_scan, dim3(1), dim3(kScanBlock), 0, l.stream, p);
+    hipLaunchKernelGGL(pages_fill, each, block, 0, l.stream, a, p);
+    if ((rc = done()) != SPARSELNR_OK) return rc;
+    // a page makes at most one tile more than its queries fill, and none without queries
+    const int64_t extra = n < p.buckets ? n : p.buckets;
+    hipLaunchKernelGGL((attend_pages<T, DP>), dim3((unsigned)(n / p.per_tile + extra)), block,
+                       sizeof(PagesShared<T, DP>), l.stream, a, p);
+    if ((rc = done()) != SPARSELNR_OK) return rc;
+    const int64_t rows = (int64_t)p.tokens * a.Hq;
+    hipLaunchKernelGGL((join_pages<T, DP>), dim3((unsigned)((rows + 3) / 4)), block, 0, l.stream, a, p);
+    if ((rc = done()) != SPARSELNR_OK) return rc;
+  }
+  return SPARSELNR_OK;
+}
+
 template <class T, int DP>
 int run_attend(const Launch &l, AttendArgs a, int64_t max_new) {
-  if (a.sel) return run_few<T, DP, true>(l, a, a.G < kFewRows ? a.G : kFewRows);
+  if (a.sel) {
+    if (by_pages(a, sizeof(T))) return run_pages<T, DP>(l, a);
+    return run_few<T, DP, true>(l, a, a.G < kFewRows ? a.G : kFewRows);
+  }
   // rows of the longest request, as far as the host knows
   const int64_t rows = (max_new > 0 && max_new < a.T ? max_new : a.T) * a.G;
   a.few = 0x7fffffff;

@@ -604,3 +604,59 @@ def test_a_captured_step_replays(gpu):
         assert int(want[3][2]) == 0
         used += int(want[3][1])
     assert used == R * (-(-50 // P))
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,P,T", [(BF16, 128, 8, 8, 64, 900), (FP16, 64, 8, 2, 32, 1500), (FP32, 128, 4, 4, 64, 500),
+                                               (BF16, 72, 6, 2, 128, 700), (BF16, 256, 2, 2, 64, 500), (BF16, 64, 4, 4, 256, 300)])
+def test_block_attention_of_many_tokens_goes_by_pages(gpu, dtype, D, Hq, Hkv, P, T):
+    """Enough tokens that the call walks the pages instead of the queries, against a
+    walk by queries (one call per token) and, for some tokens, the definition."""
+    b = pu.Batch([11 * P + 5, 3], [T, 40], Hq, Hkv, D, P, dtype, seed=40 + D)
+    top = 12
+    sel = random_selection(b, Hkv, top, 41)
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    table = table.clone()
+    table[0, 3] = -1  # a page given back
+    s = b.ints(sel, gpu)
+    s[0] = -1         # a token without pages
+    s[1, :, -1] = 10 ** 6
+    lse = torch.full(q.shape[:2], math.nan, device=gpu)
+    out = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, s, lse=lse)
+    again = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, s)
+    assert torch.equal(out, again)
+    assert (out[0] == 0).all() and (lse[0] == -math.inf).all()
+    b.table[0][3] = -1
+    n = torch.tensor([1], dtype=torch.int32, device=gpu)
+    ptr = torch.tensor([0, 1], dtype=torch.int32, device=gpu)
+    few = [0, 1, 2, 77, T - 1, T, T + 39]
+    for t in few:
+        r = 0 if t < T else 1
+        pos = b.ctx[r] + t - b.qptr[r]
+        one = slnr.sparselnr_block_attention(q[t:t + 1], kc, vc, table[r:r + 1], n * (pos + 1), ptr, s[t:t + 1])
+        sub = pu.Batch.__new__(pu.Batch)
+        ref, want_lse, weight = pu.attention(b.q[t:t + 1], b.kc, b.vc, [b.table[r]], [pos + 1], [0, 1], D ** -0.5,
+                                             sel=[s[t].tolist()])
+        tol = pu.tolerance(dtype, weight, pos + 1, D, vmax(b))
+        assert ((out[t:t + 1].double().cpu() - ref).abs() <= tol).all(), t
+        assert ((out[t:t + 1].double().cpu() - one.double().cpu()).abs() <= 2 * tol).all(), t
+        fine = want_lse[0] > -math.inf
+        assert ((lse[t].double().cpu() - want_lse[0]).abs()[fine] <= 1e-5 + 1e-6 * want_lse[0].abs()[fine]).all()
+
+
+def test_by_pages_infinities_and_nan_ahead_of_a_query(gpu):
+    """The last page holds the chunk itself: what a later token's V row holds does not reach earlier ones."""
+    b = pu.Batch([8 * 256 - 300], [300], 4, 4, 64, 256, BF16, seed=50)
+    sel = [[list(range(8)) for _ in range(4)] for _ in range(300)]
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    s = b.ints(sel, gpu)
+    want = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, s).float().cpu()
+    S = b.seq[0]
+    bad = S - 100
+    vc[b.table[0][bad // 256], bad % 256, :, 5] = math.inf
+    vc[b.table[0][bad // 256], bad % 256, :, 6] = math.nan
+    got = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, s).float().cpu()
+    first = 300 - 100  # the token at that position
+    assert torch.equal(got[:first], want[:first])
+    assert (got[first:, :, 5] == math.inf).all() and torch.isnan(got[first:, :, 6]).all()
+    rest = [d for d in range(64) if d not in (5, 6)]
+    assert torch.equal(got[first:][:, :, rest], want[first:][:, :, rest])
