@@ -59,11 +59,29 @@ __device__ __forceinline__ int bucket_of(const AttendArgs &a, const PagesArgs &p
   return (h * a.R + x) * a.W + b;
 }
 
+// Neighbouring lanes are neighbouring tokens: pages that all tokens select (the first, the
+// last) are then counted once a wave.  One by one their counters took 28 us of a
+// call on 2020 tokens.
 static __global__ __launch_bounds__(kPagesBlock) void pages_count(AttendArgs a, PagesArgs p) {
-  const int i = blockIdx.x * kPagesBlock + threadIdx.x;
-  if (i >= p.tokens * a.Hkv * a.top) return;
-  const int bucket = bucket_of(a, p, i);
-  p.rank[i] = bucket < 0 ? -1 : atomicAdd(&p.count[bucket], 1);
+  const int e = blockIdx.x * kPagesBlock + threadIdx.x;
+  const bool in = e < p.tokens * a.Hkv * a.top;
+  const int i = in ? (e % p.tokens) * a.Hkv * a.top + e / p.tokens : 0;  // (h, j) slowest
+  const int bucket = in ? bucket_of(a, p, i) : -1;
+  int rank = -1;
+  const unsigned long long some = __builtin_amdgcn_ballot_w64(bucket >= 0);
+  if (some) {
+    const int lane = threadIdx.x & 63, lead = __builtin_ctzll(some);
+    const int common = __shfl(bucket, lead);
+    const unsigned long long same = __builtin_amdgcn_ballot_w64(bucket == common);
+    int base = 0;
+    if (lane == lead) base = atomicAdd(&p.count[common], __popcll(same));
+    base = __shfl(base, lead);
+    if (bucket == common)
+      rank = base + __popcll(same & ((1ull << lane) - 1));
+    else if (bucket >= 0)
+      rank = atomicAdd(&p.count[bucket], 1);
+  }
+  if (in) p.rank[i] = rank;
 }
 
 // Running sums over the buckets, by one block: a share of them per thread, then a scan.
