@@ -1072,9 +1072,9 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
 // ------------------------------------------------------------------ the join
 //
 // Adds the pieces of one row of a split tile: the largest of their maxima, their
-// sums and values rescaled to it, in the order of the pieces.  One block per
-// piece's slot and row (or every gridDim.y-th row); blocks whose slot is not a
-// tile's first piece leave at once.  The pieces of a tile are Hkv slots apart.
+// sums and values rescaled to it, in the order of the pieces.  A block goes through
+// every gridDim.x-th slot that is a tile's first piece and every gridDim.y-th row of
+// it.  The pieces of a tile are Hkv slots apart.
 
 constexpr int kJoinBlock = 256;
 
@@ -1088,112 +1088,114 @@ __global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
   __shared__ float red[2][kJoinBlock / kWave];
   const float sc = score_unit<T>(a);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t s = blockIdx.x;
-  if (s >= a.meta[0]) return;
-  const int32_t *mt = a.meta + (1 + s) * kMeta;
-  const int np = mt[0];
-  if (np <= 1) return;
-  constexpr int64_t kSize = (int64_t)ROWS * (DP + 2);
-  const float *part = a.part + s * kSize;
-  const int64_t next = (int64_t)a.Hkv * kSize;
-  for (int i = blockIdx.y; i < mt[2]; i += gridDim.y) {
-    const float *ml = part + ROWS * DP + i * 2;
-    float mx = kNegInf;
-    for (int j = tid; j < np; j += kJoinBlock) mx = fmaxf(mx, ml[j * next]);
+  const int used = a.meta[0];
+  for (int64_t s = blockIdx.x; s < used; s += gridDim.x) {
+    const int32_t *mt = a.meta + (1 + s) * kMeta;
+    const int np = mt[0];
+    if (np <= 1) continue;
+    constexpr int64_t kSize = (int64_t)ROWS * (DP + 2);
+    const float *part = a.part + s * kSize;
+    const int64_t next = (int64_t)a.Hkv * kSize;
+    for (int i = blockIdx.y; i < mt[2]; i += gridDim.y) {
+      const float *ml = part + ROWS * DP + i * 2;
+      float mx = kNegInf;
+      for (int j = tid; j < np; j += kJoinBlock) mx = fmaxf(mx, ml[j * next]);
 #pragma unroll
-    for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-    if (lane == 0) red[0][wave] = mx;
-    __syncthreads();
+      for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+      if (lane == 0) red[0][wave] = mx;
+      __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kJoinBlock / kWave; ++w) mx = fmaxf(mx, red[0][w]);
-    const int c = (tid % kLanes) * 4, g = tid / kLanes;
-    f32x4 o{0, 0, 0, 0};
-    float sum = 0.0f;
-    for (int j0 = 0; j0 < np; j0 += kJoinBlock) {
-      const int j = j0 + tid;
-      float w = 0.0f;
-      if (j < np) {
-        const float mj = ml[j * next];
-        w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
-        sum += w == 0.0f ? 0.0f : w * ml[j * next + 1];
-      }
-      __syncthreads();
-      weight[tid] = w;
-      __syncthreads();
-      const int n = imin(np - j0, kJoinBlock);
+      for (int w = 0; w < kJoinBlock / kWave; ++w) mx = fmaxf(mx, red[0][w]);
+      const int c = (tid % kLanes) * 4, g = tid / kLanes;
+      f32x4 o{0, 0, 0, 0};
+      float sum = 0.0f;
+      for (int j0 = 0; j0 < np; j0 += kJoinBlock) {
+        const int j = j0 + tid;
+        float w = 0.0f;
+        if (j < np) {
+          const float mj = ml[j * next];
+          w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
+          sum += w == 0.0f ? 0.0f : w * ml[j * next + 1];
+        }
+        __syncthreads();
+        weight[tid] = w;
+        __syncthreads();
+        const int n = imin(np - j0, kJoinBlock);
 #pragma unroll 8
-      for (int k = g; k < n; k += kSide) {
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (j0 + k) * next + i * DP + c);
-        const float f = weight[k];
-        if (f != 0.0f) o += x * f;
+        for (int k = g; k < n; k += kSide) {
+          const f32x4 x = *reinterpret_cast<const f32x4 *>(part + (j0 + k) * next + i * DP + c);
+          const float f = weight[k];
+          if (f != 0.0f) o += x * f;
+        }
       }
+#pragma unroll
+      for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+      if (lane == 0) red[1][wave] = sum;
+      *reinterpret_cast<f32x4 *>(&acc[g][c]) = o;
+      __syncthreads();
+      sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kJoinBlock / kWave; ++w) sum += red[1][w];
+      const int row = mt[1] + i, t = row / a.G, hd = mt[3] * a.G + row % a.G;
+      const int64_t at = (int64_t)t * a.Hq + hd;
+      if (tid < a.D) {
+        float v = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) v += acc[k][tid];
+        ((T *)a.out)[at * a.D + tid] = (T)(mx == kNegInf ? 0.0f : v / sum);
+      }
+      if (tid == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
+      __syncthreads();
     }
-#pragma unroll
-    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
-    if (lane == 0) red[1][wave] = sum;
-    *reinterpret_cast<f32x4 *>(&acc[g][c]) = o;
-    __syncthreads();
-    sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kJoinBlock / kWave; ++w) sum += red[1][w];
-    const int row = mt[1] + i, t = row / a.G, hd = mt[3] * a.G + row % a.G;
-    const int64_t at = (int64_t)t * a.Hq + hd;
-    if (tid < a.D) {
-      float v = 0.0f;
-#pragma unroll
-      for (int k = 0; k < kSide; ++k) v += acc[k][tid];
-      ((T *)a.out)[at * a.D + tid] = (T)(mx == kNegInf ? 0.0f : v / sum);
-    }
-    if (tid == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
-    __syncthreads();
   }
 }
 
 // The same for the tiles of attend_many: many rows of few pieces, a wave per row.
-constexpr int kJoinRows = 32;  // rows of a block, one after the other in its four waves
+constexpr int kJoinRows = 8;  // rows of a block, two of them one after the other in each wave
 
 template <class T, int DP, int ROWS>
 __global__ __launch_bounds__(kJoinBlock) void join_many(AttendArgs a) {
   constexpr int C = DP / 64;  // columns of a lane
   const float sc = score_unit<T>(a);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t s = blockIdx.x;
-  if (s >= a.meta[0]) return;
-  const int32_t *mt = a.meta + (1 + s) * kMeta;
-  const int np = mt[0], rows = mt[2];
-  if (np <= 1) return;
   constexpr int64_t kSize = (int64_t)ROWS * (DP + 2);
   const int64_t next = (int64_t)a.Hkv * kSize;
-  for (int i = blockIdx.y * kJoinRows + wave; i < rows && i < (int)(blockIdx.y + 1) * kJoinRows;
-       i += kJoinBlock / kWave) {
-    const float *part = a.part + s * kSize + i * DP + lane * C;
-    const float *ml = a.part + s * kSize + ROWS * DP + i * 2;
-    float mx = kNegInf;
-    for (int j = lane; j < np; j += kWave) mx = fmaxf(mx, ml[j * next]);
+  const int used = a.meta[0];
+  for (int64_t s = blockIdx.x; s < used; s += gridDim.x) {
+    const int32_t *mt = a.meta + (1 + s) * kMeta;
+    const int np = mt[0], rows = mt[2];
+    if (np <= 1) continue;
+    for (int i = blockIdx.y * kJoinRows + wave; i < rows && i < (int)(blockIdx.y + 1) * kJoinRows;
+         i += kJoinBlock / kWave) {
+      const float *part = a.part + s * kSize + i * DP + lane * C;
+      const float *ml = a.part + s * kSize + ROWS * DP + i * 2;
+      float mx = kNegInf;
+      for (int j = lane; j < np; j += kWave) mx = fmaxf(mx, ml[j * next]);
 #pragma unroll
-    for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-    float sum = 0.0f, o[C];
+      for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+      float sum = 0.0f, o[C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = 0.0f;
+      for (int c = 0; c < C; ++c) o[c] = 0.0f;
 #pragma unroll 4
-    for (int j = 0; j < np; ++j) {
-      const float mj = ml[j * next], lj = ml[j * next + 1];
-      const float w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
-      float x[C];
+      for (int j = 0; j < np; ++j) {
+        const float mj = ml[j * next], lj = ml[j * next + 1];
+        const float w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
+        float x[C];
 #pragma unroll
-      for (int c = 0; c < C; ++c) x[c] = part[j * next + c];
-      if (w != 0.0f) {
-        sum += w * lj;
+        for (int c = 0; c < C; ++c) x[c] = part[j * next + c];
+        if (w != 0.0f) {
+          sum += w * lj;
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] += w * x[c];
+          for (int c = 0; c < C; ++c) o[c] += w * x[c];
+        }
       }
-    }
-    const int row = mt[1] + i, t = row / a.G, hd = mt[3] * a.G + row % a.G;
-    const int64_t at = (int64_t)t * a.Hq + hd;
+      const int row = mt[1] + i, t = row / a.G, hd = mt[3] * a.G + row % a.G;
+      const int64_t at = (int64_t)t * a.Hq + hd;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      if (lane * C + c < a.D) ((T *)a.out)[at * a.D + lane * C + c] = (T)(mx == kNegInf ? 0.0f : o[c] / sum);
-    if (lane == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
+      for (int c = 0; c < C; ++c)
+        if (lane * C + c < a.D) ((T *)a.out)[at * a.D + lane * C + c] = (T)(mx == kNegInf ? 0.0f : o[c] / sum);
+      if (lane == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
+    }
   }
 }
 

@@ -55,8 +55,7 @@ int run_few(const Launch &l, AttendArgs a, int most_rows) {
   const unsigned grid = (unsigned)(pieces < most ? pieces : most);
   rc = launch(attend_few<T, DP, SPARSE>, dim3(grid), kFewBlock, sizeof(FewShared<T, DP>), l, a);
   if (rc != SPARSELNR_OK) return rc;
-  return launch(join_few<T, DP>, dim3((unsigned)slots, most_rows < kFewRows ? most_rows : kFewRows), kJoinBlock, 0, l,
-                a);
+  return launch(join_few<T, DP>, dim3((unsigned)slots, most_rows < kFewRows ? most_rows : kFewRows), kJoinBlock, 0, l, a);
 }
 
 template <class T, int DP, int NW, bool ONE_PAGE>
@@ -74,7 +73,7 @@ int run_many(const Launch &l, AttendArgs a) {
   if (rc != SPARSELNR_OK) return rc;
   rc = launch(attend_many<T, DP, NW, ONE_PAGE>, dim3((unsigned)pieces), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
   if (rc != SPARSELNR_OK) return rc;
-  return launch(join_many<T, DP, ROWS>, dim3((unsigned)slots, ROWS / kJoinRows), kJoinBlock, 0, l, a);
+  return launch(join_many<T, DP, ROWS>, dim3((unsigned)l.cus, ROWS / kJoinRows), kJoinBlock, 0, l, a);
 }
 
 constexpr int64_t kPagesWorkspace = (int64_t)640 << 20;  // of partial results, at most
