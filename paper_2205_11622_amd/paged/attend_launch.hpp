@@ -10,8 +10,12 @@
 namespace slnr {
 namespace paged {
 
-// Pieces that the work is cut into, per compute unit: what is resident at once.
+// Pieces that the work is cut into, per compute unit.  Two blocks of attend_few are resident
+// on one.  Pieces of a selection are all alike, so they go in one round (32 tokens over 32
+// pages of 64: 69 us; at 3 a unit 87, at 4 77); contexts are ragged, and shorter pieces
+// even them out (64 of 512 to 16384 keys: 259 us; at 2 a unit 291, at 4 262).
 constexpr int kFewPerCu = 3;
+constexpr int kFewPerCuSparse = 2;
 constexpr int kManyPerCu = 1;
 // A request with more rows than this (tokens times heads of a group) goes to attend_many.
 constexpr int kFewMostRows = 64;
@@ -43,7 +47,7 @@ int partials(const Launch &l, int64_t slots, AttendArgs &a) {
 
 template <class T, int DP, bool SPARSE>
 int run_few(const Launch &l, AttendArgs a, int most_rows) {
-  a.target = l.cus * kFewPerCu;
+  a.target = l.cus * (SPARSE ? kFewPerCuSparse : kFewPerCu);
   const int64_t tiles = SPARSE ? (int64_t)a.T * ((a.G + kFewRows - 1) / kFewRows)
                                : (int64_t)a.T * a.G / kFewRows + a.R;
   const int64_t pieces = tiles * a.Hkv + a.target;
@@ -55,7 +59,8 @@ int run_few(const Launch &l, AttendArgs a, int most_rows) {
   const unsigned grid = (unsigned)(pieces < most ? pieces : most);
   rc = launch(attend_few<T, DP, SPARSE>, dim3(grid), kFewBlock, sizeof(FewShared<T, DP>), l, a);
   if (rc != SPARSELNR_OK) return rc;
-  return launch(join_few<T, DP>, dim3((unsigned)slots, most_rows < kFewRows ? most_rows : kFewRows), kJoinBlock, 0, l, a);
+  const unsigned side = most_rows < kFewRows ? most_rows : kFewRows;  // about 8000 blocks in all
+  return launch(join_few<T, DP>, dim3((unsigned)(slots < 8192 / side ? slots : 8192 / side), side), kJoinBlock, 0, l, a);
 }
 
 template <class T, int DP, int NW, bool ONE_PAGE>
