@@ -276,12 +276,16 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *     that keep each row of dim values at a multiple of 16 bytes (so a slice of a
  *     fused q/k/v projection and caches of either order of slots and heads
  *     will do); the dim values of a row are adjacent.  Anything else is
- *     SPARSELNR_ERR_UNSUPPORTED.  R < 2^24, T < 2^28, W * page_size and T * Hq < 2^31.
+ *     SPARSELNR_ERR_UNSUPPORTED.  R < 2^24, T < 2^28, T * Hq < 2^31,
+ *     W * page_size <= 2^31 - 4096; a seq_len past that of its table's row ends there.
  *   - R = 0 or T = 0 is a no-op.
- *   - The two attention calls use a workspace per (device, stream) for the
- *     results of contexts that are cut into pieces; its size depends on the
- *     type and dim class alone (at most 140 MB), so that one call of a kind allocates it,
+ *   - The two attention calls use a workspace per (device, stream).  For the
+ *     results of contexts that are cut into pieces its size depends on the type, on
+ *     dim and on max_new alone (at most 140 MB), so one call allocates it, and
  *     later ones and captured graphs find it whatever the lengths are.
+ *     sparselnr_block_attention of many tokens (four and more per page of
+ *     the table, on average) goes by pages: its partial results, at most 640 MB, and
+ *     lists grow with T, R, W and top, so a capture needs one call of those before.
  * ---------------------------------------------------------------------- */
 
 enum sparselnr_dtype { SPARSELNR_BF16 = 0, SPARSELNR_FP16 = 1, SPARSELNR_FP32 = 2 };

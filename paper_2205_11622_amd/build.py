@@ -36,8 +36,8 @@ def flags() -> list:
 
 
 def sources() -> list:
-    return [os.path.join(CSRC, "sparselnr.hip")] + sorted(
-        os.path.join(PAGED, f) for f in os.listdir(PAGED) if f.endswith(".hip"))
+    """paged/library.hip takes csrc/sparselnr.hip in."""
+    return sorted(os.path.join(PAGED, f) for f in os.listdir(PAGED) if f.endswith(".hip"))
 
 
 def build(verbose: bool = False) -> str:

@@ -14,7 +14,6 @@
 #include "walker.hpp"
 #include "epilogue.hpp"
 #include "batch.hpp"
-#include "../paged/runtime.hpp"
 
 namespace {
 
@@ -736,18 +735,6 @@ int run_epilogue(Mode mode, bool had, const int32_t *rowptr, const int32_t *coli
 }
 
 }  // namespace
-
-// For the entry points of the paged cache (paged/paged.hip).
-namespace slnr {
-
-int hip_error(hipError_t e) { return hip_fail(e); }
-int this_device(int *dev) { return current_device(dev); }
-int device_cu_count(int dev, int *cus) { return device_cus(dev, cus); }
-int stream_workspace(int dev, hipStream_t stream, size_t bytes, void **out, int slot) {
-  return get_workspace(dev, stream, bytes, out, slot);
-}
-
-}  // namespace slnr
 
 extern "C" {
 

@@ -17,6 +17,7 @@ using namespace slnr;
 using namespace slnr::paged;
 
 constexpr int64_t kMax31 = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxPositions = ((int64_t)1 << 31) - 4096;  // of a table's row: walks look a few tiles ahead
 
 int value_bytes(int32_t dtype) {
   switch (dtype) {
@@ -73,7 +74,7 @@ int check_requests(const sparselnr_requests *r, int64_t page_size) {
   if (r->R > 0 && (!r->seq_len || !r->qptr || (r->W > 0 && !r->table))) return SPARSELNR_ERR_INVALID_ARG;
   if (r->R > 1 && r->table_stride < r->W) return SPARSELNR_ERR_INVALID_ARG;
   if (r->R >= ((int64_t)1 << 24) || r->T >= ((int64_t)1 << 28)) return SPARSELNR_ERR_UNSUPPORTED;
-  if (page_size > 0 && r->W > kMax31 / page_size) return SPARSELNR_ERR_UNSUPPORTED;
+  if (page_size > 0 && r->W > kMaxPositions / page_size) return SPARSELNR_ERR_UNSUPPORTED;
   return SPARSELNR_OK;
 }
 
@@ -199,7 +200,7 @@ int sparselnr_page_tables(const int32_t *ctx_len, const int32_t *new_len, int32_
       (F > 0 && !free_pages) || (T > 0 && !slots) || (R > 1 && table_stride < W))
     return SPARSELNR_ERR_INVALID_ARG;
   const int shift = page_shift(page_size);
-  if (shift < 0 || R >= ((int64_t)1 << 24) || T >= ((int64_t)1 << 28) || F > kMax31 || W > kMax31 / page_size)
+  if (shift < 0 || R >= ((int64_t)1 << 24) || T >= ((int64_t)1 << 28) || F > kMax31 || W > kMaxPositions / page_size)
     return SPARSELNR_ERR_UNSUPPORTED;
   TablesArgs a{};
   a.ctx = ctx_len;

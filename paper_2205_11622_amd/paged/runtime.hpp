@@ -1,6 +1,6 @@
 // What the entry points of the paged cache share with the rest of the library:
 // the record of HIP errors, the device's facts and the workspaces per (device,
-// stream, slot) that sparselnr_release() frees.  Defined in csrc/sparselnr.hip.
+// stream, slot) that sparselnr_release() frees.  Defined in library.hip.
 #pragma once
 
 #include <hip/hip_runtime.h>

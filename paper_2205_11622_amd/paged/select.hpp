@@ -156,7 +156,9 @@ __global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 :
   const int t0 = qb + (id - start(r)) * TM;
   if (id < start(r) || t0 >= qe) return;
   const int tokens = qe - t0 < TM ? qe - t0 : TM;
-  const int seq = a.seq[r];
+  const int64_t row_ends = (int64_t)a.W << a.shift;  // a longer request ends with its table's row, as in attention
+  int seq = a.seq[r];
+  seq = seq < 0 ? 0 : seq < row_ends ? seq : (int)row_ends;
   const int pos0 = seq - (qe - qb) + (t0 - qb);  // position of the first token
   const int pos1 = pos0 + tokens - 1;
   const int32_t *table = a.table + (int64_t)r * a.table_row;
