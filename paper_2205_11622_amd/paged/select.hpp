@@ -165,6 +165,12 @@ __global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 :
   const int near1 = pos1 < 0 ? -1 : pos1 >> a.shift;
   const int blocks = near1 + 1 < a.W ? near1 + 1 : a.W;
 
+  auto table_entry = [&](int b) { return b < blocks ? table[b] : -1; };
+  constexpr int U = TM == 1 ? 4 : 2;  // groups of 16 pages that a wave has on their way
+  int ahead[U];  // table entries of the next ones (a segment that is not the last has some for every wave)
+#pragma unroll
+  for (int u = 0; u < U; ++u) ahead[u] = table_entry((wave + u * kSelectWaves) * 16 + col);
+
   // ------------------------------------------------------ the queries in 8 bits
   if (wave < TM) {  // a wave per token
     float u[DP / 64];
@@ -175,6 +181,7 @@ __global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 :
       double s = 0;
       if (wave < tokens && d < a.D) {
         const T *src = (const T *)a.q + (int64_t)(t0 + wave) * a.q_token + (int64_t)h * a.G * a.q_head + d;
+#pragma unroll 4
         for (int g = 0; g < a.G; ++g) s += (double)(float)src[g * a.q_head];
       }
       u[i] = (float)s;
@@ -197,7 +204,6 @@ __global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 :
   for (int i = 0; i < KS; ++i) qv[i] = *reinterpret_cast<const i32x4 *>(q8 + col * QS + i * 64 + grp * 16);
 
   const int near0 = pos0 < 0 ? -1 : pos0 >> a.shift;  // page of the first token
-  auto table_entry = [&](int b) { return b < blocks ? table[b] : -1; };
   const int my_token = TM == 1 ? 0 : wave;                   // row of the choice
   const int room_of_segment = a.capacity - a.top;
   int held = 0;                                              // carried entries of my row
@@ -207,11 +213,14 @@ __global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 :
     // Rows of the product are the tokens, columns 16 pages, so a lane has one page for
     // four tokens.  U groups at once: their entries, then their summaries are on their
     // way together.
-    constexpr int U = TM == 1 ? 4 : 2;
     for (int g0 = wave * 16; g0 < n; g0 += U * kSelectWaves * 16) {
       int page[U];
+      const int next = g0 + U * kSelectWaves * 16 < n ? seg + g0 + U * kSelectWaves * 16 : seg + room_of_segment + wave * 16;
 #pragma unroll
-      for (int u = 0; u < U; ++u) page[u] = table_entry(seg + g0 + u * kSelectWaves * 16 + col);
+      for (int u = 0; u < U; ++u) {
+        page[u] = ahead[u];
+        ahead[u] = table_entry(next + u * kSelectWaves * 16 + col);
+      }
       i32x4 kv[U][KS];
       float scale[U];
 #pragma unroll
