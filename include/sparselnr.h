@@ -284,7 +284,7 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *     dim and on max_new alone (at most 140 MB), so one call allocates it, and
  *     later ones and captured graphs find it whatever the lengths are.
  *     sparselnr_block_attention of many tokens (four and more per page of
- *     the table, on average) goes by pages: its partial results, at most 640 MB, and
+ *     the table, on average) goes by pages: its partial results, at most 144 MB, and
  *     lists grow with T, R, W and top, so a capture needs one call of those before.
  * ---------------------------------------------------------------------- */
 

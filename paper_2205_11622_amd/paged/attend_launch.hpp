@@ -48,8 +48,11 @@ int partials(const Launch &l, int64_t slots, AttendArgs &a) {
 template <class T, int DP, bool SPARSE>
 int run_few(const Launch &l, AttendArgs a, int most_rows) {
   a.target = l.cus * (SPARSE ? kFewPerCuSparse : kFewPerCu);
-  const int64_t tiles = SPARSE ? (int64_t)a.T * ((a.G + kFewRows - 1) / kFewRows)
-                               : (int64_t)a.T * a.G / kFewRows + a.R;
+  int64_t tiles = SPARSE ? (int64_t)a.T * ((a.G + kFewRows - 1) / kFewRows) : (int64_t)a.T * a.G / kFewRows + a.R;
+  // Beside attend_many: only what is left of a request has tiles here, often nothing, and
+  // a grid for more costs its launch.
+  const int64_t left = (int64_t)a.R * ((kFewMostRows + kFewRows - 1) / kFewRows);
+  if (!SPARSE && a.few <= kFewMostRows && tiles > left) tiles = left;
   const int64_t pieces = tiles * a.Hkv + a.target;
   if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
   const int64_t slots = 2 * (int64_t)a.target;  // of split tiles: see split_scan
@@ -81,7 +84,10 @@ int run_many(const Launch &l, AttendArgs a) {
   return launch(join_many<T, DP, ROWS>, dim3((unsigned)l.cus, ROWS / kJoinRows), kJoinBlock, 0, l, a);
 }
 
-constexpr int64_t kPagesWorkspace = (int64_t)640 << 20;  // of partial results, at most
+// Partial results of by_pages, at most (a call that has more is worked off by KV heads, then
+// by tokens): little enough that the join finds much of them in the 256 MB cache (2048
+// tokens over 16 pages, 8 heads, 545 MB: 405 us; at 80 MB 461, at 288 MB 421, all at once 413).
+constexpr int64_t kPagesWorkspace = (int64_t)144 << 20;
 
 // By pages (pages.hpp) rather than by queries: where a page is selected by four queries and
 // more on average, its keys are at least four times the heads of a group (the results
@@ -98,9 +104,13 @@ template <class T, int DP>
 int run_pages(const Launch &l, const AttendArgs &a) {
   PagesArgs p{};
   const int64_t per_token = (int64_t)a.Hkv * a.top;  // selected pages
-  int64_t most = kPagesWorkspace / (per_token * a.G * (DP + 2) * (int64_t)sizeof(float));
+  const int64_t bytes = (int64_t)a.top * a.G * (DP + 2) * sizeof(float);  // partial results of a token, per KV head
+  int64_t most = kPagesWorkspace / bytes;
   most = most < 1 ? 1 : most > a.T ? a.T : most;
   if (most * per_token >= ((int64_t)1 << 30)) most = (((int64_t)1 << 30) - 1) / per_token;
+  int64_t heads = kPagesWorkspace / (most * bytes);  // of a launch
+  heads = heads < 1 ? 1 : heads > a.Hkv ? a.Hkv : heads;
+  const int64_t rows = most * heads * a.top * a.G;  // of partial results
   p.buckets = a.Hkv * a.R * a.W;
   p.per_tile = kPagesRows / a.G;
   const int64_t picks = most * per_token, tiles = picks / p.per_tile + p.buckets;
@@ -113,7 +123,7 @@ int run_pages(const Launch &l, const AttendArgs &a) {
   const size_t count = take((size_t)p.buckets * 4), begin = take((size_t)p.buckets * 4),
                tile_begin = take((size_t)p.buckets * 4), total = take(4), rank = take((size_t)picks * 4),
                list = take((size_t)picks * 4), tile = take((size_t)tiles * 4),
-               part = take((size_t)picks * a.G * DP * 4), ml = take((size_t)picks * a.G * 8);
+               part = take((size_t)rows * DP * 4), ml = take((size_t)rows * 8);
   void *ws = nullptr;
   int rc = stream_workspace(l.dev, l.stream, size, &ws, kSlotAttend);
   if (rc != SPARSELNR_OK) return rc;
@@ -134,14 +144,17 @@ int run_pages(const Launch &l, const AttendArgs &a) {
     hipLaunchKernelGGL(pages_scan, dim3(1), dim3(kScanBlock), 0, l.stream, p);
     hipLaunchKernelGGL(pages_fill, each, block, 0, l.stream, a, p);
     if ((rc = done()) != SPARSELNR_OK) return rc;
-    // a page makes at most one tile more than its queries fill, and none without queries
-    const int64_t extra = n < p.buckets ? n : p.buckets;
-    hipLaunchKernelGGL((attend_pages<T, DP>), dim3((unsigned)(n / p.per_tile + extra)), block,
-                       sizeof(PagesShared<T, DP>), l.stream, a, p);
-    if ((rc = done()) != SPARSELNR_OK) return rc;
-    const int64_t rows = (int64_t)p.tokens * a.Hq;
-    hipLaunchKernelGGL((join_pages<T, DP>), dim3((unsigned)((rows + 3) / 4)), block, 0, l.stream, a, p);
-    if ((rc = done()) != SPARSELNR_OK) return rc;
+    for (p.h0 = 0; p.h0 < a.Hkv; p.h0 += p.heads) {
+      p.heads = heads < a.Hkv - p.h0 ? (int)heads : a.Hkv - p.h0;
+      // a page makes at most one tile more than its queries fill, and none without queries
+      const int64_t m = (int64_t)p.tokens * p.heads * a.top, b = (int64_t)p.heads * a.R * a.W;
+      hipLaunchKernelGGL((attend_pages<T, DP>), dim3((unsigned)(m / p.per_tile + (m < b ? m : b))), block,
+                         sizeof(PagesShared<T, DP>), l.stream, a, p);
+      if ((rc = done()) != SPARSELNR_OK) return rc;
+      const int64_t out = (int64_t)p.tokens * p.heads * a.G;
+      hipLaunchKernelGGL((join_pages<T, DP>), dim3((unsigned)((out + 3) / 4)), block, 0, l.stream, a, p);
+      if ((rc = done()) != SPARSELNR_OK) return rc;
+    }
   }
   return SPARSELNR_OK;
 }

@@ -24,8 +24,9 @@ struct PagesArgs {
   int32_t *rank;                        // per (token, h, j): place in its page's list, -1: no page
   int32_t *list;                        // (token - t0) * top + j
   int32_t *tile;                        // bucket of a tile
-  float *part, *ml;                     // per (token, h, j, g): DP values; maximum and sum
+  float *part, *ml;                     // per (token, h - h0, j, g): DP values; maximum and sum
   int32_t t0, tokens, buckets, per_tile;  // per_tile: queries of a tile
+  int32_t h0, heads;                    // the KV heads of this launch
 };
 
 constexpr int kPagesBlock = 256;
@@ -158,10 +159,12 @@ __global__ __launch_bounds__(kPagesBlock, DP <= 128 ? 2 : 1) void attend_pages(A
   const float sc = score_unit<T>(a);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 31, half = lane >> 5;
-  if ((int)blockIdx.x >= *pa.total) return;
-  const int bucket = pa.tile[blockIdx.x];
+  const int per_head = a.R * a.W, last = pa.h0 + pa.heads;  // tiles lie by heads
+  const int tile = pa.tile_begin[pa.h0 * per_head] + (int)blockIdx.x;
+  if (tile >= (last < a.Hkv ? pa.tile_begin[last * per_head] : *pa.total)) return;
+  const int bucket = pa.tile[tile];
   const int b = bucket % a.W, r = (bucket / a.W) % a.R, h = bucket / (a.W * a.R);
-  const int e0 = (blockIdx.x - pa.tile_begin[bucket]) * pa.per_tile;
+  const int e0 = (tile - pa.tile_begin[bucket]) * pa.per_tile;
   const int entries = imin(pa.count[bucket] - e0, pa.per_tile);
   const int32_t *list = pa.list + pa.begin[bucket] + e0;
   const int page = a.table[(int64_t)r * a.table_row + b];
@@ -311,7 +314,7 @@ __global__ __launch_bounds__(kPagesBlock, DP <= 128 ? 2 : 1) void attend_pages(A
   l = sum_across_32(l);
   if (l != l) m = __builtin_inff();  // NaN among the scores: the whole row is NaN
   if (have_row) {
-    const int64_t at = (((int64_t)t * a.Hkv + h) * a.top + j_of) * a.G + g;
+    const int64_t at = (((int64_t)t * pa.heads + (h - pa.h0)) * a.top + j_of) * a.G + g;
     float *dst = pa.part + at * DP;
 #pragma unroll
     for (int c = 0; c < DT; ++c)
@@ -333,13 +336,15 @@ __global__ __launch_bounds__(kPagesBlock) void join_pages(AttendArgs a, PagesArg
   typedef float Cols __attribute__((ext_vector_type(C)));
   const float sc = score_unit<T>(a);
   const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * (kPagesBlock / kWave) + (threadIdx.x >> 6);  // (token - t0) * Hq + head
-  if (row >= (int64_t)pa.tokens * a.Hq) return;
-  const int t = (int)(row / a.Hq), hd = (int)(row % a.Hq), h = hd / a.G, g = hd % a.G;
+  const int64_t row = (int64_t)blockIdx.x * (kPagesBlock / kWave) + (threadIdx.x >> 6);  // of the launch's (token, head)
+  const int share = pa.heads * a.G;
+  if (row >= (int64_t)pa.tokens * share) return;
+  const int t = (int)(row / share), hs = (int)(row % share) / a.G, g = (int)(row % share) % a.G;
+  const int h = pa.h0 + hs, hd = h * a.G + g;
   const int tok = pa.t0 + t;
   if (tok < a.qptr[0] || tok >= a.qptr[a.R]) return;  // of no request
-  const int64_t first = ((int64_t)t * a.Hkv + h) * a.top;
-  const int32_t *rank = pa.rank + first;
+  const int64_t first = ((int64_t)t * pa.heads + hs) * a.top;
+  const int32_t *rank = pa.rank + ((int64_t)t * a.Hkv + h) * a.top;
   float mx = kNegInf;
   for (int j = lane; j < a.top; j += kWave)
     if (rank[j] >= 0) mx = fmaxf(mx, pa.ml[((first + j) * a.G + g) * 2]);
