@@ -660,3 +660,32 @@ def test_by_pages_infinities_and_nan_ahead_of_a_query(gpu):
     assert (got[first:, :, 5] == math.inf).all() and torch.isnan(got[first:, :, 6]).all()
     rest = [d for d in range(64) if d not in (5, 6)]
     assert torch.equal(got[first:][:, :, rest], want[first:][:, :, rest])
+
+
+@pytest.mark.parametrize("Hkv,T", [(2, 1300), (3, 1000), (1, 2400)])
+def test_by_pages_in_several_launches(gpu, Hkv, T):
+    """More partial results than are kept at a time: one KV head after the other (of three, two and
+    one), or the tokens in two parts."""
+    D, P, G, top = 64, 64, 16, 16
+    b = pu.Batch([20 * P + 9, 5], [T, 3], G * Hkv, Hkv, D, P, FP16, seed=60 + Hkv)
+    sel = random_selection(b, Hkv, top, 61)
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    s = b.ints(sel, gpu)
+    lse = torch.full(q.shape[:2], math.nan, device=gpu)
+    out = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, s, lse=lse)
+    again = slnr.sparselnr_block_attention(q, kc, vc, table, seq, qptr, s)
+    assert torch.equal(out, again) and not torch.isnan(lse).any()
+    n = torch.tensor([1], dtype=torch.int32, device=gpu)
+    ptr = torch.tensor([0, 1], dtype=torch.int32, device=gpu)
+    # partial results of 16 * 16 rows of 66 numbers a token: 2234 tokens of a head are 144 MB
+    for t in [0, 500, 999, T - 1, T, T + 2] + [t for t in (2233, 2234) if t < T]:
+        r = 0 if t < T else 1
+        pos = b.ctx[r] + t - b.qptr[r]
+        one = slnr.sparselnr_block_attention(q[t:t + 1], kc, vc, table[r:r + 1], n * (pos + 1), ptr, s[t:t + 1])
+        ref, want_lse, weight = pu.attention(b.q[t:t + 1], b.kc, b.vc, [b.table[r]], [pos + 1], [0, 1], D ** -0.5,
+                                             sel=[s[t].tolist()])
+        tol = pu.tolerance(FP16, weight, pos + 1, D, vmax(b))
+        assert ((out[t:t + 1].double().cpu() - ref).abs() <= tol).all(), t
+        assert ((out[t:t + 1].double().cpu() - one.double().cpu()).abs() <= 2 * tol).all(), t
+        fine = want_lse[0] > -math.inf
+        assert ((lse[t].double().cpu() - want_lse[0]).abs()[fine] <= 1e-5 + 1e-6 * want_lse[0].abs()[fine]).all()
