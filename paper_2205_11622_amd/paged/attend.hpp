@@ -21,7 +21,7 @@ struct AttendArgs {
   void *out;             // [T][Hq][D], densely packed
   float *lse;            // [T][Hq] or null
   float *part;           // per piece of a split tile: rows x DP values, then rows maxima and sums
-  int32_t *meta;         // per piece, what the join has to know (see Meta)
+  int32_t *meta;         // per piece, what the join has to know (see kMeta)
   int32_t R, T, W, pages, shift, Hq, Hkv, G, D, top, window;
   int32_t few;           // requests with at most this many rows belong to attend_few, the others to attend_many
   int32_t target;        // pieces that the work is cut into, about
@@ -121,8 +121,10 @@ __device__ __forceinline__ Request request_of(const AttendArgs &a, int r) {
 // about `target` pieces, so long contexts are cut where there are few tiles and
 // left whole where there are many.  With a tail, the tiles behind the first 70% of the
 // work are cut kTailCuts times finer: the blocks that are done early find something
-// to fill the time with until the longest one is done (520 tiles on 256 compute
-// units: three rounds, the last with 8 tiles, become little more than two).
+// to fill the time with until the longest one is done.  Only attend_many has one: one
+// block fills a compute unit there, and 520 tiles on 256 of them, three rounds
+// of which the last has 8, become little more than two.  attend_few has three
+// pieces a unit, two at a time, anyway.
 // Every block derives the split from the lengths by one scan: nothing has to be
 // planned, copied or known on the host.
 
@@ -282,6 +284,12 @@ __device__ Piece split_find(const Split<NT> &sh, const AttendArgs &a, int q, F c
 //
 // Bound by memory: a key is read once for all heads of its group.  16 KB of K and V
 // are in flight per wave while the previous tile is worked on.
+//
+// 64 requests of 513 to 15096 keys, 32 / 8 heads of 128 in bf16 (1190 MB): 252 us, 4.7 TB/s,
+// what a copy of 4 GiB reaches; the join adds 7.  32 tokens over 32 selected
+// pages of 64 keys (269 MB): 64 us, 4.2 TB/s, and 5.5.  4 requests of 635 to 933 keys, 8 / 2
+// heads of 64 in fp32 (3 MB): 12 us and 4.5, the latency of the lengths, the split, the
+// table, a tile, the four waves' join and the launches.
 
 constexpr int kFewBlock = 256;
 constexpr int kFewWaves = kFewBlock / kWave;
@@ -632,11 +640,27 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
 // --------------------------------------------------------------- many rows
 //
 // attend_many: a block takes one piece of a tile of 32 * NW rows, 32 to a wave, and
-// walks it in tiles of 64 keys that all its waves share through LDS (two buffers;
-// the next tile's rows are in registers, the ones after it on their way).  As above
-// S^T = K Q^T and O^T = V^T P^T, here on the 32 x 32 x 16 products: a lane holds one
-// query and half the keys of a tile, so a row's maximum takes one exchange and P^T is
-// used where it lies.
+// walks it in tiles of 64 keys that all its waves share through LDS (two buffers of K and
+// of V, the next stage's rows on their way in registers).  As above S^T = K Q^T and
+// O^T = V^T P^T, here on the 32 x 32 x 16 products: a lane holds one query and half
+// the keys of a tile, so a row's maximum takes one exchange and P^T is used where it
+// lies; V^T comes out of LDS through transposing reads.
+//
+// Bound by the matrix products and by what feeds them: a product of 32 cycles takes 1 KB of
+// K or V from LDS, so four SIMDs at once use all of its 128 bytes a cycle, and
+// two waves of a SIMD take turns, one in its products, one in its softmax.  4073 tokens
+// behind 6818 and 7894, 32 / 8 heads of 128 in bf16 (559 GFLOP): 690 to 720 us, 0.78
+// to 0.81 PFLOP/s, and 36 us for the join (a product of 8192^3: 1.2).  Of that time, the
+// same with work left out: 0.97 without exponentials, 0.96 without loads, 0.65 without P V.
+// 24 requests under a window of 1024, 16 / 4 heads of 64 in fp16 (2.3 GFLOP): 27 us, two
+// tiles deep and bound by latency.
+// Measured and not taken: V transposed on its way into LDS, 1.07 times as long; all waves
+// in the same phase 1.08; the late half in odd waves, two of them on each of two SIMDs, 1.17;
+// 64 rows to a wave, one wave to a SIMD, 1.35 (half the bytes from LDS, but one wave issues its
+// softmax and its products one after the other).
+//
+// NW: eight waves, two to a SIMD; four where O of 256 columns or fp32 takes the
+// registers or the LDS of two.
 template <class T, int DP, int NW>
 struct ManyShared {
   T k[2][64 * Tile<T, DP>::kStride];
@@ -651,7 +675,6 @@ constexpr float kLag = 8.0f;      // the maximum that weights are taken at may b
 constexpr int kMfma = 0x008, kDsRead = 0x100;
 constexpr int kManyMinSteps = 8;  // a piece is at least so many tiles of keys long
 
-//
 // ONE_PAGE: every tile of 64 keys lies in one page (64 positions and more, which begin
 // at multiples of 64), so its address is a scalar to which a lane adds 32 bits.
 template <class T, int DP, int NW, bool ONE_PAGE>
@@ -1151,6 +1174,8 @@ __global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
 }
 
 // The same for the tiles of attend_many: many rows of few pieces, a wave per row.
+// Bound by memory and by its start: 36 us behind the 559 GFLOP above, 9 behind the
+// window's batch; one row to a block's wave at a time took 44 and 18.
 constexpr int kJoinRows = 8;  // rows of a block, two of them one after the other in each wave
 
 template <class T, int DP, int ROWS>

@@ -13,7 +13,7 @@ namespace paged {
 // Pieces that the work is cut into, per compute unit.  Two blocks of attend_few are resident
 // on one.  Pieces of a selection are all alike, so they go in one round (32 tokens over 32
 // pages of 64: 69 us; at 3 a unit 87, at 4 77); contexts are ragged, and shorter pieces
-// even them out (64 of 512 to 16384 keys: 259 us; at 2 a unit 291, at 4 262).
+// even them out (64 of 513 to 15096 keys: 259 us; at 2 a unit 291, at 4 262).
 constexpr int kFewPerCu = 3;
 constexpr int kFewPerCuSparse = 2;
 constexpr int kManyPerCu = 1;
