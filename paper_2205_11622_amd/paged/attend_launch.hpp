@@ -18,7 +18,12 @@ constexpr int kFewPerCu = 3;
 constexpr int kFewPerCuSparse = 2;
 constexpr int kManyPerCu = 1;
 // A request with more rows than this (tokens times heads of a group) goes to attend_many.
-constexpr int kFewMostRows = 64;
+// 64 requests of 4000 keys and 32 rows, 8 heads of 128 in bf16: 292 us as few rows, 382 as many;
+// of 48: 410 and 385, of 128: 1046 and 413.  256 columns cross there too; 64 columns in fp16 at
+// 64 rows (111 and 118; 48: 81 and 116; 128: 171 and 123), fp32 behind them (128 columns, 64 rows:
+// 396 and 478; 128: 700 and 490).
+template <class T, int DP>
+constexpr int kFewMostRows = sizeof(T) == 2 && DP > 64 ? 32 : 64;
 
 struct Launch {
   int dev, cus;
@@ -51,8 +56,8 @@ int run_few(const Launch &l, AttendArgs a, int most_rows) {
   int64_t tiles = SPARSE ? (int64_t)a.T * ((a.G + kFewRows - 1) / kFewRows) : (int64_t)a.T * a.G / kFewRows + a.R;
   // Beside attend_many: only what is left of a request has tiles here, often nothing, and
   // a grid for more costs its launch.
-  const int64_t left = (int64_t)a.R * ((kFewMostRows + kFewRows - 1) / kFewRows);
-  if (!SPARSE && a.few <= kFewMostRows && tiles > left) tiles = left;
+  const int64_t left = (int64_t)a.R * ((kFewMostRows<T, DP> + kFewRows - 1) / kFewRows);
+  if (!SPARSE && a.few <= kFewMostRows<T, DP> && tiles > left) tiles = left;
   const int64_t pieces = tiles * a.Hkv + a.target;
   if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
   const int64_t slots = 2 * (int64_t)a.target;  // of split tiles: see split_scan
@@ -169,10 +174,11 @@ int run_attend(const Launch &l, AttendArgs a, int64_t max_new) {
   const int64_t rows = (max_new > 0 && max_new < a.T ? max_new : a.T) * a.G;
   a.few = 0x7fffffff;
   if constexpr (!(sizeof(T) == 4 && DP > 128)) {
-    if (rows > kFewMostRows) {
+    if (rows > kFewMostRows<T, DP>) {
       constexpr int NW = sizeof(T) == 4 || DP > 128 ? 4 : 8;
-      a.few = kFewMostRows;
-      // a tile of keys within one page, 64 rows of it within 32 bits of bytes
+      a.few = kFewMostRows<T, DP>;
+      // a tile of keys within one page, 64 rows of it within 32 bits of bytes (4073 tokens
+      // behind 6818 and 7894: 706 us, 741 without)
       const bool one_page = a.shift >= 6 && a.k_slot < (1 << 23) && a.v_slot < (1 << 23);
       const int rc = one_page ? run_many<T, DP, NW, true>(l, a) : run_many<T, DP, NW, false>(l, a);
       if (rc != SPARSELNR_OK) return rc;

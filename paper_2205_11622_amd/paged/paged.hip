@@ -139,13 +139,17 @@ int attend(const void *q, int64_t q_token, int64_t q_head, int64_t Hq, const spa
   }
 }
 
-// Few tokens: the heads are shared out until there are about four blocks a compute unit.
-// Many: as many tokens a block as leave eight blocks to a unit, at most 8.
+// A block starts at about 3 ns after the one before, and the one with a page's last new row
+// reads the page: about two blocks a unit, of up to 16 tokens, or of a share of the
+// heads where the tokens are few (tokens a block x shares, 8 heads of 128 in bf16; 1024
+// tokens: 8 x 4 9.9 us, 1 x 1 19, 8 x 1 17; 8192: 16 x 1 34, 8 x 1 35, 16 x 4 39, 4 x 1 50;
+// 64: 1 x 8 8.7, 1 x 1 10.4, 8 x 1 31).
 template <class T>
 int run_append(const Launch &l, const AppendArgs &a) {
-  int64_t shares = 4 * (int64_t)l.cus / a.T, per = a.T / ((int64_t)l.cus * 8);
+  int64_t per = a.T / (l.cus / 2 > 0 ? l.cus / 2 : 1);
+  per = per < 1 ? 1 : per > 16 ? 16 : per;
+  int64_t shares = 2 * (int64_t)l.cus / ((a.T + per - 1) / per);
   shares = shares < 1 ? 1 : shares > a.Hkv ? a.Hkv : shares;
-  per = per < 1 ? 1 : per > 8 ? 8 : per;
   hipLaunchKernelGGL(cache_append<T>, dim3((unsigned)((a.T + per - 1) / per), (unsigned)shares), dim3(kAppendBlock), 0,
                      l.stream, a, (int)per);
   return launched();
@@ -171,8 +175,11 @@ int run_select(const Launch &l, SelectArgs a, int64_t Hkv) {
 template <class T, int DP>
 int select_rows(const Launch &l, const SelectArgs &a, int64_t Hkv) {
   const int64_t entries = (int64_t)a.W + 16 + a.top;
-  // Fewer than four tokens a request on average: a block per token.  Otherwise 16 tokens share a page's summary.
-  if ((int64_t)a.T < 4 * (int64_t)a.R) {
+  // Fewer than three tokens a request on average, or no more blocks than compute units: a block
+  // per token; otherwise 16 tokens share a page's summary.  64 requests behind 30000 tokens in pages
+  // of 64, 8 heads: of 1 token 25 us (16 to a block: 56), of 2 47 (53), of 3 69 (59), of 4 91 (53);
+  // 8 requests of 4 behind 200000 37 (83), 4 of 16 behind 30000 42 (22).
+  if ((int64_t)a.T < 3 * (int64_t)a.R || (int64_t)a.T * Hkv <= l.cus) {
     if (entries <= 4 * kSelectBlock) return run_select<T, DP, 1, 4>(l, a, Hkv);
     return run_select<T, DP, 1, 16>(l, a, Hkv);
   }
