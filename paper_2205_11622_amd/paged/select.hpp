@@ -117,7 +117,7 @@ __device__ __forceinline__ bool choose_few(const unsigned (&v)[NR], int top, uns
 //
 // Bound by latency: the table, the summaries behind it, the choice's steps one after
 // the other.  32 tokens, 8 heads of 128, contexts of 8302 to 55936 in pages of 64 (13 MB):
-// 16 us; 2020 tokens behind 34227 and 40918 (19 MB, 2.5 Gop): 56 us, of which vector instructions
+// 16 us; 2020 tokens behind 34227 and 40918 (19 MB, 2.5 Gop): 53 us, of which vector instructions
 // fill a third.  There two blocks share a compute unit (64 registers to a wave; one block
 // of 128: 79 us).
 //
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 :
   const int blocks = near1 + 1 < a.W ? near1 + 1 : a.W;
 
   auto table_entry = [&](int b) { return b < blocks ? table[b] : -1; };
-  constexpr int U = TM == 1 ? 4 : 2;  // groups of 16 pages that a wave has on their way
+  constexpr int U = TM == 1 ? 4 : 1;  // groups of 16 pages that a wave has on their way (16 tokens: two 55 us, one 53)
   int ahead[U];  // table entries of the next ones (a segment that is not the last has some for every wave)
 #pragma unroll
   for (int u = 0; u < U; ++u) ahead[u] = table_entry((wave + u * kSelectWaves) * 16 + col);
