@@ -63,8 +63,8 @@ __device__ __forceinline__ int bucket_of(const AttendArgs &a, const PagesArgs &p
 }
 
 // Neighbouring lanes are neighbouring tokens: pages that all tokens select (the first, the
-// last) are then counted once a wave.  One by one their counters took 28 us of a
-// call on 2020 tokens.
+// last) are then counted once a wave: 21 us for the 2020 tokens above, most of it atomics
+// on their way; one by one 28.
 static __global__ __launch_bounds__(kPagesBlock) void pages_count(AttendArgs a, PagesArgs p) {
   const int e = blockIdx.x * kPagesBlock + threadIdx.x;
   const bool in = e < p.tokens * a.Hkv * a.top;
@@ -76,13 +76,12 @@ static __global__ __launch_bounds__(kPagesBlock) void pages_count(AttendArgs a, 
     const int lane = threadIdx.x & 63, lead = __builtin_ctzll(some);
     const int common = __shfl(bucket, lead);
     const unsigned long long same = __builtin_amdgcn_ballot_w64(bucket == common);
-    int base = 0;
-    if (lane == lead) base = atomicAdd(&p.count[common], __popcll(same));
-    base = __shfl(base, lead);
-    if (bucket == common)
-      rank = base + __popcll(same & ((1ull << lane) - 1));
-    else if (bucket >= 0)
-      rank = atomicAdd(&p.count[bucket], 1);
+    // one atomic a lane, on their way together
+    const bool shared = bucket == common;
+    int got = 0;
+    if (bucket >= 0 && (!shared || lane == lead)) got = atomicAdd(&p.count[bucket], shared ? __popcll(same) : 1);
+    const int base = __shfl(got, lead);
+    if (bucket >= 0) rank = shared ? base + __popcll(same & ((1ull << lane) - 1)) : got;
   }
   if (in) p.rank[i] = rank;
 }
