@@ -279,13 +279,16 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *     SPARSELNR_ERR_UNSUPPORTED.  R < 2^24, T < 2^28, T * Hq < 2^31,
  *     W * page_size <= 2^31 - 4096; a seq_len past that of its table's row ends there.
  *   - R = 0 or T = 0 is a no-op.
- *   - The two attention calls use a workspace per (device, stream).  For the
- *     results of contexts that are cut into pieces its size depends on the type, on
- *     dim and on max_new alone (at most 140 MB), so one call allocates it, and
- *     later ones and captured graphs find it whatever the lengths are.
+ *   - The two attention calls use a workspace per (device, stream) for the results of
+ *     contexts that are cut into pieces.  It has one size for all of them, whatever
+ *     their tokens, lengths, heads, hint, type and dim are (130 MB on 256 compute
+ *     units): a stream's first call allocates it, later ones and captured graphs find it.
  *     sparselnr_block_attention of many tokens (four and more per page of
- *     the table, on average) goes by pages: its partial results, at most 144 MB, and
- *     lists grow with T, R, W and top, so a capture needs one call of those before.
+ *     the table, on average) goes by pages and has a workspace of its own: its partial
+ *     results, at most 144 MB (or those of one token and KV head, if they are more), and
+ *     lists, which grow with T, R, W, top and the heads.  A capture of such a call
+ *     needs one before, and while the graph may be replayed no call by pages on that
+ *     stream may be larger.
  * ---------------------------------------------------------------------- */
 
 enum sparselnr_dtype { SPARSELNR_BF16 = 0, SPARSELNR_FP16 = 1, SPARSELNR_FP32 = 2 };

@@ -37,16 +37,39 @@ int launch(F *fn, dim3 grid, int block, size_t lds, const Launch &l, const Atten
   return e == hipSuccess ? SPARSELNR_OK : hip_error(e);
 }
 
-// Partial results of `slots` pieces behind their records.
-template <int ROWS, int DP>
-int partials(const Launch &l, int64_t slots, AttendArgs &a) {
-  const size_t head = ((size_t)(1 + slots) * kMeta * sizeof(int32_t) + 255) / 256 * 256;
+// Slots of split tiles that cutting the work into about `target` pieces takes (see split_scan):
+// a tile of x caps makes at most x + 1 pieces and, if it is cut, at most 2 x.
+constexpr int64_t few_slots(int64_t target) { return 2 * target; }
+// With a tail: the work is `target` caps, three tenths of it (and what a tile reaches over) of
+// a kTailCuts-th.
+constexpr int64_t many_caps(int64_t target) { return target + target * kTailCuts * 3 / 10 + kTailCuts; }
+constexpr int64_t many_slots(int64_t target) { return 2 * many_caps(target); }
+
+// Partial results of `slots` pieces of `values` numbers, behind their records.
+constexpr size_t records_bytes(int64_t slots) {
+  return ((size_t)(1 + slots) * kMeta * sizeof(int32_t) + 255) / 256 * 256;
+}
+constexpr size_t partials_bytes(int64_t slots, int64_t values) {
+  return records_bytes(slots) + (size_t)slots * values * sizeof(float);
+}
+
+// The workspace has one size for all calls on a device, the largest need there is (130 MB on 256
+// units): a captured graph holds its address, so no later call of other tokens, heads, hint,
+// type or dim may be one that has to grow it.
+constexpr int64_t kFewValues = kFewRows * (kMaxDim + 2);
+constexpr int64_t kManyValues = 256 * (128 + 2);  // eight waves of 32 rows up to 128 columns, four up to 256
+inline size_t attend_bytes(int cus) {
+  const size_t few = partials_bytes(few_slots((int64_t)cus * kFewPerCu), kFewValues);
+  const size_t many = partials_bytes(many_slots((int64_t)cus * kManyPerCu), kManyValues);
+  return few > many ? few : many;
+}
+
+inline int partials(const Launch &l, int64_t slots, AttendArgs &a) {
   void *ws = nullptr;
-  const int rc = stream_workspace(l.dev, l.stream, head + (size_t)slots * ROWS * (DP + 2) * sizeof(float), &ws,
-                                  kSlotAttend);
+  const int rc = stream_workspace(l.dev, l.stream, attend_bytes(l.cus), &ws, kSlotAttend);
   if (rc != SPARSELNR_OK) return rc;
   a.meta = (int32_t *)ws;
-  a.part = (float *)((char *)ws + head);
+  a.part = (float *)((char *)ws + records_bytes(slots));
   return SPARSELNR_OK;
 }
 
@@ -60,8 +83,9 @@ int run_few(const Launch &l, AttendArgs a, int most_rows) {
   if (!SPARSE && a.few <= kFewMostRows<T, DP> && tiles > left) tiles = left;
   const int64_t pieces = tiles * a.Hkv + a.target;
   if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
-  const int64_t slots = 2 * (int64_t)a.target;  // of split tiles: see split_scan
-  int rc = partials<kFewRows, DP>(l, slots, a);
+  static_assert(kFewRows * (DP + 2) <= kFewValues && kFewPerCuSparse <= kFewPerCu, "fits the workspace");
+  const int64_t slots = few_slots(a.target);
+  int rc = partials(l, slots, a);
   if (rc != SPARSELNR_OK) return rc;
   const int64_t most = (int64_t)l.cus * 8;
   const unsigned grid = (unsigned)(pieces < most ? pieces : most);
@@ -76,13 +100,10 @@ int run_many(const Launch &l, AttendArgs a) {
   constexpr int ROWS = 32 * NW;
   a.target = l.cus * kManyPerCu;
   const int64_t tiles = ((int64_t)a.T * a.G / ROWS + a.R) * a.Hkv;
-  // Of split_scan: a tile of x caps makes at most x + 1 and, if it is cut, at most 2 x pieces;
-  // the work is `target` caps, three tenths of it (and what a tile reaches over) of a kTailCuts-th.
-  const int64_t caps = (int64_t)a.target + (int64_t)a.target * kTailCuts * 3 / 10 + kTailCuts;
-  const int64_t pieces = tiles + caps;
+  static_assert(ROWS * (DP + 2) <= kManyValues, "fits the workspace");
+  const int64_t pieces = tiles + many_caps(a.target);
   if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
-  const int64_t slots = 2 * caps;
-  int rc = partials<ROWS, DP>(l, slots, a);
+  int rc = partials(l, many_slots(a.target), a);
   if (rc != SPARSELNR_OK) return rc;
   rc = launch(attend_many<T, DP, NW, ONE_PAGE>, dim3((unsigned)pieces), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
   if (rc != SPARSELNR_OK) return rc;
@@ -130,7 +151,7 @@ int run_pages(const Launch &l, const AttendArgs &a) {
                list = take((size_t)picks * 4), tile = take((size_t)tiles * 4),
                part = take((size_t)rows * DP * 4), ml = take((size_t)rows * 8);
   void *ws = nullptr;
-  int rc = stream_workspace(l.dev, l.stream, size, &ws, kSlotAttend);
+  int rc = stream_workspace(l.dev, l.stream, size, &ws, kSlotPages);
   if (rc != SPARSELNR_OK) return rc;
   auto at = [&](size_t offset) { return (int32_t *)((char *)ws + offset); };
   p.count = at(count), p.begin = at(begin), p.tile_begin = at(tile_begin), p.total = at(total), p.rank = at(rank);

@@ -1,0 +1,48 @@
+"""What the paged-cache entry points allocate and launch, on a recording stand-in for the HIP
+runtime: no GPU is needed."""
+import pytest
+
+from tests import host_record as hr
+
+
+# ------------------------------------------------------------- workspaces
+
+
+def workspace_scenario(rec):
+    """Dense and sparse calls of every kind on one stream, a few tokens first."""
+    out = []
+
+    def look(what, call):
+        events = rec.events(call)
+        out.append([what, [e.bytes for e in events if e.kind == hr.MALLOC], len([e for e in events if e.kind == hr.FREE])])
+
+    look("4 tokens", lambda: rec.attend(4))
+    look("64 tokens", lambda: rec.attend(64))
+    look("64 tokens, hint 1", lambda: rec.attend(64, max_new=1))
+    look("64 heads a group", lambda: rec.attend(4, Hq=64, heads=1))
+    look("4096 tokens of 64 requests", lambda: rec.attend(4096, requests=rec.requests(4096, 64)))
+    look("selection of 4", lambda: rec.sparse(4, 16))
+    for dtype in (0, 1, 2):
+        for dim in (64, 128, 256):
+            look("dim %d, dtype %d" % (dim, dtype), lambda: rec.attend(600, dim=dim, dtype=dtype))
+    pages = rec.events(lambda: rec.sparse(2000, 16))
+    out.append(["by pages", [e.bytes for e in pages if e.kind == hr.MALLOC], len([e for e in pages if e.kind == hr.FREE])])
+    assert any("attend_pages" in e.name for e in pages)
+    look("more by pages", lambda: rec.sparse(4000, 32))
+    look("4 tokens again", lambda: rec.attend(4))
+    return out
+
+
+def test_a_streams_attention_workspace_is_allocated_once(tmp_path):
+    """The first call allocates it and no later one frees or grows it, whatever its tokens, heads, hint,
+    type and dim are: a captured graph that holds its address stays right.  Attention by pages has one of its own."""
+    seen = hr.run(workspace_scenario, tmp_path)
+    what, allocated, freed = seen[0]
+    assert len(allocated) == 1 and freed == 0 and allocated[0] <= 140e6
+    for what, allocated, freed in seen[1:]:
+        if what == "by pages":
+            assert len(allocated) == 1 and freed == 0
+        elif what == "more by pages":
+            assert freed <= 1  # of its own
+        else:
+            assert allocated == [] and freed == 0, what
