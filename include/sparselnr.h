@@ -50,7 +50,10 @@
  *     on first use, grown when a call needs more, reused, and freed by
  *     sparselnr_release().
  *     Calls on different streams use different workspaces; calls on one
- *     stream are ordered by the stream.
+ *     stream are ordered by the stream.  A call of the sparse products is several
+ *     launches over its workspace: host threads that share a stream have to
+ *     make them one after the other (the calls of the paged cache, below, hold their
+ *     workspace until their last launch is queued and need no such care).
  *   - HIP graph capture: once a stream's workspace is large enough (after
  *     one uncaptured call of the same size, width and grid factor on that
  *     stream), a call launches kernels only, with no allocation,
@@ -429,7 +432,8 @@ SPARSELNR_API int sparselnr_set_grid_factor(int factor);
 SPARSELNR_API int sparselnr_get_grid_factor(void);
 
 /* Waits for the device(s) and frees every workspace the library allocated.
- * Safe to call at any time; later calls allocate again. */
+ * Safe to call at any time that no other thread is inside a call of the sparse
+ * products; later calls allocate again. */
 SPARSELNR_API int sparselnr_release(void);
 
 #ifdef __cplusplus

@@ -64,12 +64,11 @@ inline size_t attend_bytes(int cus) {
   return few > many ? few : many;
 }
 
-inline int partials(const Launch &l, int64_t slots, AttendArgs &a) {
-  void *ws = nullptr;
-  const int rc = stream_workspace(l.dev, l.stream, attend_bytes(l.cus), &ws, kSlotAttend);
+inline int partials(const Launch &l, int64_t slots, AttendArgs &a, HeldWorkspace *ws) {
+  const int rc = hold_workspace(l.dev, l.stream, attend_bytes(l.cus), kSlotAttend, ws);
   if (rc != SPARSELNR_OK) return rc;
-  a.meta = (int32_t *)ws;
-  a.part = (float *)((char *)ws + records_bytes(slots));
+  a.meta = (int32_t *)ws->ptr;
+  a.part = (float *)((char *)ws->ptr + records_bytes(slots));
   return SPARSELNR_OK;
 }
 
@@ -85,7 +84,8 @@ int run_few(const Launch &l, AttendArgs a, int most_rows) {
   if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
   static_assert(kFewRows * (DP + 2) <= kFewValues && kFewPerCuSparse <= kFewPerCu, "fits the workspace");
   const int64_t slots = few_slots(a.target);
-  int rc = partials(l, slots, a);
+  HeldWorkspace ws;
+  int rc = partials(l, slots, a, &ws);
   if (rc != SPARSELNR_OK) return rc;
   const int64_t most = (int64_t)l.cus * 8;
   const unsigned grid = (unsigned)(pieces < most ? pieces : most);
@@ -103,7 +103,8 @@ int run_many(const Launch &l, AttendArgs a) {
   static_assert(ROWS * (DP + 2) <= kManyValues, "fits the workspace");
   const int64_t pieces = tiles + many_caps(a.target);
   if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
-  int rc = partials(l, many_slots(a.target), a);
+  HeldWorkspace ws;
+  int rc = partials(l, many_slots(a.target), a, &ws);
   if (rc != SPARSELNR_OK) return rc;
   rc = launch(attend_many<T, DP, NW, ONE_PAGE>, dim3((unsigned)pieces), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
   if (rc != SPARSELNR_OK) return rc;
@@ -150,10 +151,10 @@ int run_pages(const Launch &l, const AttendArgs &a) {
                tile_begin = take((size_t)p.buckets * 4), total = take(4), rank = take((size_t)picks * 4),
                list = take((size_t)picks * 4), tile = take((size_t)tiles * 4),
                part = take((size_t)rows * DP * 4), ml = take((size_t)rows * 8);
-  void *ws = nullptr;
-  int rc = stream_workspace(l.dev, l.stream, size, &ws, kSlotPages);
+  HeldWorkspace ws;
+  int rc = hold_workspace(l.dev, l.stream, size, kSlotPages, &ws);
   if (rc != SPARSELNR_OK) return rc;
-  auto at = [&](size_t offset) { return (int32_t *)((char *)ws + offset); };
+  auto at = [&](size_t offset) { return (int32_t *)((char *)ws.ptr + offset); };
   p.count = at(count), p.begin = at(begin), p.tile_begin = at(tile_begin), p.total = at(total), p.rank = at(rank);
   p.list = at(list), p.tile = at(tile), p.part = (float *)at(part), p.ml = (float *)at(ml);
   auto done = [&]() {

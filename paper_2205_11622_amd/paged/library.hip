@@ -11,8 +11,24 @@ namespace slnr {
 int hip_error(hipError_t e) { return hip_fail(e); }
 int this_device(int *dev) { return current_device(dev); }
 int device_cu_count(int dev, int *cus) { return device_cus(dev, cus); }
-int stream_workspace(int dev, hipStream_t stream, size_t bytes, void **out, int slot) {
-  return get_workspace(dev, stream, bytes, out, slot);
+
+int hold_workspace(int dev, hipStream_t stream, size_t bytes, int slot, HeldWorkspace *out) {
+  try {
+    for (;;) {
+      void *p = nullptr;
+      const int rc = get_workspace(dev, stream, bytes, &p, slot);
+      if (rc != SPARSELNR_OK) return rc;
+      // get_workspace has let go of the lock: another thread may have grown or released it since
+      std::unique_lock<std::mutex> lock(g_mu);
+      const auto it = g_workspace.find(WsKey{dev, (uintptr_t)stream, slot});
+      if (it == g_workspace.end() || it->second.ptr != p || it->second.bytes < bytes) continue;
+      out->lock = std::move(lock);
+      out->ptr = p;
+      return SPARSELNR_OK;
+    }
+  } catch (...) {  // no memory for a record of it
+    return SPARSELNR_ERR_NO_MEMORY;
+  }
 }
 
 }  // namespace slnr

@@ -47,3 +47,31 @@ def test_a_captured_step_outlives_larger_calls_on_its_stream(gpu, sparse):
             assert torch.equal(out.view(torch.int16), want.view(torch.int16)), i
     ref = pu.attention(x[2].cpu(), b.kc, b.vc, b.table, b.seq, b.qptr, 128 ** -0.5, sel=sel.tolist() if sparse else None)
     pu.check(out.cpu(), None, ref, torch.bfloat16, max(b.seq), 128, float(b.vc.float().nan_to_num(0.0).abs().max()))
+
+
+def test_two_host_threads_on_one_stream(gpu):
+    """Each thread's calls give what they give alone."""
+    import threading
+    batches = [pu.Batch([5000, 900], [1, 3], 8, 2, 128, 64, torch.bfloat16, seed=73 + i) for i in range(2)]
+    ups = [b.upload(gpu) for b in batches]
+    sel = torch.arange(64, dtype=torch.int32, device=gpu).expand(4, 2, 64).contiguous()
+    calls = [lambda u: slnr.sparselnr_paged_attention(*u), lambda u: slnr.sparselnr_block_attention(*u, sel)]
+    want = [[call(u) for call in calls] for u in ups]
+    torch.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        for _ in range(40):
+            got[i].append([call(ups[i]) for call in calls])
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert len(got[i]) == 40
+        for outs in got[i]:
+            for x, y in zip(outs, want[i]):
+                assert torch.equal(x.view(torch.int16), y.view(torch.int16))

@@ -46,3 +46,51 @@ def test_a_streams_attention_workspace_is_allocated_once(tmp_path):
             assert freed <= 1  # of its own
         else:
             assert allocated == [] and freed == 0, what
+
+
+# ------------------------------------------------------------- host threads
+
+
+def thread_scenario(rec):
+    """Two threads call on one stream, every launch waiting for the other thread's next one."""
+    import threading
+    out = []
+    for kind in ("decode", "chunk", "selection", "by pages"):
+        call = {"decode": lambda: rec.attend(4), "chunk": lambda: rec.attend(600), "selection": lambda: rec.sparse(4, 16),
+                "by pages": lambda: rec.sparse(2000, 16)}[kind]
+        call()  # workspaces
+        rec.events()
+        rec.wait(150)
+        threads = [threading.Thread(target=call) for _ in range(2)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        rec.wait(0)
+        out.append([kind, [[e.thread, e.name] for e in rec.events() if e.kind == hr.LAUNCH]])
+    # a larger call by pages and one that is under way
+    rec.wait(150)
+    threads = [threading.Thread(target=lambda n=n: rec.sparse(n, 32)) for n in (2000, 4000)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    rec.wait(0)
+    out.append(["growth", [[e.thread, e.name or "malloc"] for e in rec.events()]])
+    return out
+
+
+def test_calls_of_two_threads_on_one_stream_do_not_mix(tmp_path):
+    """A call's launches share partial results in the stream's workspace: the other thread's come before
+    or after all of them, and so does an allocation that frees the workspace."""
+    for kind, events in hr.run(thread_scenario, tmp_path):
+        who = [t for t, _ in events]
+        runs = 1 + sum(a != b for a, b in zip(who, who[1:]))
+        names = [n for _, n in events]
+        assert len(set(who)) == 2, kind
+        if kind in ("decode", "chunk", "selection"):  # a walk and its join at a time
+            assert len(names) % 2 == 0
+            for i in range(0, len(names), 2):
+                assert who[i] == who[i + 1] and "attend" in names[i] and "join" in names[i + 1], (kind, names)
+        else:
+            assert runs == 2, (kind, names)
