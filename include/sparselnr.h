@@ -288,10 +288,9 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *     units): a stream's first call allocates it, later ones and captured graphs find it.
  *     sparselnr_block_attention of many tokens (four and more per page of
  *     the table, on average) goes by pages and has a workspace of its own: its partial
- *     results, at most 144 MB (or those of one token and KV head, if they are more), and
- *     lists, which grow with T, R, W, top and the heads.  A capture of such a call
- *     needs one before, and while the graph may be replayed no call by pages on that
- *     stream may be larger.
+ *     results, at most 144 MB, and lists, which grow with T, R, W, top and the heads.
+ *     A capture of such a call needs one before, and while the graph may be
+ *     replayed no call by pages on that stream may be larger.
  * ---------------------------------------------------------------------- */
 
 enum sparselnr_dtype { SPARSELNR_BF16 = 0, SPARSELNR_FP16 = 1, SPARSELNR_FP32 = 2 };

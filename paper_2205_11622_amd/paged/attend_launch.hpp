@@ -120,11 +120,15 @@ constexpr int64_t kPagesWorkspace = (int64_t)144 << 20;
 // more on average, its keys are at least four times the heads of a group (the results
 // of a page are then at most half of what is gathered by queries), and 256 MB and more are
 // gathered, which take longer than the four small launches before and the join.
-inline bool by_pages(const AttendArgs &a, int64_t bytes) {
+// Not where one token's entries pass the lists' numbers, or its partial results of one KV head (`dp` columns)
+// what is kept of them.
+inline bool by_pages(const AttendArgs &a, int64_t bytes, int64_t dp) {
   const int64_t picks = (int64_t)a.T * a.top;
   return a.W > 0 && picks >= 4 * (int64_t)a.R * a.W && ((int64_t)1 << a.shift) >= 4 * (int64_t)a.G &&
-         ((picks * a.Hkv) << a.shift) * a.D * 2 * bytes >= (int64_t)256 << 20 &&
-         (int64_t)a.R * a.W * a.Hkv < ((int64_t)1 << 30) && a.G <= kPagesRows;
+         (double)picks * a.Hkv * (1 << a.shift) * a.D * 2 * bytes >= (double)((int64_t)256 << 20) &&
+         (int64_t)a.R * a.W * a.Hkv < ((int64_t)1 << 30) && a.G <= kPagesRows &&
+         (int64_t)a.Hkv * a.top < ((int64_t)1 << 30) &&
+         (int64_t)a.top * a.G * (dp + 2) * (int64_t)sizeof(float) <= kPagesWorkspace;
 }
 
 template <class T, int DP>
@@ -133,10 +137,10 @@ int run_pages(const Launch &l, const AttendArgs &a) {
   const int64_t per_token = (int64_t)a.Hkv * a.top;  // selected pages
   const int64_t bytes = (int64_t)a.top * a.G * (DP + 2) * sizeof(float);  // partial results of a token, per KV head
   int64_t most = kPagesWorkspace / bytes;
-  most = most < 1 ? 1 : most > a.T ? a.T : most;
+  most = most > a.T ? a.T : most;
   if (most * per_token >= ((int64_t)1 << 30)) most = (((int64_t)1 << 30) - 1) / per_token;
   int64_t heads = kPagesWorkspace / (most * bytes);  // of a launch
-  heads = heads < 1 ? 1 : heads > a.Hkv ? a.Hkv : heads;
+  heads = heads > a.Hkv ? a.Hkv : heads;
   const int64_t rows = most * heads * a.top * a.G;  // of partial results
   p.buckets = a.Hkv * a.R * a.W;
   p.per_tile = kPagesRows / a.G;
@@ -189,7 +193,7 @@ int run_pages(const Launch &l, const AttendArgs &a) {
 template <class T, int DP>
 int run_attend(const Launch &l, AttendArgs a, int64_t max_new) {
   if (a.sel) {
-    if (by_pages(a, sizeof(T))) return run_pages<T, DP>(l, a);
+    if (by_pages(a, sizeof(T), DP)) return run_pages<T, DP>(l, a);
     return run_few<T, DP, true>(l, a, a.G < kFewRows ? a.G : kFewRows);
   }
   // rows of the longest request, as far as the host knows

@@ -94,3 +94,20 @@ def test_calls_of_two_threads_on_one_stream_do_not_mix(tmp_path):
                 assert who[i] == who[i + 1] and "attend" in names[i] and "join" in names[i + 1], (kind, names)
         else:
             assert runs == 2, (kind, names)
+
+
+# ------------------------------------------------------------- limits
+
+
+def huge_selection_scenario(rec):
+    """Selections of so many pages a token that one token's entries pass 2^30."""
+    out = []
+    for top, heads in ((1 << 26, 16), (1 << 26, 64), ((1 << 27) - 1, 8), (1 << 26, 15)):
+        c = dict(page_size=4, heads=heads, dim=64)
+        out.append(rec.sparse(2, top, Hq=heads, requests=rec.requests(2, 1, 1 << 24), **c))
+    return out
+
+
+def test_selections_past_the_lists_do_not_divide_by_nothing(tmp_path):
+    """They go by queries, whose walk has no lists."""
+    assert hr.run(huge_selection_scenario, tmp_path) == [0, 0, 0, 0]
