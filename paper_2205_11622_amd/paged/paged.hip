@@ -163,7 +163,10 @@ int run_select(const Launch &l, SelectArgs a, int64_t Hkv) {
   // pages of the longest request, and the carried entries in front, if they fit
   const int64_t pages = ((int64_t)a.W + 15) / 16 * 16;
   const int64_t want = (pages < 2 * kWave ? 2 * kWave : pages) + a.top;
-  a.capacity = (int32_t)(want < most ? want : most);
+  // A multiple of four words: so is then the row's stride, and what lies behind the rows, the 8-bit
+  // queries among it, begins at a multiple of the 16 bytes that it is read in.
+  static_assert(most % 4 == 0, "a full row keeps the alignment");
+  a.capacity = (int32_t)(want < most ? (want + 3) / 4 * 4 : most);
   const size_t lds = (size_t)TM * (a.capacity + 4) * 4 + ((size_t)TM * a.top + 3) / 4 * 16 + 16 * (DP + 16) +
                      2 * kSelectWaves * 4 + (TM == 1 ? kSelectWaves * 4 * kWave * 4 : 0);
   const int64_t tiles = TM == 1 ? (int64_t)a.T : (int64_t)a.T / TM + a.R;

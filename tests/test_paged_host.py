@@ -111,3 +111,26 @@ def huge_selection_scenario(rec):
 def test_selections_past_the_lists_do_not_divide_by_nothing(tmp_path):
     """They go by queries, whose walk has no lists."""
     assert hr.run(huge_selection_scenario, tmp_path) == [0, 0, 0, 0]
+
+
+def select_shapes_scenario(rec):
+    out = []
+    for T in (1, 3, 700):
+        for W in (1, 20, 100, 511, 5000):
+            for top in (1, 2, 3, 4, 5, 6, 7, 64, 101, 254, 255, 256):
+                for dim in (8, 72, 256):
+                    def call():
+                        rc = rec.lib.sparselnr_block_select(1 << 37, 8 * dim, dim, 8, 0, 1 << 32, 1 << 33, 1 << 20, 16, 2, dim,
+                                                            rec.requests(T, 1, W), top, 0, 1, 1 << 38, 1)
+                        assert rc == 0
+                    e, = rec.events(call)
+                    assert "block_select" in e.name
+                    out.append([T, W, top, dim, e.lds])
+    return out
+
+
+def test_selection_lays_its_lds_out_in_16_bytes(tmp_path):
+    """Its parts (keys, indices, 8-bit queries, which are read 16 bytes at a time, counts) follow one another, and the
+    last ones are multiples of 16 bytes: so is the whole, if the queries begin at one."""
+    for T, W, top, dim, lds in hr.run(select_shapes_scenario, tmp_path):
+        assert lds % 16 == 0 and lds <= 160 * 1024, (T, W, top, dim, lds)
