@@ -276,11 +276,12 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *     rows hold (NaN and infinities included).  NaN in what it sees gives NaN.
  *   - dim: a multiple of 8 up to 256.  page_size: a power of two up to
  *     SPARSELNR_MAX_PAGE.  Row, page and head strides are in values, may be any
- *     that keep each row of dim values at a multiple of 16 bytes (so a slice of a
- *     fused q/k/v projection and caches of either order of slots and heads
- *     will do); the dim values of a row are adjacent.  Anything else is
- *     SPARSELNR_ERR_UNSUPPORTED.  R < 2^24, T < 2^28, T * Hq < 2^31,
- *     W * page_size <= 2^31 - 4096; a seq_len past that of its table's row ends there.
+ *     that keep each row of dim values at a multiple of 16 bytes (the stride of an
+ *     extent of one does not count; so a slice of a fused q/k/v projection and caches
+ *     of either order of slots and heads will do); the dim values of a row are
+ *     adjacent.  Anything else is SPARSELNR_ERR_UNSUPPORTED.  R < 2^24, T < 2^28,
+ *     T * Hq < 2^31, W * page_size <= 2^31 - 4096; a seq_len past that of its table's
+ *     row ends there.
  *   - R = 0 or T = 0 is a no-op.
  *   - The two attention calls use a workspace per (device, stream) for the results of
  *     contexts that are cut into pieces.  It has one size for all of them, whatever

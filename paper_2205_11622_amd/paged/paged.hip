@@ -43,6 +43,9 @@ bool strides16(int bytes, int64_t a, int64_t b, int64_t c = 0) {
   return a * bytes % 16 == 0 && b * bytes % 16 == 0 && c * bytes % 16 == 0;
 }
 
+// An extent of one has no next row: its stride, which may be anything, counts as 0.
+int64_t stride_of(int64_t stride, int64_t extent) { return extent > 1 ? stride : 0; }
+
 int check_dim(int64_t dim) {
   if (dim < 0) return SPARSELNR_ERR_INVALID_ARG;
   return dim >= 8 && dim <= kMaxDim && dim % 8 == 0 ? SPARSELNR_OK : SPARSELNR_ERR_UNSUPPORTED;
@@ -53,7 +56,8 @@ int check_heads(int64_t Hq, int64_t Hkv) {
   return Hq <= 65535 ? SPARSELNR_OK : SPARSELNR_ERR_UNSUPPORTED;
 }
 
-int check_cache(const sparselnr_kv_cache *c) {
+// `out` is the cache with strides that count.
+int check_cache(const sparselnr_kv_cache *c, sparselnr_kv_cache *out) {
   if (!c || c->pages < 0 || c->heads < 1) return SPARSELNR_ERR_INVALID_ARG;
   const int e = value_bytes(c->dtype);
   if (!e) return SPARSELNR_ERR_INVALID_ARG;
@@ -63,8 +67,12 @@ int check_cache(const sparselnr_kv_cache *c) {
   const int rc = check_dim(c->dim);
   if (rc != SPARSELNR_OK) return rc;
   if (page_shift(c->page_size) < 0 || c->pages > kMax31 || c->heads > 65535) return SPARSELNR_ERR_UNSUPPORTED;
-  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !strides16(e, c->k_page, c->k_slot, c->k_head) ||
-      !strides16(e, c->v_page, c->v_slot, c->v_head))
+  *out = *c;
+  out->k_page = stride_of(c->k_page, c->pages), out->v_page = stride_of(c->v_page, c->pages);
+  out->k_slot = stride_of(c->k_slot, c->page_size), out->v_slot = stride_of(c->v_slot, c->page_size);
+  out->k_head = stride_of(c->k_head, c->heads), out->v_head = stride_of(c->v_head, c->heads);
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !strides16(e, out->k_page, out->k_slot, out->k_head) ||
+      !strides16(e, out->v_page, out->v_slot, out->v_head))
     return SPARSELNR_ERR_UNSUPPORTED;
   return SPARSELNR_OK;
 }
@@ -92,11 +100,13 @@ int launched() {
 }
 
 // Common part of the two attention calls.
-int attend(const void *q, int64_t q_token, int64_t q_head, int64_t Hq, const sparselnr_kv_cache *c,
+int attend(const void *q, int64_t q_token, int64_t q_head, int64_t Hq, const sparselnr_kv_cache *cache,
            const sparselnr_requests *r, const int32_t *sel, int64_t top, double scale, int64_t window, int64_t max_new,
            void *out, float *lse, void *stream) {
-  int rc = check_cache(c);
+  sparselnr_kv_cache kv;
+  int rc = check_cache(cache, &kv);
   if (rc != SPARSELNR_OK) return rc;
+  const sparselnr_kv_cache *c = &kv;
   if ((rc = check_requests(r, c->page_size)) != SPARSELNR_OK) return rc;
   if ((rc = check_heads(Hq, c->heads)) != SPARSELNR_OK) return rc;
   if (q_token < 0 || q_head < 0 || window < 0 || max_new < 0 || !(scale > 0) || !std::isfinite(scale))
@@ -105,6 +115,7 @@ int attend(const void *q, int64_t q_token, int64_t q_head, int64_t Hq, const spa
   if (!(scale2 > 0) || !std::isfinite(scale2)) return SPARSELNR_ERR_INVALID_ARG;
   if (r->T > 0 && r->R > 0 && (!q || !out)) return SPARSELNR_ERR_INVALID_ARG;
   const int e = value_bytes(c->dtype);
+  q_token = stride_of(q_token, r->T), q_head = stride_of(q_head, Hq);
   if (!aligned(q, 16) || !aligned(out, 16) || !strides16(e, q_token, q_head)) return SPARSELNR_ERR_UNSUPPORTED;
   if (r->T * Hq > kMax31) return SPARSELNR_ERR_UNSUPPORTED;
   if (r->T == 0 || r->R == 0) return SPARSELNR_OK;
@@ -233,30 +244,33 @@ int sparselnr_page_tables(const int32_t *ctx_len, const int32_t *new_len, int32_
 int sparselnr_cache_append(const void *k, int64_t k_token, int64_t k_head, const void *v, int64_t v_token,
                            int64_t v_head, const int64_t *slots, const sparselnr_kv_cache *cache, int8_t *kq,
                            float *kscale, int64_t T, void *stream) {
-  int rc = check_cache(cache);
+  sparselnr_kv_cache kv;
+  int rc = check_cache(cache, &kv);
   if (rc != SPARSELNR_OK) return rc;
   if (T < 0 || k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0) return SPARSELNR_ERR_INVALID_ARG;
   if (T > 0 && (!k || !v || !slots)) return SPARSELNR_ERR_INVALID_ARG;
   if ((kq == nullptr) != (kscale == nullptr)) return SPARSELNR_ERR_INVALID_ARG;
-  const int e = value_bytes(cache->dtype);
+  const int e = value_bytes(kv.dtype);
+  k_token = stride_of(k_token, T), v_token = stride_of(v_token, T);
+  k_head = stride_of(k_head, kv.heads), v_head = stride_of(v_head, kv.heads);
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(kq, 8) || !strides16(e, k_token, k_head) ||
       !strides16(e, v_token, v_head))
     return SPARSELNR_ERR_UNSUPPORTED;
   if (T > kMax31) return SPARSELNR_ERR_UNSUPPORTED;
-  if (T == 0 || cache->pages == 0) return SPARSELNR_OK;
+  if (T == 0 || kv.pages == 0) return SPARSELNR_OK;
   AppendArgs a{};
   a.k = k, a.k_token = k_token, a.k_head_in = k_head;
   a.v = v, a.v_token = v_token, a.v_head_in = v_head;
   a.slots = slots;
-  a.kc = cache->k, a.vc = cache->v;
-  a.k_page = cache->k_page, a.k_slot = cache->k_slot, a.k_head = cache->k_head;
-  a.v_page = cache->v_page, a.v_slot = cache->v_slot, a.v_head = cache->v_head;
+  a.kc = kv.k, a.vc = kv.v;
+  a.k_page = kv.k_page, a.k_slot = kv.k_slot, a.k_head = kv.k_head;
+  a.v_page = kv.v_page, a.v_slot = kv.v_slot, a.v_head = kv.v_head;
   a.kq = kq, a.kscale = kscale;
-  a.T = (int32_t)T, a.pages = (int32_t)cache->pages, a.shift = page_shift(cache->page_size);
-  a.Hkv = (int32_t)cache->heads, a.D = (int32_t)cache->dim;
+  a.T = (int32_t)T, a.pages = (int32_t)kv.pages, a.shift = page_shift(kv.page_size);
+  a.Hkv = (int32_t)kv.heads, a.D = (int32_t)kv.dim;
   Launch l;
   if ((rc = current(&l, stream)) != SPARSELNR_OK) return rc;
-  switch (cache->dtype) {
+  switch (kv.dtype) {
     case SPARSELNR_BF16: return run_append<__bf16>(l, a);
     case SPARSELNR_FP16: return run_append<_Float16>(l, a);
     default: return run_append<float>(l, a);

@@ -689,3 +689,25 @@ def test_by_pages_in_several_launches(gpu, Hkv, T):
         assert ((out[t:t + 1].double().cpu() - one.double().cpu()).abs() <= 2 * tol).all(), t
         fine = want_lse[0] > -math.inf
         assert ((lse[t].double().cpu() - want_lse[0]).abs()[fine] <= 1e-5 + 1e-6 * want_lse[0].abs()[fine]).all()
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_strides_of_extents_of_one(gpu, new):
+    """One request of one page, KV head and (decode) token, with strides of 1 where there is no next."""
+    b = pu.Batch([20], [new], 4, 1, 64, 128, BF16, seed=80, spare=0)
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    odd_k, odd_v = (x.as_strided(x.shape, (1, x.stride(1), 3, 1), x.storage_offset()) for x in (kc, vc))
+    odd_q = q.as_strided(q.shape, (1, q.stride(1), 1), q.storage_offset()) if new == 1 else q
+    sel = torch.zeros(new, 1, 2, dtype=torch.int32, device=gpu)
+    sel[..., 1] = -1
+    for call, args in ((slnr.sparselnr_paged_attention, ()), (slnr.sparselnr_block_attention, (sel,))):
+        assert torch.equal(call(odd_q, odd_k, odd_v, table, seq, qptr, *args), call(q, kc, vc, table, seq, qptr, *args))
+    k = b.qkv[:, 4:5].to(gpu)
+    odd = k[:1].as_strided((1, 1, 64), (1, 5, 1), k.storage_offset())
+    slots = torch.tensor([127], device=gpu)
+    kq, ks = torch.zeros(1, 1, 64, dtype=torch.int8, device=gpu), torch.zeros(1, 1, device=gpu)
+    kc.nan_to_num_(0.0)
+    slnr.sparselnr_cache_append(odd, odd, slots, odd_k, odd_v, kq, ks)
+    assert torch.equal(kc[0, 127], k[0]) and torch.equal(vc[0, 127], k[0])
+    want_q, want_s = pu.summary(kc[0, :, 0].cpu().double())
+    assert torch.equal(kq[0, 0].cpu(), want_q) and float(ks[0, 0]) == want_s

@@ -170,3 +170,17 @@ def test_structs_have_the_layout_of_the_header(tmp_path):
     got = subprocess.check_output([exe], text=True).split("\n")
     for line, st in zip(got, (slnr._KvCache, slnr._Requests)):
         assert [int(x) for x in line.split()] == [getattr(st, f).offset for f, _ in st._fields_] + [ctypes.sizeof(st)]
+
+
+def test_strides_of_extents_of_one_do_not_count():
+    """One token, page, place or head has no next one: torch gives such a dimension any stride."""
+    one = dict(pages=1, k_page=1, v_page=3)
+    r = requests(T=0)
+    assert attend(cache(**one), r) == OK and attend(cache(**dict(one, pages=2))) == UNSUPPORTED
+    assert attend(cache(page_size=1, k_slot=1, v_slot=5), r) == OK
+    assert attend(cache(heads=1, k_head=1, v_head=7), r) == OK
+    assert attend(cache(page_size=1, k_slot=-1), r) == INVALID
+    assert attend(r=requests(T=1, R=0), qt=1) == OK and attend(r=requests(T=2, R=0), qt=1) == UNSUPPORTED
+    assert attend(cache(heads=1), requests(T=1, R=0), Hq=1, qh=1) == OK
+    assert append(cache(pages=0, heads=1), T=1, kt=1, kh=1) == OK  # no pages: nothing to do
+    assert append(cache(pages=0), T=2, kt=1) == UNSUPPORTED
