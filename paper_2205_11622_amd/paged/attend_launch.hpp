@@ -30,6 +30,9 @@ struct Launch {
   hipStream_t stream;
 };
 
+// A launch has fewer than 2^32 threads a dimension.
+constexpr int64_t grid_limit(int block) { return (((int64_t)1 << 32) - 1) / block; }
+
 template <class F>
 int launch(F *fn, dim3 grid, int block, size_t lds, const Launch &l, const AttendArgs &a) {
   hipLaunchKernelGGL(fn, grid, dim3(block), lds, l.stream, a);
@@ -75,13 +78,13 @@ inline int partials(const Launch &l, int64_t slots, AttendArgs &a, HeldWorkspace
 template <class T, int DP, bool SPARSE>
 int run_few(const Launch &l, AttendArgs a, int most_rows) {
   a.target = l.cus * (SPARSE ? kFewPerCuSparse : kFewPerCu);
-  int64_t tiles = SPARSE ? (int64_t)a.T * ((a.G + kFewRows - 1) / kFewRows) : (int64_t)a.T * a.G / kFewRows + a.R;
+  const int64_t requests = a.R < a.T ? a.R : a.T;  // that have tokens, at most
+  int64_t tiles = SPARSE ? (int64_t)a.T * ((a.G + kFewRows - 1) / kFewRows) : (int64_t)a.T * a.G / kFewRows + requests;
   // Beside attend_many: only what is left of a request has tiles here, often nothing, and
   // a grid for more costs its launch.
-  const int64_t left = (int64_t)a.R * ((kFewMostRows<T, DP> + kFewRows - 1) / kFewRows);
+  const int64_t left = requests * ((kFewMostRows<T, DP> + kFewRows - 1) / kFewRows);
   if (!SPARSE && a.few <= kFewMostRows<T, DP> && tiles > left) tiles = left;
   const int64_t pieces = tiles * a.Hkv + a.target;
-  if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
   static_assert(kFewRows * (DP + 2) <= kFewValues && kFewPerCuSparse <= kFewPerCu, "fits the workspace");
   const int64_t slots = few_slots(a.target);
   HeldWorkspace ws;
@@ -99,14 +102,13 @@ template <class T, int DP, int NW, bool ONE_PAGE>
 int run_many(const Launch &l, AttendArgs a) {
   constexpr int ROWS = 32 * NW;
   a.target = l.cus * kManyPerCu;
-  const int64_t tiles = ((int64_t)a.T * a.G / ROWS + a.R) * a.Hkv;
+  const int64_t tiles = ((int64_t)a.T * a.G / ROWS + (a.R < a.T ? a.R : a.T)) * a.Hkv;
   static_assert(ROWS * (DP + 2) <= kManyValues, "fits the workspace");
-  const int64_t pieces = tiles + many_caps(a.target);
-  if (pieces >= ((int64_t)1 << 31)) return SPARSELNR_ERR_UNSUPPORTED;
+  const int64_t pieces = tiles + many_caps(a.target), most = grid_limit(NW * kWave);
   HeldWorkspace ws;
   int rc = partials(l, many_slots(a.target), a, &ws);
   if (rc != SPARSELNR_OK) return rc;
-  rc = launch(attend_many<T, DP, NW, ONE_PAGE>, dim3((unsigned)pieces), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
+  rc = launch(attend_many<T, DP, NW, ONE_PAGE>, dim3((unsigned)(pieces < most ? pieces : most)), NW * kWave, sizeof(ManyShared<T, DP, NW>), l, a);
   if (rc != SPARSELNR_OK) return rc;
   return launch(join_many<T, DP, ROWS>, dim3((unsigned)l.cus, ROWS / kJoinRows), kJoinBlock, 0, l, a);
 }

@@ -159,6 +159,8 @@ template <class T>
 int run_append(const Launch &l, const AppendArgs &a) {
   int64_t per = a.T / (l.cus / 2 > 0 ? l.cus / 2 : 1);
   per = per < 1 ? 1 : per > 16 ? 16 : per;
+  const int64_t least = (a.T + grid_limit(kAppendBlock) - 1) / grid_limit(kAppendBlock);
+  per = per < least ? least : per;
   int64_t shares = 2 * (int64_t)l.cus / ((a.T + per - 1) / per);
   shares = shares < 1 ? 1 : shares > a.Hkv ? a.Hkv : shares;
   hipLaunchKernelGGL(cache_append<T>, dim3((unsigned)((a.T + per - 1) / per), (unsigned)shares), dim3(kAppendBlock), 0,
@@ -181,9 +183,15 @@ int run_select(const Launch &l, SelectArgs a, int64_t Hkv) {
   const size_t lds = (size_t)TM * (a.capacity + 4) * 4 + ((size_t)TM * a.top + 3) / 4 * 16 + 16 * (DP + 16) +
                      2 * kSelectWaves * 4 + (TM == 1 ? kSelectWaves * 4 * kWave * 4 : 0);
   const int64_t tiles = TM == 1 ? (int64_t)a.T : (int64_t)a.T / TM + a.R;
-  hipLaunchKernelGGL((block_select<T, DP, TM, NR>), dim3((unsigned)tiles, (unsigned)Hkv), dim3(kSelectBlock), lds,
-                     l.stream, a);
-  return launched();
+  const int64_t once = grid_limit(kSelectBlock);
+  for (int64_t first = 0; first < tiles; first += once) {  // one launch, but for millions of tiles
+    a.tile0 = (int32_t)first;
+    const unsigned n = (unsigned)(tiles - first < once ? tiles - first : once);
+    hipLaunchKernelGGL((block_select<T, DP, TM, NR>), dim3(n, (unsigned)Hkv), dim3(kSelectBlock), lds, l.stream, a);
+    const int rc = launched();
+    if (rc != SPARSELNR_OK) return rc;
+  }
+  return SPARSELNR_OK;
 }
 
 template <class T, int DP>
@@ -256,7 +264,7 @@ int sparselnr_cache_append(const void *k, int64_t k_token, int64_t k_head, const
   if (!aligned(k, 16) || !aligned(v, 16) || !aligned(kq, 8) || !strides16(e, k_token, k_head) ||
       !strides16(e, v_token, v_head))
     return SPARSELNR_ERR_UNSUPPORTED;
-  if (T > kMax31) return SPARSELNR_ERR_UNSUPPORTED;
+  if (T >= ((int64_t)1 << 28)) return SPARSELNR_ERR_UNSUPPORTED;
   if (T == 0 || kv.pages == 0) return SPARSELNR_OK;
   AppendArgs a{};
   a.k = k, a.k_token = k_token, a.k_head_in = k_head;

@@ -16,6 +16,7 @@ struct SelectArgs {
   const int32_t *seq, *qptr;
   int32_t *sel;  // [T][Hkv][top]
   int32_t R, T, W, pages, shift, Hkv, G, D, top, first, local;
+  int32_t tile0;     // number of the launch's first tile
   int32_t capacity;  // entries of a row in LDS: top carried ones, then a segment of pages
 };
 
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(kSelectBlock, TM > 1 && NR <= 16 && DP <= 128 ? 8 :
   // ------------------------------------------------------ which tokens
   // TM = 16: request r's tiles begin at number floor(qptr[r] / 16) + r, which leaves
   // room for all of them and never runs back.  TM = 1: token by token.
-  const int id = blockIdx.x;
+  const int id = a.tile0 + (int)blockIdx.x;
   auto start = [&](int r) {
     int b = a.qptr[r];
     b = b < 0 ? 0 : b > a.T ? a.T : b;

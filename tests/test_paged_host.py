@@ -134,3 +134,42 @@ def test_selection_lays_its_lds_out_in_16_bytes(tmp_path):
     last ones are multiples of 16 bytes: so is the whole, if the queries begin at one."""
     for T, W, top, dim, lds in hr.run(select_shapes_scenario, tmp_path):
         assert lds % 16 == 0 and lds <= 160 * 1024, (T, W, top, dim, lds)
+
+
+def huge_batches_scenario(rec):
+    """The largest numbers of requests and tokens that the interface admits."""
+    out = []
+
+    def look(what, call):
+        rc = []
+        events = rec.events(lambda: rc.append(call()))
+        out.append([what, rc[0], [[e.name, list(e.grid), list(e.block)] for e in events if e.kind == hr.LAUNCH]])
+
+    R, T = (1 << 24) - 1, (1 << 28) - 1
+    for heads, Hq in ((1, 1), (4, 4), (2, 6), (8, 8), (128, 128)):
+        T = min((1 << 28) - 1, ((1 << 31) - 1) // Hq)
+        c = dict(heads=heads, dim=64)
+        look("attend", lambda: rec.attend(T, Hq=Hq, requests=rec.requests(T, R, 4), **c))
+        look("sparse", lambda: rec.sparse(T, 2, Hq=Hq, requests=rec.requests(T, R, 4), **c))
+        look("sparse", lambda: rec.sparse(T, 4, Hq=Hq, requests=rec.requests(T, 3, 4), **c))
+        for r in (R, 16, 1 << 23):
+            look("select", lambda: rec.lib.sparselnr_block_select(1 << 37, 64 * Hq, 64, Hq, 0, 1 << 32, 1 << 33, 1 << 20, 16, heads, 64,
+                                                                  rec.requests(T, r, 4), 2, 1, 1, 1 << 38, 1))
+    T = (1 << 28) - 1
+    k = rec.cache(heads=2, dim=64)
+    look("append", lambda: rec.lib.sparselnr_cache_append(1 << 32, 128, 64, 1 << 33, 128, 64, 1 << 34, k, 1 << 35, 1 << 36, T, 1))
+    look("append too many", lambda: rec.lib.sparselnr_cache_append(1 << 32, 128, 64, 1 << 33, 128, 64, 1 << 34, k, 1 << 35, 1 << 36,
+                                                                   T + 1, 1))
+    look("tables", lambda: rec.lib.sparselnr_page_tables(1 << 32, 1 << 33, 1 << 34, 4, 1 << 35, 1 << 36, 1 << 37, 1 << 38, 1 << 39, R, 4,
+                                                         1 << 30, T, 16, 1))
+    return out
+
+
+def test_launches_of_the_largest_batches_fit(tmp_path):
+    """A launch has fewer than 2^32 threads a dimension, whatever sizes are admitted."""
+    for what, rc, launches in hr.run(huge_batches_scenario, tmp_path):
+        assert rc == (2 if what == "append too many" else 0), what
+        assert bool(launches) == (rc == 0)
+        for name, grid, block in launches:
+            for g, b in zip(grid, block):
+                assert 0 < g * b < 1 << 32, (what, name, grid, block)
