@@ -33,7 +33,8 @@
  *     never frees or retains them.  The base pointers must be 4-byte aligned;
  *     16-byte alignment of all of them enables the kernels of fixed width.
  *   - Calls are asynchronous on `stream` (a hipStream_t; NULL is the null
- *     stream).  No call synchronises with the host.
+ *     stream).  No call synchronises with the host.  The arrays and the stream are
+ *     of the calling thread's current device.
  *   - Columns within a row may be unsorted and may repeat (repeats add).
  *     Preconditions on the CSR arrays are not checked on the device; use
  *     sparselnr_validate_csr in tests.  nnz and N + nnz must be < 2^31.

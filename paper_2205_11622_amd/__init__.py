@@ -204,6 +204,21 @@ def _stream(stream, device):
     return getattr(stream, "cuda_stream", stream)
 
 
+_get_device = None
+
+
+def _on(index, entry, *args):
+    """entry(*args) with GPU `index` current: the library launches and allocates there."""
+    global _get_device
+    if _get_device is None:
+        torch = _torch()
+        _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    if _get_device() == index:
+        return entry(*args)
+    with _torch().cuda.device(index):
+        return entry(*args)
+
+
 def _csr(rowptr, colidx, vals, vals_name="vals"):
     torch = _torch()
     device = rowptr.device
@@ -243,9 +258,9 @@ def sparselnr_fused_sddmm_spmm(rowptr, colidx, vals, C, D, E, A=None, stream=Non
         A = torch.empty((N, L), dtype=torch.float32, device=device)
     elif _dense(A, "A", N, device) != L:
         raise ValueError("A must be N x L")
-    rc = lib().sparselnr_fused_sddmm_spmm(
-        _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device),
-        _ptr(D, device), _ptr(E, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_fused_sddmm_spmm,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
+             _ptr(E, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_fused_sddmm_spmm")
     return A
@@ -264,9 +279,9 @@ def sparselnr_fused_sddmm_spmm_noalloc(rowptr, colidx, vals, C, D, E, A, stream=
     L = _dense(E, "E", M, device)
     if A is None or _dense(A, "A", N, device) != L:
         raise ValueError("A must be given, N x L")
-    rc = lib().sparselnr_fused_sddmm_spmm_noalloc(
-        _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device),
-        _ptr(D, device), _ptr(E, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_fused_sddmm_spmm_noalloc,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
+             _ptr(E, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_fused_sddmm_spmm_noalloc")
     return A
@@ -286,9 +301,9 @@ def sparselnr_sddmm(rowptr, colidx, vals, C, D, Y=None, stream=None):
         _check(Y, "Y", torch.float32, device, 1)
         if Y.numel() != colidx.numel():
             raise ValueError("Y must have nnz entries")
-    rc = lib().sparselnr_sddmm(_ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device),
-                               _ptr(C, device), _ptr(D, device), _ptr(Y, device), N, M, K,
-                               _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_sddmm,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
+             _ptr(Y, device), N, M, K, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_sddmm")
     return Y
@@ -304,8 +319,9 @@ def sparselnr_spmm(rowptr, colidx, Y, E, A=None, stream=None):
         A = torch.empty((N, L), dtype=torch.float32, device=device)
     elif _dense(A, "A", N, device) != L:
         raise ValueError("A must be N x L")
-    rc = lib().sparselnr_spmm(_ptr(rowptr, device), _ptr(colidx, device), _ptr(Y, device),
-                              _ptr(E, device), _ptr(A, device), N, M, L, _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_spmm,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(Y, device), _ptr(E, device), _ptr(A, device), N, M, L,
+             _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_spmm")
     return A
@@ -330,10 +346,9 @@ def sparselnr_unfused_sddmm_spmm(rowptr, colidx, vals, C, D, E, Y=None, A=None, 
         A = torch.empty((N, L), dtype=torch.float32, device=device)
     elif _dense(A, "A", N, device) != L:
         raise ValueError("A must be N x L")
-    rc = lib().sparselnr_unfused_sddmm_spmm(
-        _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device),
-        _ptr(D, device), _ptr(E, device), _ptr(Y, device), _ptr(A, device), N, M, K, L,
-        _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_unfused_sddmm_spmm,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
+             _ptr(E, device), _ptr(Y, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_unfused_sddmm_spmm")
     return Y, A
@@ -360,10 +375,9 @@ def sparselnr_fused_sddmm_spmm_gemm(rowptr, colidx, vals, C, D, F, W, A=None, st
     L = _dense(F, "F", M, device)
     Mo = _dense(W, "W", L, device)
     A = _out(A, N, Mo, device)
-    rc = lib().sparselnr_fused_sddmm_spmm_gemm(
-        _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device),
-        _ptr(D, device), _ptr(F, device), _ptr(W, device), _ptr(A, device), N, M, K, L, Mo,
-        _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_fused_sddmm_spmm_gemm,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
+             _ptr(F, device), _ptr(W, device), _ptr(A, device), N, M, K, L, Mo, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_fused_sddmm_spmm_gemm")
     return A
@@ -377,9 +391,9 @@ def sparselnr_spmm_gemm(rowptr, colidx, vals, C, D, A=None, stream=None):
     K = _dense(C, "C", M, device)
     L = _dense(D, "D", K, device)
     A = _out(A, N, L, device)
-    rc = lib().sparselnr_spmm_gemm(_ptr(rowptr, device), _ptr(colidx, device),
-                                   _ptr(vals, device), _ptr(C, device), _ptr(D, device),
-                                   _ptr(A, device), N, M, K, L, _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_spmm_gemm,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
+             _ptr(A, device), N, M, K, L, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_spmm_gemm")
     return A
@@ -395,10 +409,9 @@ def sparselnr_spmmh_gemm(rowptr, colidx, vals, C, D, E, A=None, stream=None):
         raise ValueError("C and D must have the same shape")
     L = _dense(E, "E", J, device)
     A = _out(A, N, L, device)
-    rc = lib().sparselnr_spmmh_gemm(_ptr(rowptr, device), _ptr(colidx, device),
-                                    _ptr(vals, device), _ptr(C, device), _ptr(D, device),
-                                    _ptr(E, device), _ptr(A, device), N, M, J, L,
-                                    _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_spmmh_gemm,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
+             _ptr(E, device), _ptr(A, device), N, M, J, L, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_spmmh_gemm")
     return A
@@ -414,9 +427,9 @@ def sparselnr_fused_sddmm_spmm_dt(rowptr, colidx, vals, C, Dt, E, A=None, stream
         raise ValueError("Dt must be K x M")
     L = _dense(E, "E", M, device)
     A = _out(A, N, L, device)
-    rc = lib().sparselnr_fused_sddmm_spmm_dt(
-        _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device),
-        _ptr(Dt, device), _ptr(E, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_fused_sddmm_spmm_dt,
+             _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(Dt, device),
+             _ptr(E, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_fused_sddmm_spmm_dt")
     return A
@@ -430,9 +443,9 @@ def sparselnr_validate_csr(rowptr, colidx, M, stream=None) -> int:
     _check(rowptr, "rowptr", torch.int32, device, 1)
     _check(colidx, "colidx", torch.int32, device, 1)
     nnz = ctypes.c_int64(-1)
-    rc = lib().sparselnr_validate_csr(_ptr(rowptr, device), _ptr(colidx, device),
-                                      rowptr.numel() - 1, M, colidx.numel(), ctypes.byref(nnz),
-                                      _stream(stream, device))
+    rc = _on(device.index, lib().sparselnr_validate_csr,
+             _ptr(rowptr, device), _ptr(colidx, device), rowptr.numel() - 1, M, colidx.numel(), ctypes.byref(nnz),
+             _stream(stream, device))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_validate_csr")
     return int(nnz.value)
@@ -565,10 +578,10 @@ def sparselnr_page_tables(ctx_len, new_len, table, free_pages, tokens, page_size
     seq_len = torch.empty(R, dtype=int32, device=device) if seq_len is None else seq_len
     counts = torch.empty(3, dtype=int32, device=device) if counts is None else counts
     slots = torch.empty(tokens, dtype=torch.int64, device=device) if slots is None else slots
-    rc = lib().sparselnr_page_tables(
-        *args, _packed(qptr, "qptr", int32, index, (R + 1,)), _packed(seq_len, "seq_len", int32, index, (R,)),
-        _packed(slots, "slots", torch.int64, index, (tokens,)), _packed(counts, "counts", int32, index, (3,)), R, W, F,
-        tokens, page_size, _launch_stream(stream, index))
+    rc = _on(index, lib().sparselnr_page_tables,
+             *args, _packed(qptr, "qptr", int32, index, (R + 1,)), _packed(seq_len, "seq_len", int32, index, (R,)),
+             _packed(slots, "slots", torch.int64, index, (tokens,)), _packed(counts, "counts", int32, index, (3,)),
+             R, W, F, tokens, page_size, _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_page_tables")
     return qptr, seq_len, slots, counts
@@ -591,9 +604,10 @@ def sparselnr_cache_append(k, v, slots, kcache, vcache, kq=None, kscale=None, st
     if kq is not None:
         kq_at = _packed(kq, "kq", torch.int8, index, (shape[0], shape[2], shape[3]))
         ks_at = _packed(kscale, "kscale", torch.float32, index, (shape[0], shape[2]))
-    rc = lib().sparselnr_cache_append(k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
-                                      _packed(slots, "slots", torch.int64, index, (T,)), cache, kq_at, ks_at, T,
-                                      _launch_stream(stream, index))
+    rc = _on(index, lib().sparselnr_cache_append,
+             k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+             _packed(slots, "slots", torch.int64, index, (T,)), cache, kq_at, ks_at, T,
+             _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_cache_append")
 
@@ -625,8 +639,8 @@ def sparselnr_paged_attention(q, kcache, vcache, table, seq_len, qptr, scale=Non
     how far back a token sees; max_new > 0 says that no request has more new
     tokens.  lse (float32 T x Hq), if given, is filled.  Returns out (T x Hq x D)."""
     index, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse)
-    rc = lib().sparselnr_paged_attention(*head, scale, window, max_new, out.data_ptr(), lse,
-                                         _launch_stream(stream, index))
+    rc = _on(index, lib().sparselnr_paged_attention,
+             *head, scale, window, max_new, out.data_ptr(), lse, _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_paged_attention")
     return out
@@ -656,8 +670,9 @@ def sparselnr_block_select(q, kq, kscale, table, seq_len, qptr, page_size, top, 
         sel = torch.empty((T, Hkv, max(top, 0)), dtype=torch.int32, device=q.device)
     else:
         _packed(sel, "sel", torch.int32, index, (T, Hkv, top))
-    rc = lib().sparselnr_block_select(q.data_ptr(), qs[0], qs[1], Hq, code, kq_at, ks_at, pages, page_size, Hkv, D,
-                                      requests, top, first, local, sel.data_ptr(), _launch_stream(stream, index))
+    rc = _on(index, lib().sparselnr_block_select,
+             q.data_ptr(), qs[0], qs[1], Hq, code, kq_at, ks_at, pages, page_size, Hkv, D, requests, top, first,
+             local, sel.data_ptr(), _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_block_select")
     return sel
@@ -672,7 +687,8 @@ def sparselnr_block_attention(q, kcache, vcache, table, seq_len, qptr, sel, scal
         raise ValueError("sel must have 3 dimensions")
     top = sel.shape[2]
     sel_at = _packed(sel, "sel", _torch().int32, index, (q.shape[0], kcache.shape[2], top))
-    rc = lib().sparselnr_block_attention(*head, sel_at, top, scale, out.data_ptr(), lse, _launch_stream(stream, index))
+    rc = _on(index, lib().sparselnr_block_attention,
+             *head, sel_at, top, scale, out.data_ptr(), lse, _launch_stream(stream, index))
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_block_attention")
     return out
