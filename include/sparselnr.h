@@ -283,7 +283,7 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *     adjacent.  Anything else is SPARSELNR_ERR_UNSUPPORTED.  R < 2^24, T < 2^28,
  *     T * Hq < 2^31, W * page_size <= 2^31 - 4096; a seq_len past that of its table's
  *     row ends there.
- *   - R = 0 or T = 0 is a no-op.
+ *   - R = 0 or T = 0 is a no-op, but for sparselnr_page_tables.
  *   - The two attention calls use a workspace per (device, stream) for the results of
  *     contexts that are cut into pieces.  It has one size for all of them, whatever
  *     their tokens, lengths, heads, hint, type and dim are (130 MB on 256 compute
@@ -324,13 +324,16 @@ typedef struct sparselnr_requests {
  *   seq_len[r]  = ctx_len[r] + new_len[r]
  *   table[r][j] for the pages j that the new tokens begin, handed out of
  *               free_pages[0 .. F) in the order of requests and positions; -1 where
- *               the list is used up.  Entries from W on do not exist.
+ *               the list is used up.  Entries from W on do not exist.  A negative entry
+ *               of the list is no page (so a list of fixed length can be filled up).
  *   slots[t]    = page * page_size + place of new token t, -1 if it has no page;
  *               T >= qptr[R] entries, those from qptr[R] on -1
- *   counts      = { qptr[R], pages wanted, tokens without a slot }
+ *   counts      = { qptr[R], pages wanted, tokens without a page }
  * counts[1] is what the free list goes forward by (if it is at most F); a
- * counts[2] above zero tells that F or W was too small.  If T < qptr[R], tokens
- * from T on get no slot and no table entry.  The sums have to stay below 2^31.
+ * counts[2] above zero tells that F or W was too small.  A counts[0] above T
+ * tells that T was: tokens from T on get no slot and enter no page into the table, but
+ * counts[1] holds their pages, and counts[2] only those of them that found none.
+ * qptr and counts are written for R = 0 and T = 0 too.  The sums have to stay below 2^31.
  */
 SPARSELNR_API int sparselnr_page_tables(const int32_t *ctx_len, const int32_t *new_len, int32_t *table,
                                         int64_t table_stride, const int32_t *free_pages, int32_t *qptr,

@@ -36,6 +36,9 @@ __global__ __launch_bounds__(kTablesBlock) void page_tables(TablesArgs a) {
   const int P = 1 << a.shift;
   const int per = (a.R + NT - 1) / NT;
   const int r0 = tid * per < a.R ? tid * per : a.R, r1 = r0 + per < a.R ? r0 + per : a.R;
+  // the first block counts the tokens that find no page; its look at the list is on its way early
+  int listed = 0;
+  if (blockIdx.x == 0 && tid < a.F) listed = a.free_pages[tid];
   auto lengths = [&](int r, int &c, int &n, int &have, int &grow) {
     c = a.ctx[r];
     n = a.len[r];
@@ -70,6 +73,19 @@ __global__ __launch_bounds__(kTablesBlock) void page_tables(TablesArgs a) {
   pages[tid] = y - fresh;
   __syncthreads();
 
+  // The last thread whose requests begin at or before number i of a running sum.
+  auto owner = [&](const int *sum, int i) {
+    int lo = 0, hi = NT - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (sum[mid] <= i)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return lo;
+  };
+
   if (blockIdx.x == 0) {
     int at = x - tokens, page = y - fresh, lost = 0;
     for (int r = r0; r < r1; ++r) {
@@ -88,6 +104,22 @@ __global__ __launch_bounds__(kTablesBlock) void page_tables(TablesArgs a) {
         lost += n < P - (c & (P - 1)) ? n : P - (c & (P - 1));
       at += n;
       page += grow;
+    }
+    // entries of the list that are no pages (a list of fixed length is filled up with them)
+    for (int k = tid; k < (taken < a.F ? taken : a.F); k += NT) {
+      if ((k == tid ? listed : a.free_pages[k]) >= 0) continue;
+      const int o = owner(pages, k);
+      int first = pages[o];
+      for (int r = o * per; r < a.R; ++r) {
+        int c, n, have, grow;
+        lengths(r, c, n, have, grow);
+        if (k < first + grow) {
+          const int64_t j = (int64_t)have + (k - first), end = (int64_t)c + n;  // its tokens from j P on
+          if (j < a.W) lost += (int)(end - (j << a.shift) < P ? end - (j << a.shift) : P);
+          break;
+        }
+        first += grow;
+      }
     }
 #pragma unroll
     for (int o = 32; o; o >>= 1) lost += __shfl_xor(lost, o);
@@ -108,14 +140,7 @@ __global__ __launch_bounds__(kTablesBlock) void page_tables(TablesArgs a) {
   if (t >= a.T) return;
   int64_t slot = -1;
   if (t < all) {
-    int lo = 0, hi = NT - 1;  // the last thread whose requests begin at or before token t
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (begin[mid] <= t)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
+    const int lo = owner(begin, t);
     int at = begin[lo], page = pages[lo];
     int c = 0, n = 0, have = 0, grow = 0, r = lo * per;
     for (; r < a.R; ++r) {

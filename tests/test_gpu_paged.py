@@ -711,3 +711,31 @@ def test_strides_of_extents_of_one(gpu, new):
     assert torch.equal(kc[0, 127], k[0]) and torch.equal(vc[0, 127], k[0])
     want_q, want_s = pu.summary(kc[0, :, 0].cpu().double())
     assert torch.equal(kq[0, 0].cpu(), want_q) and float(ks[0, 0]) == want_s
+
+
+@pytest.mark.parametrize("R,P,seed", [(1, 16, 0), (5, 1, 1), (64, 64, 2), (300, 8, 3), (1500, 16, 4)])
+@pytest.mark.parametrize("gone", ["the last half", "some", "all"])
+def test_page_tables_with_entries_of_the_free_list_that_are_no_pages(gpu, R, P, seed, gone):
+    """A list of fixed length, -1 where it has no page: the tokens there have no slot and are counted."""
+    rng = random.Random(seed)
+    ctx = [rng.choice([0, 1, P - 1, P, rng.randrange(0, 4 * P + 9)]) for _ in range(R)]
+    new = [rng.choice([0, 1, P, rng.randrange(0, 3 * P + 9)]) for _ in range(R)]
+    new[0] = 3 * P + 1
+    have, want = [-(-c // P) for c in ctx], [-(-(c + n) // P) for c, n in zip(ctx, new)]
+    need = sum(w - h for w, h in zip(want, have))
+    W = max(want) - 1  # and one request's table is too narrow
+    ids = list(range(sum(want) + 7))
+    table, at = [], 0
+    for h in have:
+        table.append((ids[at:at + h] + [-1] * W)[:W])
+        at += h
+    free = ids[at:]
+    for i in range(len(free)):
+        if gone == "all" or (gone == "some" and rng.random() < 0.2) or (gone == "the last half" and i >= need // 2):
+            free[i] = -1
+    T = sum(new)
+    got = run_tables(ctx, new, table, free, T, P, gpu)
+    exp = pu.page_tables(ctx, new, table, free, T, P)
+    assert exp[3][2] > 0
+    for name, x, y in zip(("qptr", "seq", "slots", "counts", "table"), got, exp):
+        assert x == list(y), (name, gone)
