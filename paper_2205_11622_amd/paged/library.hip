@@ -10,7 +10,13 @@ namespace slnr {
 
 int hip_error(hipError_t e) { return hip_fail(e); }
 int this_device(int *dev) { return current_device(dev); }
-int device_cu_count(int dev, int *cus) { return device_cus(dev, cus); }
+int device_cu_count(int dev, int *cus) {
+  try {
+    return device_cus(dev, cus);
+  } catch (...) {  // no memory for a record of it
+    return SPARSELNR_ERR_NO_MEMORY;
+  }
+}
 
 int hold_workspace(int dev, hipStream_t stream, size_t bytes, int slot, HeldWorkspace *out) {
   try {

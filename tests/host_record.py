@@ -10,7 +10,7 @@ import subprocess
 import sys
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-SOURCE = os.path.join(ROOT, "tests", "host_runtime", "record_hip.c")
+SOURCE = os.path.join(ROOT, "tests", "host_runtime", "record_hip.cpp")
 LAUNCH, MALLOC, FREE = 0, 1, 2
 
 
@@ -76,7 +76,7 @@ class Recorder:
 def run(scenario, folder, timeout=100):
     """The value that scenario(recorder) returns, in a process of its own."""
     lib = os.path.join(str(folder), "librecord_hip.so")
-    subprocess.check_call(["gcc", "-std=gnu11", "-O1", "-Wall", "-shared", "-fPIC", "-fvisibility=hidden",
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC", "-fvisibility=hidden",
                            "-I/opt/rocm/include", SOURCE, "-o", lib, "-lpthread"])
     code = ("import importlib, json, sys; sys.path.insert(0, %r); from tests import host_record as h; "
             "print(json.dumps(getattr(importlib.import_module(%r), %r)(h.Recorder(%r))))"

@@ -12,7 +12,10 @@
 #include <string.h>
 #include <time.h>
 
-#define API __attribute__((visibility("default")))
+#include <cstdlib>
+#include <new>
+
+#define API extern "C" __attribute__((visibility("default")))
 
 enum { kLaunch = 0, kMalloc = 1, kFree = 2 };
 
@@ -41,6 +44,17 @@ static pthread_cond_t g_other = PTHREAD_COND_INITIALIZER;
 API int record_count(void) { return g_count; }
 API const record_event *record_get(int i) { return &g_events[i]; }
 API void record_reset(void) { g_count = 0; }
+static bool g_no_memory;
+/* From here on allocations of C++ objects fail. */
+API void record_no_memory(int on) { g_no_memory = on != 0; }
+__attribute__((visibility("default"))) void *operator new(size_t n) {
+  void *p = g_no_memory ? nullptr : malloc(n ? n : 1);
+  if (!p) throw std::bad_alloc();
+  return p;
+}
+__attribute__((visibility("default"))) void operator delete(void *p) noexcept { free(p); }
+__attribute__((visibility("default"))) void operator delete(void *p, size_t) noexcept { free(p); }
+
 /* From here on a thread's launch returns only after another thread's, or after so long. */
 API void record_wait(int ms) { g_wait_ms = ms; }
 
@@ -111,7 +125,7 @@ API hipError_t hipOccupancyMaxActiveBlocksPerMultiprocessor(int *blocks, const v
 }
 
 /* What a kernel's host side calls: the launch's shape is pushed, popped and passed on. */
-static __thread struct {
+static thread_local struct {
   dim3 grid, block;
   size_t lds;
   hipStream_t stream;

@@ -173,3 +173,22 @@ def test_launches_of_the_largest_batches_fit(tmp_path):
         for name, grid, block in launches:
             for g, b in zip(grid, block):
                 assert 0 < g * b < 1 << 32, (what, name, grid, block)
+
+
+# ------------------------------------------------------------- memory of the host
+
+
+def no_memory_scenario(rec):
+    """Calls whose records cannot be allocated: the device's facts first, then a stream's workspace."""
+    out = []
+    for _ in range(2):
+        rec.fake.record_no_memory(1)
+        out.append([rec.attend(4, stream=7), rec.sparse(2000, 16, stream=7)])
+        rec.fake.record_no_memory(0)
+        assert rec.attend(4) == 0 and rec.sparse(2000, 16) == 0  # the device is known from here on
+    return out
+
+
+def test_no_memory_is_a_status(tmp_path):
+    """No exception crosses the interface."""
+    assert hr.run(no_memory_scenario, tmp_path) == [[4, 4], [4, 4]]
