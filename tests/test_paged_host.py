@@ -192,3 +192,17 @@ def no_memory_scenario(rec):
 def test_no_memory_is_a_status(tmp_path):
     """No exception crosses the interface."""
     assert hr.run(no_memory_scenario, tmp_path) == [[4, 4], [4, 4]]
+
+
+def by_pages_scenario(rec):
+    out = []
+    for G, P, D, T, Hkv, top in ((128, 512, 64, 900, 1, 3), (40, 256, 128, 900, 1, 3), (1, 64, 64, 3000, 8, 16), (3, 4096, 72, 200, 1, 3),
+                                 (1, 64, 128, 900, 8, 12), (129, 1024, 64, 900, 1, 3), (16, 32, 64, 900, 1, 3)):
+        events = rec.events(lambda: rec.sparse(T, top, Hq=G * Hkv, requests=rec.requests(T, 1, 40), heads=Hkv, dim=D, page_size=P))
+        out.append(any("attend_pages" in e.name for e in events))
+    return out
+
+
+def test_which_selections_go_by_pages(tmp_path):
+    """The shapes that the GPU tests mean to; not groups past a tile's rows, nor pages of less than four keys a head."""
+    assert hr.run(by_pages_scenario, tmp_path) == [True] * 5 + [False] * 2
