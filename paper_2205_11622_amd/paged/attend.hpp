@@ -121,21 +121,19 @@ __device__ __forceinline__ Request request_of(const AttendArgs &a, int r) {
 // about `target` pieces, so long contexts are cut where there are few tiles and
 // left whole where there are many.  With a tail, the tiles behind the first 70% of the
 // work are cut kTailCuts times finer: the blocks that are done early find something
-// to fill the time with until the longest one is done.  Only attend_many has one: one
-// block fills a compute unit there, and 520 tiles on 256 of them, three rounds
-// of which the last has 8, become little more than two.  attend_few has three
-// pieces a unit, two at a time, anyway.
+// to fill the time with until the longest one is done (see has_tail).
 // Every block derives the split from the lengths by one scan: nothing has to be
 // planned, copied or known on the host.
 
 constexpr int kTailCuts = 3;
+constexpr int kTailSteps = 40;
 
 template <int NT>
 struct Split {
   int begin[NT];         // pieces (of one KV head) before this thread's requests
   int slot[NT];          // the same of split tiles only
   long long before[NT];  // steps before them
-  long long work[NT / kWave];
+  long long work[NT / kWave], least[NT / kWave];
   int wave_a[NT / kWave], wave_b[NT / kWave];
   long long whole;       // steps up to which tiles are cut by cap, behind them by cap_tail
   int total, total_split, cap, cap_tail, per;
@@ -161,17 +159,43 @@ __device__ __forceinline__ Cut cut_of(const Split<NT> &sh, long long before, int
   return c;
 }
 
-// count(r, tiles, steps) gives a request's tiles and the steps of its longest one.
-template <int NT, class F>
-__device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, bool tail, F count) {
+// A tail pays where long tiles are a little more than the rounds that the units take them in, so that the last
+// round is nearly empty; elsewhere it only makes more pieces to be joined.  Only attend_many has one: a block of it
+// fills a compute unit.  attend_few has three pieces a unit, two at a time, anyway.  `least` is the sum of all tiles'
+// steps, each request's at its shortest one.  us with / without, 32 / 8 heads of 128 in bf16 on 256 units, one request:
+// behind 8000 tokens 2048 of them (256 tiles) 383 / 328, 2112 (264) 387 / 501, 2560 (320) 429 / 528, 2816 (352) 501 /
+// 543, 3584 (448) 633 / 592, 4096 (512) 785 / 658, 4160 (520) 792 / 873, 5632 (704) 1039 / 1005; from 768 tiles on
+// they are shorter than the cut, alike; two requests behind 3000, 2 x 1056 185 / 221; four behind 1500, 4 x 528 126 / 138, but
+// 4 x 1040 227 / 213; none cached, 2112 100 / 87, 4160 219 / 187.
+__device__ __forceinline__ bool has_tail(const AttendArgs &a, long long tiles, long long least) {
+  const long long all = tiles * a.Hkv, over = all % a.target;
+  return all > a.target && over > 0 && over <= a.target * 3 / 8 && least >= tiles * kTailSteps;
+}
+
+// count(r, tiles, steps) gives a request's tiles and the steps of its longest one; shortest(r, steps) with a
+// tail those of its shortest one.
+struct NoTail {
+  __device__ int operator()(int, int steps) const { return steps; }
+};
+
+template <int NT, class F, class S = NoTail>
+__device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, F count, S shortest = S()) {
+  constexpr bool kTail = !__is_same(S, NoTail);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (a.R + NT - 1) / NT;
   const int r0 = imin(tid * per, a.R), r1 = imin(r0 + per, a.R);
-  long long w = 0;
+  long long w = 0, least = 0;
+  int rows = 0;
   for (int r = r0; r < r1; ++r) {
     int tiles, steps;
     count(r, tiles, steps);
     w += (long long)tiles * imax(steps, 1);
+    if (kTail) least += (long long)tiles * shortest(r, steps), rows += tiles;
+  }
+  if (kTail) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) least += __shfl_xor(least, o), rows += __shfl_xor(rows, o);
+    if (lane == 0) sh.least[wave] = least, sh.wave_a[wave] = rows;
   }
   long long upto = w;
 #pragma unroll
@@ -188,6 +212,14 @@ __device__ void split_scan(Split<NT> &sh, const AttendArgs &a, int min_steps, bo
     all += sh.work[i];
   }
   if (tid == 0) {
+    bool tail = false;
+    if (kTail) {
+      long long tiles = 0;
+      least = 0;
+#pragma unroll
+      for (int i = 0; i < NT / kWave; ++i) least += sh.least[i], tiles += sh.wave_a[i];
+      tail = has_tail(a, tiles, least);
+    }
     const long long want = (all * a.Hkv + a.target - 1) / a.target;
     sh.cap = imax(min_steps, (int)(want < (1 << 28) ? want : (1 << 28)));
     sh.cap_tail = tail ? imax(min_steps, (sh.cap + kTailCuts - 1) / kTailCuts) : sh.cap;
@@ -338,7 +370,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
     total = a.T * row_tiles * np_sparse;
     used = np_sparse > 1 ? total : 0;
   } else {
-    split_scan<kFewBlock>(sh.split, a, 1, false, count);
+    split_scan<kFewBlock>(sh.split, a, 1, count);
     total = sh.split.total;
     used = sh.split.total_split;
   }
@@ -700,7 +732,10 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
     const int lo = (a.window ? imax(q.S - q.n - a.window + 1, 0) : 0) & -kManyKeys;
     steps = (q.S - lo + kManyKeys - 1) / kManyKeys;
   };
-  split_scan<NT>(sh.split, a, kManyMinSteps, true, count);
+  split_scan<NT>(sh.split, a, kManyMinSteps, count, [&](int r, int steps) {
+    const Request q = request_of(a, r);
+    return a.window ? steps : imax(steps - q.n / kManyKeys, 0);  // causal: the first tile sees the context only
+  });
   const int total = sh.split.total;
   if (blockIdx.x == 0 && tid == 0) a.meta[0] = sh.split.total_split * a.Hkv;
 
