@@ -197,3 +197,19 @@ def test_select_any_number_of_pages(gpu, top, D):
     q, _, _, table, seq, qptr = b.upload(gpu)
     got = slnr.sparselnr_block_select(q, kq.to(gpu), ks.to(gpu), table, seq, qptr, 4, top, first=0, local=1).cpu()
     assert torch.equal(got, pu.select(b.q, kq, ks, b.table, b.seq, b.qptr, 4, top, 0, 1))
+
+
+@pytest.mark.parametrize("dtype,D,P", [(BF16, 64, 64), (FP16, 128, 32), (FP32, 64, 64), (BF16, 256, 128)])
+def test_chunks_whose_last_tiles_are_cut_finer(gpu, dtype, D, P):
+    """Eight tiles more than the GPU has units, 42 steps of 64 keys and more each."""
+    units = torch.cuda.get_device_properties(0).multi_processor_count
+    rows = 128 if dtype == FP32 or D > 128 else 256  # of a tile; 8 KV heads of 32 heads each
+    T = (units + 8) * rows // 256
+    b = pu.Batch([2700], [T], 256, 8, D, P, dtype, seed=96)
+    q, kc, vc, table, seq, qptr = b.upload(gpu)
+    lse = torch.full(q.shape[:2], math.nan, device=gpu)
+    out = slnr.sparselnr_paged_attention(q, kc, vc, table, seq, qptr, lse=lse)
+    again = slnr.sparselnr_paged_attention(q, kc, vc, table, seq, qptr)
+    assert torch.equal(out, again) and torch.isfinite(lse).all()
+    every = list(range(len(b.table[0])))
+    sampled(b, [[every] * 8] * T, out, lse, sorted({0, 1, 5, T // 3, T // 2, 3 * T // 4, T - 9, T - 1}), dtype)
