@@ -702,7 +702,14 @@ struct ManyShared {
 };
 
 constexpr int kManyKeys = 64;
-constexpr float kLag = 8.0f;      // the maximum that weights are taken at may be so many powers of two low
+// The maximum that weights are taken at may be so many powers of two low, so that O is seldom rescaled.
+// This costs precision: at the exact maximum the largest weight is one and is not rounded to the type of V; an error of
+// 2.1e-3 of the chunk's result below becomes 2.3e-3.  It pays above 64 columns (us with / without, 32 / 8 heads in bf16: 128
+// columns 4 of 500 tokens behind 3000 144 / 150, 1 of 4000 175 / 183, 64 of 1 to 200 410 / 436; 256 columns, 16 / 4
+// heads, 208 / 218, 252 / 279, 597 / 646); at 64 the maximum is exact (132 / 126, 151 / 144, 365 / 358; fp16
+// 126 / 121, 144 / 147, 363 / 367).
+template <class T, int DP>
+constexpr float kLag = sizeof(T) == 2 && DP > 64 ? 8.0f : 0.0f;
 // Instruction classes of sched_group_barrier.
 constexpr int kMfma = 0x008, kDsRead = 0x100;
 constexpr int kManyMinSteps = 8;  // a piece is at least so many tiles of keys long
@@ -936,9 +943,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many(AttendArgs a) {
 #pragma unroll
       for (int j = 1; j < 32; ++j) top = fmaxf(top, x[j >> 4][j & 15]);
       top = max_across_32(top);
-      // The maximum may lag: weights up to 2^kLag are as good as weights up to 1 (their
-      // sums are in 32 bits, the type's rounding is relative), and O is seldom rescaled.
-      if (__builtin_amdgcn_ballot_w64((top - m) * sc > (sizeof(T) == 4 ? 0.0f : kLag))) {
+      if (__builtin_amdgcn_ballot_w64((top - m) * sc > kLag<T, DP>)) {
         const float mn = fmaxf(m, top);
         const float fade = mn == kNegInf ? 1.0f : exp2_of((m - mn) * sc);
         l *= fade;

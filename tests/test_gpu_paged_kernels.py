@@ -213,3 +213,26 @@ def test_chunks_whose_last_tiles_are_cut_finer(gpu, dtype, D, P):
     assert torch.equal(out, again) and torch.isfinite(lse).all()
     every = list(range(len(b.table[0])))
     sampled(b, [[every] * 8] * T, out, lse, sorted({0, 1, 5, T // 3, T // 2, 3 * T // 4, T - 9, T - 1}), dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("P", [16, 64])
+def test_the_largest_weight_is_not_rounded_at_64_columns(gpu, dtype, P):
+    """Two keys matter, the second, of the larger score, in a later tile and alone with a value: the result is its weight
+    over the sum, which is rounded once only if the weight is exactly one."""
+    T, ctx = 60, 200
+    b = pu.Batch([ctx], [T], 2, 1, 64, P, dtype, seed=97)
+    b.q.zero_()
+    b.q[:, :, 0] = torch.linspace(0.5, 5.5, 2 * T).view(T, 2).to(dtype)
+    k = torch.zeros(ctx + T, 64)
+    k[:, 0] = -64.0
+    k[3, 0], k[130, 0] = 0.0, 1.0
+    v = torch.zeros(ctx + T, 64)
+    v[130] = 1.0
+    for j in range(ctx + T):
+        b.kc[b.table[0][j // P], j % P, 0], b.vc[b.table[0][j // P], j % P, 0] = k[j].to(dtype), v[j].to(dtype)
+    out, _ = run_attention(b, gpu, scale=1.0)
+    x = b.q[:, :, :1].double()
+    want = (1 / (1 + (-x).exp())).expand(-1, -1, 64)  # the others weigh below e^-32
+    # one rounding of a number of [1/2, 1): half a unit, which is EPS / 2; the rest in 32 bits
+    assert ((out.double() - want).abs() <= pu.EPS[dtype] / 2 + 2.0 ** -20).all()
