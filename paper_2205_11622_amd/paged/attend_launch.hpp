@@ -13,7 +13,9 @@ namespace paged {
 // Pieces that the work is cut into, per compute unit.  Two blocks of attend_few are resident
 // on one.  Pieces of a selection are all alike, so they go in one round (32 tokens over 32
 // pages of 64: 69 us; at 3 a unit 87, at 4 77); contexts are ragged, and shorter pieces
-// even them out (64 of 513 to 15096 keys: 259 us; at 2 a unit 291, at 4 262).
+// even them out (64 of 513 to 15096 keys: 259 us; at 2 a unit 291, at 4 262).  A block of attend_many fills a unit: at 2
+// pieces a unit 2 of 2000 tokens behind 7000 738 us (at 1 706), 1 of 512 behind 8000 179 (133), 16 of 64 behind 4000 197
+// (134), 64 of 1 to 200 behind up to 4000 417 (418).
 constexpr int kFewPerCu = 3;
 constexpr int kFewPerCuSparse = 2;
 constexpr int kManyPerCu = 1;
@@ -114,14 +116,21 @@ int run_many(const Launch &l, AttendArgs a) {
 }
 
 // Partial results of by_pages, at most (a call that has more is worked off by KV heads, then
-// by tokens): little enough that the join finds much of them in the 256 MB cache (2048
-// tokens over 16 pages, 8 heads, 545 MB: 405 us; at 80 MB 461, at 288 MB 421, all at once 413).
+// by tokens): little enough that the join finds much of them in the 256 MB cache.  us at 144 MB / at 80 / at 288, of 507 MB: 2000
+// tokens over 16 of 1400 pages, 8 heads 392 / 453 / 411; 4000 over 8 of 400 381 / 416 / 409; 4000 over 16 of 1000, 2 heads
+// 342 / 439 / 375; 1000 over 16, 256 columns 521 / 659 / 536; 1024 over 32 of 256 359 / 400 / 412.
 constexpr int64_t kPagesWorkspace = (int64_t)144 << 20;
 
 // By pages (pages.hpp) rather than by queries: where a page is selected by four queries and
 // more on average, its keys are at least four times the heads of a group (the results
 // of a page are then at most half of what is gathered by queries), and 256 MB and more are
-// gathered, which take longer than the four small launches before and the join.
+// gathered, which take longer than the four small launches before and the join.  us by queries / by pages, 8 heads of
+// 128 in bf16, 16 pages a query:
+// * queries a page (pages of 64, groups of 4): 1 45 / 84, 2 85 / 108, 4 163 / 140 (of 1024 pages) and 43 / 48 (of 256), 8
+//   82 / 52, 16 155 / 67;
+// * keys of a page to heads (512 tokens, 256 pages): 16 to 8 92 / 165, 32 to 16 164 / 314; 16 to 4 90 / 97, 32 to 8 160 / 168, 64
+//   to 16 304 / 323; 32 to 4 158 / 98, 64 to 8 302 / 173;
+// * MB gathered (16 queries a page and more): 128 30 / 32, 256 43 / 38, 512 79 / 45.
 // Not where one token's entries pass the lists' numbers, or its partial results of one KV head (`dp` columns)
 // what is kept of them.
 inline bool by_pages(const AttendArgs &a, int64_t bytes, int64_t dp) {

@@ -119,8 +119,9 @@ __device__ __forceinline__ bool choose_few(const unsigned (&v)[NR], int top, uns
 // Bound by latency: the table, the summaries behind it, the choice's steps one after
 // the other.  32 tokens, 8 heads of 128, contexts of 8302 to 55936 in pages of 64 (13 MB):
 // 16 us; 2020 tokens behind 34227 and 40918 (19 MB, 2.5 Gop): 53 us, of which vector instructions
-// fill a third.  There two blocks share a compute unit (64 registers to a wave; one block
-// of 128: 79 us).
+// fill a third.  There two blocks share a compute unit (64 registers to a wave): us with / with one block of 128, 128
+// columns 2 requests of 1000 behind 30000 47 / 55, 8 of 250 behind 4000 28 / 38, 1 of 4000 behind 30000 70 / 88; 64 columns 43 / 46, 25 /
+// 25, 63 / 65.
 //
 // NR: keys of a row that a lane holds in the choice.
 template <class T, int DP, int TM, int NR>
