@@ -318,9 +318,9 @@ __device__ Piece split_find(const Split<NT> &sh, const AttendArgs &a, int q, F c
 // are in flight per wave while the previous tile is worked on.
 //
 // 64 requests of 513 to 15096 keys, 32 / 8 heads of 128 in bf16 (1190 MB): 252 us, 4.7 TB/s,
-// what a copy of 4 GiB reaches; the join adds 7.  32 tokens over 32 selected
-// pages of 64 keys (269 MB): 64 us, 4.2 TB/s, and 5.5.  4 requests of 635 to 933 keys, 8 / 2
-// heads of 64 in fp32 (3 MB): 12 us and 4.5, the latency of the lengths, the split, the
+// what a copy of 4 GiB reaches; the join adds 6.  32 tokens over 32 selected
+// pages of 64 keys (269 MB): 63 us, 4.2 TB/s, and 5.  4 requests of 635 to 933 keys, 8 / 2
+// heads of 64 in fp32 (3 MB): 12 us and 4, the latency of the lengths, the split, the
 // table, a tile, the four waves' join and the launches.
 
 constexpr int kFewBlock = 256;
@@ -681,10 +681,10 @@ __global__ __launch_bounds__(kFewBlock) void attend_few(AttendArgs a) {
 // Bound by the matrix products and by what feeds them: a product of 32 cycles takes 1 KB of
 // K or V from LDS, so four SIMDs at once use all of its 128 bytes a cycle, and
 // two waves of a SIMD take turns, one in its products, one in its softmax.  4073 tokens
-// behind 6818 and 7894, 32 / 8 heads of 128 in bf16 (559 GFLOP): 690 to 720 us, 0.78
-// to 0.81 PFLOP/s, and 36 us for the join (a product of 8192^3: 1.2).  Of that time, the
+// behind 6818 and 7894, 32 / 8 heads of 128 in bf16 (559 GFLOP): 632 and 654 us on
+// two cards, 0.85 to 0.88 PFLOP/s, after a first 10 ms at up to 730, and 34 us for the join (a product of 8192^3: 1.2).  Of that time, the
 // same with work left out: 0.97 without exponentials, 0.96 without loads, 0.65 without P V.
-// 24 requests under a window of 1024, 16 / 4 heads of 64 in fp16 (2.3 GFLOP): 27 us, two
+// 24 requests under a window of 1024, 16 / 4 heads of 64 in fp16 (2.3 GFLOP): 26 us, two
 // tiles deep and bound by latency.
 // Measured and not taken: V transposed on its way into LDS, 1.07 times as long; all waves
 // in the same phase 1.08; the late half in odd waves, two of them on each of two SIMDs, 1.17;
@@ -1217,7 +1217,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
 }
 
 // The same for the tiles of attend_many: many rows of few pieces, a wave per row.
-// Bound by memory and by its start: 36 us behind the 559 GFLOP above, 9 behind the
+// Bound by memory and by its start: 34 us behind the 559 GFLOP above, 9 behind the
 // window's batch; one row to a block's wave at a time took 44 and 18.
 constexpr int kJoinRows = 8;  // rows of a block, two of them one after the other in each wave
 

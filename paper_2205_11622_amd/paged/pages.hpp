@@ -11,8 +11,8 @@
 // What it moves: every selected page once, and D + 2 values in 32 bits per row and page,
 // written and read; against 2 P D values per query and page that the walk by queries
 // (attend_few) gathers.  2020 tokens over 16 pages of 64 keys, 32 / 8 heads of 128 in
-// bf16: 545 MB there and back and 360 MB of pages, in 48 us for the lists, 4 times 61 for the
-// pages and 4 times 32 for the join; by queries 8.5 GB are gathered.
+// bf16: 545 MB there and back and 360 MB of pages, in 46 us for the lists, 4 times 60 for the
+// pages and 4 times 29 for the join; by queries 8.5 GB are gathered.
 #pragma once
 
 #include "attend.hpp"
@@ -147,7 +147,7 @@ struct PagesShared {
 
 // A block of four waves, 32 rows each, as attend_many; a page is short, so nothing is
 // pipelined here: other blocks on the compute unit fill the waits.  Bound by memory, by the
-// partial results above all: 136 MB of them, 90 MB of pages in 61 us, 3.7 TB/s.
+// partial results above all: 134 MB of them written, 130 MB read in 60 us, 4.4 TB/s.
 template <class T, int DP>
 __global__ __launch_bounds__(kPagesBlock, DP <= 128 ? 2 : 1) void attend_pages(AttendArgs a, PagesArgs pa) {
   typedef typename Type<T>::Vec Vec;
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kPagesBlock, DP <= 128 ? 2 : 1) void attend_pages(A
 }
 
 // The pages of one row (token, head) added up, a wave per row; eight pages' values on
-// their way at a time.  Bound by memory: 136 MB in 32 us, 4.3 TB/s.
+// their way at a time.  Bound by memory: 136 MB in 29 us, 4.7 TB/s.
 template <class T, int DP>
 __global__ __launch_bounds__(kPagesBlock) void join_pages(AttendArgs a, PagesArgs pa) {
   constexpr int C = DP / 64;  // columns of a lane

@@ -27,7 +27,7 @@ constexpr int kTablesBlock = 256;
 // start of a new page enters it into the table: pages of the table that some block
 // reads are never written in the same call.  Latency: one scan and two dependent
 // loads; blocks do not wait for one another.  64 requests of one token: 3.3 us; 1024 of
-// 0 to 40: 6.8 us, four requests to a thread before the scan.
+// 0 to 40: 7.2 us, four requests to a thread before the scan.
 __global__ __launch_bounds__(kTablesBlock) void page_tables(TablesArgs a) {
   constexpr int NT = kTablesBlock, NW = NT / kWave;
   __shared__ int begin[NT], pages[NT];
@@ -191,7 +191,7 @@ struct AppendArgs {
 // rows at once), so the heads go to different blocks there; memory for a chunk, where
 // more tokens a block keep the number of blocks, which start at about 3 ns each, down.
 // 64 tokens, 8 heads of 128 in bf16 (4 MB with the pages' old rows): 9 us; 7868 tokens, 4
-// heads of 64 in fp16 (16 MB): 17 us.
+// heads of 64 in fp16 (16 MB): 16 us.
 constexpr int kAppendBlock = 256;
 
 template <class T>
