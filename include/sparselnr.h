@@ -287,9 +287,9 @@ SPARSELNR_API int sparselnr_validate_csr(const int32_t *rowptr, const int32_t *c
  *   - The two attention calls use a workspace per (device, stream) for the results of
  *     contexts that are cut into pieces.  It has one size for all of them, whatever
  *     their tokens, lengths, heads, hint, type and dim are (130 MB on 256 compute
- *     units): a stream's first call allocates it, later ones and captured graphs find it.
+ *     units): a stream's first such call allocates it, later ones and captured graphs find it.
  *     sparselnr_block_attention of many tokens (four and more per page of
- *     the table, on average) goes by pages and has a workspace of its own: its partial
+ *     the table, on average) goes by pages and has another workspace instead: its partial
  *     results, at most 144 MB, and lists, which grow with T, R, W, top and the heads.
  *     A capture of such a call needs one before, and while the graph may be
  *     replayed no call by pages on that stream may be larger.

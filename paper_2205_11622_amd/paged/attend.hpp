@@ -712,9 +712,9 @@ template <class T, int DP>
 constexpr float kLag = sizeof(T) == 2 && DP > 64 ? 8.0f : 0.0f;
 // Instruction classes of sched_group_barrier.
 constexpr int kMfma = 0x008, kDsRead = 0x100;
-// A piece is at least so many tiles of keys long; fewer hide no latency.  It decides little: at 4, 12 and 16 nine of eleven
-// batches take within 1% of the time at 8, 16 of 64 tokens behind 4000 133, 133 and 132 us (134); 8 of 40 behind 2000 72, 57 and
-// 67 (73).
+// A piece is at least so many tiles of keys long.  It decides little: at 4, 12 and 16 ten of eleven batches take
+// within 2% of the time at 8 (16 of 64 tokens behind 4000 133, 133 and 132 us against 134); 8 of 40 behind 2000 72, 57 and 67
+// against 73.
 constexpr int kManyMinSteps = 8;
 
 // ONE_PAGE: every tile of 64 keys lies in one page (64 positions and more, which begin
