@@ -403,6 +403,148 @@ SPARSELNR_API int sparselnr_block_attention(const void *q, int64_t q_token, int6
                                             int64_t top, double scale, void *out, float *lse,
                                             void *stream);
 
+/* ------------------------------------------------------------------------
+ * A cache in 4 bits.
+ *
+ * The same pages, slots and block tables, with rows of a quarter of the size: a row
+ * of dim values is NG = ceil(dim / 32) groups of 32, the last one filled up with
+ * zeros.  A group has 16 bytes, two values each, the first in the low half: a sign
+ * (8) and 0..7 for 0, 0.5, 1, 1.5, 2, 3, 4, 6.  It has one more byte e + 127 elsewhere: its values are
+ * multiplied by 2^e.  255 stands for a group that is NaN.  (The public formats E2M1
+ * and E8M0 of microscaled numbers.)
+ *
+ * Conventions as above, and:
+ *   - e is the least whole number with max|x| <= 7 * 2^e of the group, at least -125 and at
+ *     most 125 in bf16 and fp32, -23 and 13 in fp16, so that what a group stands for are values of
+ *     the type it came from.  A value is rounded to the nearest, ties to an even code, and
+ *     is off by at most 2^e (0.25, 0.5 or 1 times 2^e by its size), but for values above 7 times 2 to the
+ *     largest e, which become 6 times that.  A group with an infinity or a NaN is NaN.
+ *   - Strides are in bytes; those of k and v keep rows at multiples of 16 bytes, those of the
+ *     exponents may be any.  The 16 * NG bytes of a row, and its NG exponents, are adjacent.
+ *     Heads before places in memory (a head's rows of a page adjacent) is the faster order.
+ *   - dtype is that of the rows that are written and of q and out.  A cache is read in the type
+ *     that it was written in: bf16 and fp32 have the same exponents, fp16 has fewer.
+ *   - sparselnr_paged_attention_fp4 uses the workspace of sparselnr_paged_attention.
+ * ---------------------------------------------------------------------- */
+
+typedef struct sparselnr_fp4_cache {
+  void *k, *v;             /* 16 * NG bytes for every page, place and KV head */
+  void *k_scale, *v_scale; /* NG bytes for each */
+  int64_t pages, page_size, heads, dim;
+  int64_t k_page, k_slot, k_head; /* strides, in bytes */
+  int64_t v_page, v_slot, v_head;
+  int64_t ks_page, ks_slot, ks_head; /* of k_scale */
+  int64_t vs_page, vs_slot, vs_head; /* of v_scale */
+  int32_t dtype;                     /* sparselnr_dtype, of k, v, q and out outside the cache */
+} sparselnr_fp4_cache;
+
+/*
+ * Writes the new tokens' K and V rows (T x Hkv x dim of dtype, strides in values) into
+ * their slots in 4 bits; slots outside the cache are left out, and no slot may occur twice.
+ */
+SPARSELNR_API int sparselnr_cache_append_fp4(const void *k, int64_t k_token, int64_t k_head,
+                                             const void *v, int64_t v_token, int64_t v_head,
+                                             const int64_t *slots, const sparselnr_fp4_cache *cache,
+                                             int64_t T, void *stream);
+
+/*
+ * What the rows of T slots stand for, as values of dtype: k and v are T x Hkv x dim, packed.
+ * Zeros for slots outside the cache; a slot may occur any number of times.
+ */
+SPARSELNR_API int sparselnr_cache_read_fp4(const int64_t *slots, const sparselnr_fp4_cache *cache,
+                                           void *k, void *v, int64_t T, void *stream);
+
+/*
+ * As sparselnr_paged_attention, over a cache in 4 bits.  q.k is computed on its bytes: a query's
+ * groups of 32 values are written as sums of 6-bit pieces, exact to 2^-14 of the group's largest
+ * value for bf16 and fp16 and to 2^-23 for fp32, and summed in fp32.  V is exact; the weights are
+ * rounded to the type of q, in fp32 to 24 bits.
+ */
+SPARSELNR_API int sparselnr_paged_attention_fp4(const void *q, int64_t q_token, int64_t q_head,
+                                                int64_t Hq, const sparselnr_fp4_cache *cache,
+                                                const sparselnr_requests *requests, double scale,
+                                                int64_t window, int64_t max_new, void *out,
+                                                float *lse, void *stream);
+
+/* ------------------------------------------------------------------------
+ * The pages' life: rows of the block table that share pages, rows given up, pages
+ * moved to the front, and copies.
+ *
+ * shares (int32 [pages]) counts the rows that hold a page beyond the first: 0 for a
+ * page of one row and for a free one.  So a program whose rows never share anything
+ * passes zeros, and sparselnr_page_tables, which hands out pages, need not know of it.
+ * Only pages that are full are ever shared, so rows that share pages never write to them.
+ *
+ * Conventions as above, and:
+ *   - seq_len[r] (int32 [R]) is the length of row r; its pages are the first
+ *     ceil(seq_len[r] / page_size) entries of its row of the table, at most W.  What
+ *     lies behind them counts for nothing.  Entries outside [0, pages) are no pages.
+ *   - Whatever the arrays on the device hold, no call reads or writes outside them, and
+ *     results do not depend on the order in which the device works.
+ *   - sparselnr_page_free and sparselnr_page_compact use a workspace per (device, stream) that
+ *     grows with `pages` alone (33 bits a page).  A capture of either needs one call before it
+ *     with as many pages, and while the graph may be replayed no such call on that stream may have more.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * Row children[i] of the table becomes a continuation of row parents[i], i < n: the
+ * parent's full pages are shared (shares + 1 each), and where its last page is not full
+ * the child gets a page of its own from free_pages, in the order of i; the rest of the child's
+ * row is -1.  seq_len[child] becomes the parent's.  pairs[i] (int32 [n][2]) = { the
+ * parent's last page, the child's }, which sparselnr_page_copy copies, or { -1, -1 }.
+ *   counts = { pages taken from the list, forks among them that found none }
+ * A fork that finds no page (the list is used up, or its entry is no page) has -1 there: its child
+ * does not see those positions.  counts[0] is what the free list goes forward by, if it is at most F.
+ * Forks whose parent or child is no row, or whose child is its parent, are left out.
+ * A child's row must hold nothing (what it held is forgotten, not freed), may occur
+ * once, and may not be a parent in the same call.
+ */
+SPARSELNR_API int sparselnr_page_fork(const int32_t *parents, const int32_t *children,
+                                      int32_t *table, int64_t table_stride, int32_t *seq_len,
+                                      int32_t *shares, const int32_t *free_pages, int32_t *pairs,
+                                      int32_t *counts, int64_t n, int64_t R, int64_t W, int64_t F,
+                                      int64_t pages, int64_t page_size, void *stream);
+
+/*
+ * Gives up the rows rows[i], i < n: their entries become -1 and their seq_len 0.  A
+ * page that another row shares loses one of its shares; one that no other row holds is freed.
+ *   freed (int32 [most]): the freed pages, ascending, -1 behind them
+ *   counts = { pages freed, entries given up }
+ * A row that occurs twice is given up once; numbers that are no rows are left out.  Pages
+ * beyond `most` are freed but not listed (counts[0] tells).  min(pages, n * W) is always enough.
+ */
+SPARSELNR_API int sparselnr_page_free(const int32_t *rows, int32_t *table, int64_t table_stride,
+                                      int32_t *seq_len, int32_t *shares, int32_t *freed,
+                                      int32_t *counts, int64_t n, int64_t R, int64_t W, int64_t most,
+                                      int64_t pages, int64_t page_size, void *stream);
+
+/*
+ * Moves the pages that rows hold to the front: of `used` pages in use the k-th one (ascending)
+ * at or behind page `used` goes to the k-th free page before it.  Table and shares
+ * follow at once; the contents do with sparselnr_page_copy on the pairs, before anything else
+ * is written to the cache.  Afterwards the pages from `used` on are free, and all that are.
+ *   pairs (int32 [pages / 2][2]): { from, to }, -1 behind them
+ *   counts = { pages in use, pages moved }
+ */
+SPARSELNR_API int sparselnr_page_compact(int32_t *table, int64_t table_stride, const int32_t *seq_len,
+                                         int32_t *shares, int32_t *pairs, int32_t *counts, int64_t R,
+                                         int64_t W, int64_t pages, int64_t page_size, void *stream);
+
+/* An array whose first dimension is the page.  Page p is outer * inner rows of `row` adjacent
+ * bytes, row (i, j) at data + p * page + i * outer_stride + j * inner_stride.  All in bytes. */
+typedef struct sparselnr_page_array {
+  void *data;
+  int64_t page, outer, outer_stride, inner, inner_stride, row;
+} sparselnr_page_array;
+
+/*
+ * Copies page pairs[i][0] to page pairs[i][1], i < n, in each of `count` arrays (at most 8; a
+ * host array): caches of any type and order, their summaries or exponents.  Pairs with an entry outside
+ * [0, pages) are left out.  A page that is copied to may not occur in another pair.
+ */
+SPARSELNR_API int sparselnr_page_copy(const int32_t *pairs, int64_t n, const sparselnr_page_array *arrays,
+                                      int64_t count, int64_t pages, void *stream);
+
 /* Static text for a status code (never NULL). */
 SPARSELNR_API const char *sparselnr_status_string(int status);
 

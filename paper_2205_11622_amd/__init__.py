@@ -22,6 +22,20 @@ or, over the pages that a cheap score selects for each token and KV head,
 
     sel = sparselnr_block_select(q, kq, kscale, table, seq, qptr, P, top)
     out = sparselnr_block_attention(q, kcache, vcache, table, seq, qptr, sel)
+
+A cache may be kept in 4 bits, a quarter of its size (append, attention, and what it
+stands for):
+
+    sparselnr_cache_append_fp4(k, v, slots, kcache, vcache, kscale, vscale)
+    out = sparselnr_paged_attention_fp4(q, kcache, vcache, kscale, vscale, table, seq, qptr)
+    k, v = sparselnr_cache_read_fp4(slots, kcache, vcache, kscale, vscale, dim, dtype)
+
+and pages shared between requests, given back, and moved together, whatever they hold:
+
+    pairs, counts = sparselnr_page_fork(parents, children, table, seq, shares, free, P)
+    freed, counts = sparselnr_page_free(rows, table, seq, shares, P)
+    pairs, counts = sparselnr_page_compact(table, seq, shares, P)
+    sparselnr_page_copy(pairs, (kcache, vcache))
 """
 from __future__ import annotations
 
@@ -41,6 +55,8 @@ __all__ = [
     "sparselnr_last_hip_error", "sparselnr_abi_version", "sparselnr_set_grid_factor",
     "sparselnr_get_grid_factor", "sparselnr_page_tables", "sparselnr_cache_append",
     "sparselnr_paged_attention", "sparselnr_block_select", "sparselnr_block_attention",
+    "sparselnr_cache_append_fp4", "sparselnr_cache_read_fp4", "sparselnr_paged_attention_fp4",
+    "sparselnr_page_fork", "sparselnr_page_free", "sparselnr_page_compact", "sparselnr_page_copy",
     "SparseLNRError", "lib", "LIB_PATH",
 ]
 
@@ -58,6 +74,18 @@ class _KvCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [
         (n, ctypes.c_int64) for n in ("pages", "page_size", "heads", "dim", "k_page", "k_slot", "k_head",
                                       "v_page", "v_slot", "v_head")] + [("dtype", ctypes.c_int32)]
+
+
+class _Fp4Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [
+        (n, ctypes.c_int64) for n in ("pages", "page_size", "heads", "dim", "k_page", "k_slot", "k_head", "v_page",
+                                      "v_slot", "v_head", "ks_page", "ks_slot", "ks_head", "vs_page", "vs_slot",
+                                      "vs_head")] + [("dtype", ctypes.c_int32)]
+
+
+class _PageArray(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p)] + [(n, ctypes.c_int64) for n in ("page", "outer", "outer_stride", "inner",
+                                                                           "inner_stride", "row")]
 
 
 class _Requests(ctypes.Structure):
@@ -123,6 +151,22 @@ def lib() -> ctypes.CDLL:
         L.sparselnr_block_attention.argtypes = [vp, i64, i64, i64, cache, requests, vp, i64,
                                                 ctypes.c_double, vp, vp, vp]
         L.sparselnr_block_attention.restype = ci
+        fp4, arrays = ctypes.POINTER(_Fp4Cache), ctypes.POINTER(_PageArray)
+        L.sparselnr_cache_append_fp4.argtypes = [vp, i64, i64, vp, i64, i64, vp, fp4, i64, vp]
+        L.sparselnr_cache_append_fp4.restype = ci
+        L.sparselnr_cache_read_fp4.argtypes = [vp, fp4, vp, vp, i64, vp]
+        L.sparselnr_cache_read_fp4.restype = ci
+        L.sparselnr_paged_attention_fp4.argtypes = [vp, i64, i64, i64, fp4, requests, ctypes.c_double, i64, i64, vp,
+                                                    vp, vp]
+        L.sparselnr_paged_attention_fp4.restype = ci
+        L.sparselnr_page_fork.argtypes = [vp, vp, vp, i64] + [vp] * 5 + [i64] * 6 + [vp]
+        L.sparselnr_page_fork.restype = ci
+        L.sparselnr_page_free.argtypes = [vp, vp, i64] + [vp] * 4 + [i64] * 6 + [vp]
+        L.sparselnr_page_free.restype = ci
+        L.sparselnr_page_compact.argtypes = [vp, i64] + [vp] * 4 + [i64] * 4 + [vp]
+        L.sparselnr_page_compact.restype = ci
+        L.sparselnr_page_copy.argtypes = [vp, i64, arrays, i64, i64, vp]
+        L.sparselnr_page_copy.restype = ci
         _lib = L
     return _lib
 
@@ -692,3 +736,214 @@ def sparselnr_block_attention(q, kcache, vcache, table, seq_len, qptr, sel, scal
     if rc != OK:
         raise SparseLNRError(rc, "sparselnr_block_attention")
     return out
+
+
+# ------------------------------------------------------------ cache in 4 bits
+
+
+def _fp4_cache(kcache, vcache, kscale, vscale, dim, dtype_of):
+    """The cache's descriptor; `dtype_of` is a tensor of the type outside the cache."""
+    uint8 = _torch().uint8
+    index = _gpu(kcache, "kcache")
+    code = _dtype_code(dtype_of, "rows")
+    k = _rows(kcache, "kcache", 4, uint8, index)
+    v = _rows(vcache, "vcache", 4, uint8, index)
+    ks = _rows(kscale, "kscale", 4, uint8, index)
+    vs = _rows(vscale, "vscale", 4, uint8, index)
+    shape = kcache.shape
+    pages, P, Hkv, width = shape
+    groups = -(-dim // 32)
+    if vcache.shape != shape:
+        raise ValueError("kcache and vcache differ in shape")
+    if width != 16 * groups:
+        raise ValueError("the caches' rows must have 16 bytes for each 32 of %d values" % dim)
+    if kscale.shape != (pages, P, Hkv, groups) or vscale.shape != kscale.shape:
+        raise ValueError("kscale and vscale must have a byte for each 32 of %d values of a row" % dim)
+    return index, shape, _Fp4Cache(kcache.data_ptr(), vcache.data_ptr(), kscale.data_ptr(), vscale.data_ptr(), pages, P,
+                                   Hkv, dim, k[0], k[1], k[2], v[0], v[1], v[2], ks[0], ks[1], ks[2], vs[0], vs[1],
+                                   vs[2], code)
+
+
+def sparselnr_cache_append_fp4(k, v, slots, kcache, vcache, kscale, vscale, stream=None):
+    """Writes k and v (T x Hkv x D) into the slots (int64[T]; -1: left out) of a cache in 4
+    bits: kcache and vcache uint8 pages x page_size x Hkv x 16 ceil(D / 32), kscale and vscale
+    uint8 pages x page_size x Hkv x ceil(D / 32), any order of memory."""
+    torch = _torch()
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must have 3 dimensions")
+    index, shape, cache = _fp4_cache(kcache, vcache, kscale, vscale, k.shape[2], k)
+    ks = _rows(k, "k", 3, k.dtype, index)
+    vs = _rows(v, "v", 3, k.dtype, index)
+    T = k.shape[0]
+    if k.shape != v.shape or k.shape[1] != shape[2]:
+        raise ValueError("k and v must be T x Hkv x D, as the cache's rows")
+    rc = _on(index, lib().sparselnr_cache_append_fp4,
+             k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], _packed(slots, "slots", torch.int64, index, (T,)),
+             cache, T, _launch_stream(stream, index))
+    if rc != OK:
+        raise SparseLNRError(rc, "sparselnr_cache_append_fp4")
+
+
+def sparselnr_cache_read_fp4(slots, kcache, vcache, kscale, vscale, dim, dtype, k=None, v=None, stream=None):
+    """What the rows of the slots (int64[T]) of a cache in 4 bits stand for, as (k, v), T x Hkv x
+    dim of `dtype`, in the tensors given for them if any; zeros for slots outside the cache."""
+    torch = _torch()
+    index = _gpu(slots, "slots")
+    T = slots.numel()
+    shape = (T, kcache.shape[2] if isinstance(kcache, torch.Tensor) and kcache.dim() == 4 else 0, dim)
+    k = torch.empty(shape, dtype=dtype, device=slots.device) if k is None else k
+    v = torch.empty(shape, dtype=dtype, device=slots.device) if v is None else v
+    index, _, cache = _fp4_cache(kcache, vcache, kscale, vscale, dim, k)
+    rc = _on(index, lib().sparselnr_cache_read_fp4,
+             _packed(slots, "slots", torch.int64, index, (T,)), cache, _packed(k, "k", dtype, index, shape),
+             _packed(v, "v", dtype, index, shape), T, _launch_stream(stream, index))
+    if rc != OK:
+        raise SparseLNRError(rc, "sparselnr_cache_read_fp4")
+    return k, v
+
+
+def sparselnr_paged_attention_fp4(q, kcache, vcache, kscale, vscale, table, seq_len, qptr, scale=None, window=0,
+                                  max_new=0, out=None, lse=None, stream=None):
+    """sparselnr_paged_attention over a cache in 4 bits (see sparselnr_cache_append_fp4).
+    Returns out (T x Hq x D, of the type of q)."""
+    torch = _torch()
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must have 3 dimensions")
+    T, Hq, D = q.shape
+    index, shape, cache = _fp4_cache(kcache, vcache, kscale, vscale, D, q)
+    qs = _rows(q, "q", 3, q.dtype, index)
+    if shape[2] == 0 or Hq % shape[2]:
+        raise ValueError("query heads must be a multiple of the cache's heads")
+    requests = _requests(table, seq_len, qptr, T, index)
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    else:
+        _packed(out, "out", q.dtype, index, (T, Hq, D))
+    lse_at = None if lse is None else _packed(lse, "lse", torch.float32, index, (T, Hq))
+    rc = _on(index, lib().sparselnr_paged_attention_fp4,
+             q.data_ptr(), qs[0], qs[1], Hq, cache, requests, D ** -0.5 if scale is None else scale, window, max_new,
+             out.data_ptr(), lse_at, _launch_stream(stream, index))
+    if rc != OK:
+        raise SparseLNRError(rc, "sparselnr_paged_attention_fp4")
+    return out
+
+
+# ------------------------------------------------------------ the pages' life
+
+
+def _held(table, seq_len, shares):
+    """GPU, table stride, rows, width, number of pages, addresses of table, lengths and shares."""
+    int32 = _torch().int32
+    index = _gpu(table, "table")
+    stride, R, W = _table(table, index)
+    pages = shares.numel() if isinstance(shares, _torch().Tensor) else 0
+    return (index, stride, R, W, pages, table.data_ptr(), _packed(seq_len, "seq_len", int32, index, (R,)),
+            _packed(shares, "shares", int32, index, (pages,)))
+
+
+def sparselnr_page_fork(parents, children, table, seq_len, shares, free_pages, page_size, pairs=None, counts=None,
+                        stream=None):
+    """Rows children[i] of the table (int32[R, W]) go on from rows parents[i] (int32[n]):
+    full pages are shared (shares int32[pages]), a last page that is not full becomes one of
+    free_pages (int32[F]) and a pair for sparselnr_page_copy.  Returns (pairs int32[n, 2], counts
+    int32[2]: pages taken, forks that found none); table, seq_len and shares change in place."""
+    torch = _torch()
+    int32 = torch.int32
+    index, stride, R, W, pages, at, seq_at, shares_at = _held(table, seq_len, shares)
+    n = parents.numel() if isinstance(parents, torch.Tensor) else 0
+    F = free_pages.numel() if isinstance(free_pages, torch.Tensor) else 0
+    pairs = torch.empty((n, 2), dtype=int32, device=table.device) if pairs is None else pairs
+    counts = torch.empty(2, dtype=int32, device=table.device) if counts is None else counts
+    rc = _on(index, lib().sparselnr_page_fork,
+             _packed(parents, "parents", int32, index, (n,)), _packed(children, "children", int32, index, (n,)), at,
+             stride, seq_at, shares_at, _packed(free_pages, "free_pages", int32, index, (F,)),
+             _packed(pairs, "pairs", int32, index, (n, 2)), _packed(counts, "counts", int32, index, (2,)), n, R, W, F,
+             pages, page_size, _launch_stream(stream, index))
+    if rc != OK:
+        raise SparseLNRError(rc, "sparselnr_page_fork")
+    return pairs, counts
+
+
+def sparselnr_page_free(rows, table, seq_len, shares, page_size, freed=None, counts=None, stream=None):
+    """Gives up rows of the table (rows int32[n]): entries -1, seq_len 0, shared pages with a
+    share less.  Returns (freed int32: pages that no row holds any more, ascending, -1 behind them,
+    counts int32[2]: pages freed, entries given up)."""
+    torch = _torch()
+    int32 = torch.int32
+    index, stride, R, W, pages, at, seq_at, shares_at = _held(table, seq_len, shares)
+    n = rows.numel() if isinstance(rows, torch.Tensor) else 0
+    freed = torch.empty(min(pages, n * W), dtype=int32, device=table.device) if freed is None else freed
+    counts = torch.empty(2, dtype=int32, device=table.device) if counts is None else counts
+    most = freed.numel() if isinstance(freed, torch.Tensor) else 0
+    rc = _on(index, lib().sparselnr_page_free,
+             _packed(rows, "rows", int32, index, (n,)), at, stride, seq_at, shares_at,
+             _packed(freed, "freed", int32, index, (most,)), _packed(counts, "counts", int32, index, (2,)), n, R, W,
+             most, pages, page_size, _launch_stream(stream, index))
+    if rc != OK:
+        raise SparseLNRError(rc, "sparselnr_page_free")
+    return freed, counts
+
+
+def sparselnr_page_compact(table, seq_len, shares, page_size, pairs=None, counts=None, stream=None):
+    """Moves the pages in use to the front of the cache: table and shares change in place, and
+    sparselnr_page_copy does the rest.  Returns (pairs int32[pages // 2, 2], -1 behind them,
+    counts int32[2]: pages in use, pages moved)."""
+    torch = _torch()
+    int32 = torch.int32
+    index, stride, R, W, pages, at, seq_at, shares_at = _held(table, seq_len, shares)
+    pairs = torch.empty((pages // 2, 2), dtype=int32, device=table.device) if pairs is None else pairs
+    counts = torch.empty(2, dtype=int32, device=table.device) if counts is None else counts
+    rc = _on(index, lib().sparselnr_page_compact,
+             at, stride, seq_at, shares_at, _packed(pairs, "pairs", int32, index, (pages // 2, 2)),
+             _packed(counts, "counts", int32, index, (2,)), R, W, pages, page_size, _launch_stream(stream, index))
+    if rc != OK:
+        raise SparseLNRError(rc, "sparselnr_page_compact")
+    return pairs, counts
+
+
+def _page_array(t, name, index, pages):
+    """A tensor's pages as rows of adjacent bytes, with at most two strides above them."""
+    if not isinstance(t, _torch().Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if t.get_device() != index:
+        raise ValueError("%s is on %s, expected GPU %d" % (name, t.device, index))
+    if t.dim() < 1 or t.shape[0] != pages:
+        raise ValueError("the first dimension of %s must be the page, %d of them" % (name, pages))
+    e = t.element_size()
+    dims = sorted((s * e, n) for s, n in zip(t.stride()[1:], t.shape[1:]) if n != 1)
+    inside = e
+    for stride, n in sorted(dims + [(t.stride(0) * e, pages)] if pages != 1 else dims):
+        if stride < inside and t.numel():
+            raise ValueError("%s has elements at one address, or strides that do not nest" % name)
+        inside += stride * (n - 1)
+    row, levels = e, []
+    for stride, n in dims:
+        if not levels and stride == row:
+            row *= n
+        elif levels and stride == levels[-1][0] * levels[-1][1]:
+            levels[-1] = (levels[-1][0], levels[-1][1] * n)
+        else:
+            levels.append((stride, n))
+    if len(levels) > 2:
+        raise ValueError("the pages of %s have more than two strides" % name)
+    (inner_stride, inner), (outer_stride, outer) = (levels + [(0, 1), (0, 1)])[:2]
+    return _PageArray(t.data_ptr(), t.stride(0) * e, outer, outer_stride, inner, inner_stride, row)
+
+
+def sparselnr_page_copy(pairs, arrays, stream=None):
+    """Copies page pairs[i, 0] to page pairs[i, 1] (int32[n, 2]; pairs with a negative entry are
+    left out) in each of the arrays (up to 8 tensors of any type whose first dimension is the page)."""
+    torch = _torch()
+    index = _gpu(pairs, "pairs")
+    arrays = (arrays,) if isinstance(arrays, torch.Tensor) else tuple(arrays)
+    if pairs.dim() != 2:
+        raise ValueError("pairs must have 2 dimensions")
+    n = pairs.shape[0]
+    at = _packed(pairs, "pairs", torch.int32, index, (n, 2))
+    if not arrays:
+        return
+    pages = arrays[0].shape[0] if isinstance(arrays[0], torch.Tensor) and arrays[0].dim() else 0
+    list_of = (_PageArray * len(arrays))(*(_page_array(t, "arrays[%d]" % i, index, pages) for i, t in enumerate(arrays)))
+    rc = _on(index, lib().sparselnr_page_copy, at, n, list_of, len(arrays), pages, _launch_stream(stream, index))
+    if rc != OK:
+        raise SparseLNRError(rc, "sparselnr_page_copy")

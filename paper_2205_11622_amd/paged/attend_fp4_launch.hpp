@@ -1,0 +1,95 @@
+// Launches of the attention kernels over a cache in 4 bits, for one type.
+#pragma once
+
+#include "attend_fp4.hpp"
+#include "launch.hpp"
+
+namespace slnr {
+namespace paged {
+
+// A request with more rows than this goes to attend_many_fp4.
+template <class T, int DP>
+constexpr int kFew4MostRows = sizeof(T) == 2 && DP > 64 ? 32 : 64;
+// Waves of a block of attend_many_fp4: two to a SIMD, one where O of 256 columns takes the registers of two.
+template <class T, int DP>
+constexpr int kMany4Waves = DP > 128 ? 4 : 8;
+
+template <class F>
+int launch_fp4(F *fn, dim3 grid, int block, size_t lds, const Launch &l, const AttendFp4Args &a) {
+  hipLaunchKernelGGL(fn, grid, dim3(block), lds, l.stream, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? SPARSELNR_OK : hip_error(e);
+}
+
+template <class T, int DP, bool ONE_PAGE>
+int run_few_fp4(const Launch &l, AttendFp4Args a, int most_rows) {
+  a.target = l.cus * kFewPerCu;
+  const int64_t requests = a.R < a.T ? a.R : a.T;  // that have tokens, at most
+  int64_t tiles = (int64_t)a.T * a.G / kFewRows + requests;
+  // Beside attend_many_fp4: only what is left of a request has tiles here.
+  const int64_t left = requests * ((kFew4MostRows<T, DP> + kFewRows - 1) / kFewRows);
+  if (a.few <= kFew4MostRows<T, DP> && tiles > left) tiles = left;
+  const int64_t pieces = tiles * a.Hkv + a.target;
+  static_assert(kFewRows * (DP + 2) <= kFewValues, "fits the workspace");
+  const int64_t slots = few_slots(a.target);
+  HeldWorkspace ws;
+  int rc = partials(l, slots, a, &ws);
+  if (rc != SPARSELNR_OK) return rc;
+  const int64_t most = (int64_t)l.cus * 8;
+  const unsigned grid = (unsigned)(pieces < most ? pieces : most);
+  rc = launch_fp4(attend_few_fp4<T, DP, ONE_PAGE>, dim3(grid), kFewBlock, sizeof(Few4Shared<T, DP>), l, a);
+  if (rc != SPARSELNR_OK) return rc;
+  const unsigned side = most_rows < kFewRows ? most_rows : kFewRows;  // about 8000 blocks in all
+  return launch(join_few<T, DP>, dim3((unsigned)(slots < 8192 / side ? slots : 8192 / side), side), kJoinBlock, 0, l, a);
+}
+
+template <class T, int DP, bool ONE_PAGE>
+int run_many_fp4(const Launch &l, AttendFp4Args a) {
+  constexpr int NW = kMany4Waves<T, DP>, ROWS = 32 * NW;
+  a.target = l.cus * kManyPerCu;
+  const int64_t tiles = ((int64_t)a.T * a.G / ROWS + (a.R < a.T ? a.R : a.T)) * a.Hkv;
+  static_assert(ROWS * (DP + 2) <= kManyValues, "fits the workspace");
+  const int64_t pieces = tiles + many_caps(a.target), most = grid_limit(NW * kWave);
+  HeldWorkspace ws;
+  int rc = partials(l, many_slots(a.target), a, &ws);
+  if (rc != SPARSELNR_OK) return rc;
+  rc = launch_fp4(attend_many_fp4<T, DP, NW, ONE_PAGE>, dim3((unsigned)(pieces < most ? pieces : most)), NW * kWave,
+                  sizeof(Many4SharedOf<T, DP, NW>), l, a);
+  if (rc != SPARSELNR_OK) return rc;
+  return launch(join_many<T, DP, ROWS>, dim3((unsigned)l.cus, ROWS / kJoinRows), kJoinBlock, 0, l, a);
+}
+
+template <class T, int DP, bool ONE_PAGE>
+int run_attend_fp4(const Launch &l, AttendFp4Args a, int64_t max_new) {
+  // rows of the longest request, as far as the host knows
+  const int64_t rows = (max_new > 0 && max_new < a.T ? max_new : a.T) * a.G;
+  a.few = 0x7fffffff;
+  if (rows > kFew4MostRows<T, DP>) {
+    a.few = kFew4MostRows<T, DP>;
+    const int rc = run_many_fp4<T, DP, ONE_PAGE>(l, a);
+    if (rc != SPARSELNR_OK) return rc;
+  }
+  return run_few_fp4<T, DP, ONE_PAGE>(l, a, rows < kFewRows ? (int)rows : kFewRows);
+}
+
+template <class T, int DP>
+int attend_fp4_width(const Launch &l, const AttendFp4Args &a, int64_t max_new) {
+  // a tile of 64 keys within one page, its rows within 32 bits of bytes
+  const int64_t most = 1 << 24;
+  const bool one_page = a.shift >= 6 && a.k_slot < most && a.v_slot < most && a.ks_slot < most && a.vs_slot < most;
+  return one_page ? run_attend_fp4<T, DP, true>(l, a, max_new) : run_attend_fp4<T, DP, false>(l, a, max_new);
+}
+
+template <class T>
+int attend_fp4_type(const Launch &l, const AttendFp4Args &a, int64_t max_new) {
+  if (a.D <= 64) return attend_fp4_width<T, 64>(l, a, max_new);
+  if (a.D <= 128) return attend_fp4_width<T, 128>(l, a, max_new);
+  return attend_fp4_width<T, 256>(l, a, max_new);
+}
+
+int attend_fp4_bf16(const Launch &l, const AttendFp4Args &a, int64_t max_new);
+int attend_fp4_fp16(const Launch &l, const AttendFp4Args &a, int64_t max_new);
+int attend_fp4_fp32(const Launch &l, const AttendFp4Args &a, int64_t max_new);
+
+}  // namespace paged
+}  // namespace slnr

@@ -1,0 +1,173 @@
+// Entry points of the pages' life: argument checks and launches.  The C ABI is declared in
+// include/sparselnr.h.
+#include "life.hpp"
+
+#include "checks.hpp"
+
+namespace {
+
+using namespace slnr;
+using namespace slnr::paged;
+
+// Blocks for `n` things of a thread each, at most `most`.
+unsigned blocks_for(int64_t n, int64_t most) {
+  const int64_t b = (n + kLifeBlock - 1) / kLifeBlock;
+  return (unsigned)(b < 1 ? 1 : b > most ? most : b);
+}
+
+int check_table(const int32_t *table, int64_t table_stride, const int32_t *seq_len, const int32_t *shares, int64_t R,
+                int64_t W, int64_t pages, int64_t page_size) {
+  if (R < 0 || W < 0 || pages < 0 || table_stride < 0) return SPARSELNR_ERR_INVALID_ARG;
+  if ((R > 0 && !seq_len) || (R > 0 && W > 0 && !table) || (pages > 0 && !shares) || (R > 1 && table_stride < W))
+    return SPARSELNR_ERR_INVALID_ARG;
+  if (page_shift(page_size) < 0 || R >= ((int64_t)1 << 24) || pages > kMax31 || W > kMaxPositions / page_size)
+    return SPARSELNR_ERR_UNSUPPORTED;
+  return SPARSELNR_OK;
+}
+
+// The marks of `pages` pages and, behind them, a number for each.
+int life_workspace(const Launch &l, LifeArgs &a, bool ranks, HeldWorkspace *ws) {
+  a.words = ((int64_t)a.pages + 63) / 64;
+  const size_t marks = (size_t)(a.words < 1 ? 1 : a.words) * sizeof(Word);
+  const int rc = hold_workspace(l.dev, l.stream, marks + (size_t)a.pages * sizeof(int32_t), kSlotLife, ws);
+  if (rc != SPARSELNR_OK) return rc;
+  a.marks = (Word *)ws->ptr;
+  a.rank = ranks ? (int32_t *)((char *)ws->ptr + marks) : nullptr;
+  return SPARSELNR_OK;
+}
+
+// Rows along x, up to eight blocks to a long one.
+dim3 grid_of_rows(int64_t rows, int64_t W) {
+  return dim3((unsigned)(rows < 1 ? 1 : rows > 8192 ? 8192 : rows), blocks_for(W, 8));
+}
+
+// Blocks that go through the marks; each of them counts all marks before its own.
+unsigned grid_of_words(const LifeArgs &a) {
+  const int64_t b = (a.words + 63) / 64;
+  return (unsigned)(b < 1 ? 1 : b > 256 ? 256 : b);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sparselnr_page_fork(const int32_t *parents, const int32_t *children, int32_t *table, int64_t table_stride,
+                        int32_t *seq_len, int32_t *shares, const int32_t *free_pages, int32_t *pairs, int32_t *counts,
+                        int64_t n, int64_t R, int64_t W, int64_t F, int64_t pages, int64_t page_size, void *stream) {
+  if (n < 0 || F < 0) return SPARSELNR_ERR_INVALID_ARG;
+  const int rc = check_table(table, table_stride, seq_len, shares, R, W, pages, page_size);
+  if (rc != SPARSELNR_OK) return rc;
+  if (!counts || (n > 0 && (!parents || !children || !pairs)) || (F > 0 && !free_pages)) return SPARSELNR_ERR_INVALID_ARG;
+  if (n >= ((int64_t)1 << 24) || F > kMax31) return SPARSELNR_ERR_UNSUPPORTED;
+  ForkArgs a{};
+  a.parents = parents, a.children = children;
+  a.table = table, a.table_row = table_stride;
+  a.seq = seq_len, a.shares = shares;
+  a.free_pages = free_pages;
+  a.pairs = pairs, a.counts = counts;
+  a.n = (int32_t)n, a.R = (int32_t)R, a.W = (int32_t)W, a.F = (int32_t)F, a.pages = (int32_t)pages;
+  a.shift = page_shift(page_size);
+  // every block counts the forks before its own
+  const int64_t per = (n + 2047) / 2048 > 0 ? (n + 2047) / 2048 : 1;
+  const unsigned blocks = (unsigned)(n > 0 ? (n + per - 1) / per : 1);
+  hipLaunchKernelGGL(page_fork, dim3(blocks), dim3(kLifeBlock), 0, (hipStream_t)stream, a, (int)per);
+  return launched();
+}
+
+int sparselnr_page_free(const int32_t *rows, int32_t *table, int64_t table_stride, int32_t *seq_len, int32_t *shares,
+                        int32_t *freed, int32_t *counts, int64_t n, int64_t R, int64_t W, int64_t most, int64_t pages,
+                        int64_t page_size, void *stream) {
+  if (n < 0 || most < 0) return SPARSELNR_ERR_INVALID_ARG;
+  int rc = check_table(table, table_stride, seq_len, shares, R, W, pages, page_size);
+  if (rc != SPARSELNR_OK) return rc;
+  if (!counts || (n > 0 && !rows) || (most > 0 && !freed)) return SPARSELNR_ERR_INVALID_ARG;
+  if (n >= ((int64_t)1 << 24) || most > kMax31) return SPARSELNR_ERR_UNSUPPORTED;
+  LifeArgs a{};
+  a.rows = rows;
+  a.table = table, a.table_row = table_stride;
+  a.seq = seq_len, a.shares = shares;
+  a.out = freed, a.counts = counts;
+  a.n = (int32_t)n, a.R = (int32_t)R, a.W = (int32_t)W, a.pages = (int32_t)pages, a.most = (int32_t)most;
+  a.shift = page_shift(page_size);
+  Launch l;
+  if ((rc = current(&l, stream)) != SPARSELNR_OK) return rc;
+  HeldWorkspace ws;
+  if ((rc = life_workspace(l, a, false, &ws)) != SPARSELNR_OK) return rc;
+  const dim3 block(kLifeBlock);
+  hipLaunchKernelGGL(life_clear, dim3(blocks_for(most > a.words ? most : a.words, 1024)), block, 0, l.stream, a, most);
+  if ((rc = launched()) != SPARSELNR_OK) return rc;
+  hipLaunchKernelGGL(page_free_rows, grid_of_rows(n, W), block, 0, l.stream, a);
+  if ((rc = launched()) != SPARSELNR_OK) return rc;
+  hipLaunchKernelGGL(page_free_list, dim3(grid_of_words(a)), block, 0, l.stream, a);
+  return launched();
+}
+
+int sparselnr_page_compact(int32_t *table, int64_t table_stride, const int32_t *seq_len, int32_t *shares,
+                           int32_t *pairs, int32_t *counts, int64_t R, int64_t W, int64_t pages, int64_t page_size,
+                           void *stream) {
+  int rc = check_table(table, table_stride, seq_len, shares, R, W, pages, page_size);
+  if (rc != SPARSELNR_OK) return rc;
+  if (!counts || (pages > 1 && !pairs)) return SPARSELNR_ERR_INVALID_ARG;
+  LifeArgs a{};
+  a.table = table, a.table_row = table_stride;
+  a.seq = const_cast<int32_t *>(seq_len), a.shares = shares;
+  a.out = pairs, a.counts = counts;
+  a.R = (int32_t)R, a.W = (int32_t)W, a.pages = (int32_t)pages, a.most = (int32_t)(pages / 2);
+  a.shift = page_shift(page_size);
+  Launch l;
+  if ((rc = current(&l, stream)) != SPARSELNR_OK) return rc;
+  HeldWorkspace ws;
+  if ((rc = life_workspace(l, a, true, &ws)) != SPARSELNR_OK) return rc;
+  const dim3 block(kLifeBlock), rows = grid_of_rows(R, W);
+  const int64_t outs = 2 * (int64_t)a.most;
+  hipLaunchKernelGGL(life_clear, dim3(blocks_for(outs > a.words ? outs : a.words, 1024)), block, 0, l.stream, a, outs);
+  if ((rc = launched()) != SPARSELNR_OK) return rc;
+  hipLaunchKernelGGL(page_mark_used, rows, block, 0, l.stream, a);
+  if ((rc = launched()) != SPARSELNR_OK) return rc;
+  hipLaunchKernelGGL(page_compact_pairs, dim3(grid_of_words(a)), block, 0, l.stream, a);
+  if ((rc = launched()) != SPARSELNR_OK) return rc;
+  hipLaunchKernelGGL(page_compact_tables, rows, block, 0, l.stream, a);
+  return launched();
+}
+
+int sparselnr_page_copy(const int32_t *pairs, int64_t n, const sparselnr_page_array *arrays, int64_t count,
+                        int64_t pages, void *stream) {
+  if (n < 0 || count < 0 || pages < 0 || (n > 0 && !pairs) || (count > 0 && !arrays)) return SPARSELNR_ERR_INVALID_ARG;
+  if (count > kCopyArrays || n > kMax31 || pages > kMax31) return SPARSELNR_ERR_UNSUPPORTED;
+  CopyArgs a{};
+  int64_t steps = 0;
+  for (int64_t k = 0; k < count; ++k) {
+    const sparselnr_page_array &in = arrays[k];
+    if (in.page < 0 || in.outer < 0 || in.inner < 0 || in.row < 0 || in.outer_stride < 0 || in.inner_stride < 0)
+      return SPARSELNR_ERR_INVALID_ARG;
+    if (in.outer == 0 || in.inner == 0 || in.row == 0 || pages == 0) continue;
+    if (!in.data) return SPARSELNR_ERR_INVALID_ARG;
+    if (in.outer > kMax31 || in.inner > kMax31 || in.row > kMax31 || in.outer * in.inner > (kMax31 << 10) / in.row)
+      return SPARSELNR_ERR_UNSUPPORTED;
+    CopyArray &x = a.array[a.arrays++];
+    x.data = (uint8_t *)in.data;
+    x.page = stride_of(in.page, pages);
+    x.outer_stride = stride_of(in.outer_stride, in.outer), x.inner_stride = stride_of(in.inner_stride, in.inner);
+    x.row = (unsigned)in.row, x.inner = (unsigned)in.inner;
+    x.bytes = in.outer * in.inner * in.row;
+    x.dense = (in.inner == 1 || x.inner_stride == in.row) && (in.outer == 1 || x.outer_stride == in.inner * in.row);
+    const int64_t all = (int64_t)(uintptr_t)in.data | x.page | x.bytes |
+                        (x.dense ? 0 : x.outer_stride | x.inner_stride | in.row);
+    x.unit = all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1;
+    x.steps = (int)((x.bytes + kCopyBytes - 1) / kCopyBytes);
+    steps += x.steps;
+  }
+  if (steps > kMax31) return SPARSELNR_ERR_UNSUPPORTED;
+  if (n == 0 || a.arrays == 0) return SPARSELNR_OK;
+  a.pairs = pairs;
+  a.n = (int32_t)n, a.pages = (int32_t)pages, a.steps = (int32_t)steps;
+  a.items = n * steps;
+  Launch l;
+  const int rc = current(&l, stream);
+  if (rc != SPARSELNR_OK) return rc;
+  const int64_t most = (int64_t)l.cus * 8;
+  hipLaunchKernelGGL(page_copy, dim3((unsigned)(a.items < most ? a.items : most)), dim3(kLifeBlock), 0, l.stream, a);
+  return launched();
+}
+
+}  // extern "C"

@@ -1,0 +1,347 @@
+// What becomes of the cache's pages: rows of the block table that share pages with others, rows
+// given up, pages moved to the front of the cache, and the copies that go with it.
+//
+// shares[p] counts the rows that hold page p beyond the first: 0 for a page of one row and
+// for a free one, so that page_tables, which knows no shares, leaves them right.
+#pragma once
+
+#include "attend.hpp"
+
+namespace slnr {
+namespace paged {
+
+constexpr int kLifeBlock = 256;
+
+struct ForkArgs {
+  const int32_t *parents, *children;  // [n]
+  int32_t *table;                     // [R][W]
+  int64_t table_row;
+  int32_t *seq, *shares;              // [R], [pages]
+  const int32_t *free_pages;          // [F]
+  int32_t *pairs, *counts;            // [n][2], [2]
+  int32_t n, R, W, F, pages, shift;
+};
+
+__device__ __forceinline__ bool is_page(int page, int pages) { return (unsigned)page < (unsigned)pages; }
+
+// A row's length, as far as its table goes.
+__device__ __forceinline__ int row_length(const int32_t *seq, int r, int W, int shift) {
+  const int64_t room = (int64_t)W << shift;
+  const int s = imax(seq[r], 0);
+  return s < room ? s : (int)room;
+}
+
+struct Fork {
+  int parent, child, length, last;  // child < 0: left out; last: the page that is not full, or -1
+};
+
+__device__ __forceinline__ Fork fork_of(const ForkArgs &a, int i) {
+  Fork f{a.parents[i], a.children[i], 0, -1};
+  if ((unsigned)f.parent >= (unsigned)a.R || (unsigned)f.child >= (unsigned)a.R || f.parent == f.child) {
+    f.child = -1;
+    return f;
+  }
+  f.length = row_length(a.seq, f.parent, a.W, a.shift);
+  if (f.length & ((1 << a.shift) - 1)) {
+    const int page = a.table[f.parent * a.table_row + (f.length >> a.shift)];
+    if (is_page(page, a.pages)) f.last = page;
+  }
+  return f;
+}
+
+__device__ __forceinline__ int block_sum(int x, int *shared) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = x;
+  __syncthreads();
+  x = 0;
+#pragma unroll
+  for (int w = 0; w < kLifeBlock / kWave; ++w) x += shared[w];
+  return x;
+}
+
+// A block takes `per` adjacent forks.  It counts the pages that the forks before them take from the
+// list by itself, so blocks do not wait for one another; then it copies one parent's row
+// after the other.  Latency: a parent, its length, its last page, its row, in turn.
+__global__ __launch_bounds__(kLifeBlock) void page_fork(ForkArgs a, int per) {
+  __shared__ int sums[kLifeBlock / kWave];
+  const int tid = threadIdx.x, P = 1 << a.shift;
+  const int first = blockIdx.x * per, last = imin(first + per, a.n);
+  int taken = 0;
+  for (int i = tid; i < first; i += kLifeBlock) taken += fork_of(a, i).last >= 0;
+  taken = block_sum(taken, sums);
+  for (int i = first; i < last; ++i) {
+    const Fork f = fork_of(a, i);
+    int fresh = -1;
+    if (f.last >= 0) {
+      if (taken < a.F) fresh = a.free_pages[taken];
+      if (!is_page(fresh, a.pages)) fresh = -1;
+      ++taken;
+    }
+    if (tid == 0) {
+      a.pairs[2 * (int64_t)i] = fresh < 0 ? -1 : f.last;
+      a.pairs[2 * (int64_t)i + 1] = fresh;
+    }
+    if (f.child < 0) continue;
+    const int32_t *from = a.table + f.parent * a.table_row;
+    int32_t *to = a.table + f.child * a.table_row;
+    const int full = f.length >> a.shift;
+    const bool part = f.length & (P - 1);
+    for (int j = tid; j < a.W; j += kLifeBlock) {
+      int page = -1;
+      if (j < full) {
+        page = from[j];
+        if (is_page(page, a.pages))
+          atomicAdd(a.shares + page, 1);
+        else
+          page = -1;
+      } else if (part && j == full) {
+        page = fresh;
+      }
+      to[j] = page;
+    }
+    if (tid == 0) a.seq[f.child] = f.length;
+  }
+  if (blockIdx.x == gridDim.x - 1) {  // it has counted them all
+    int lost = 0;
+    for (int k = tid; k < taken; k += kLifeBlock) lost += k >= a.F || !is_page(a.free_pages[k], a.pages);
+    lost = block_sum(lost, sums);
+    if (tid == 0) a.counts[0] = taken, a.counts[1] = lost;
+  }
+}
+
+// -------------------------------------------------------------- sets of pages
+//
+// Rows given up and rows in use mark pages in a bitmap, which is then gone through in the order of the pages: that
+// order, and not the one in which blocks ran, is the order of what the calls hand out.
+
+typedef unsigned long long Word;  // 64 pages
+
+struct LifeArgs {
+  const int32_t *rows;  // [n] (free)
+  int32_t *table;       // [R][W]
+  int64_t table_row;
+  int32_t *seq, *shares;  // [R], [pages]
+  int32_t *out, *counts;  // freed pages [most], or pairs [most][2]; counts [2]
+  Word *marks;            // [words]
+  int32_t *rank;          // [pages] (compact): number of a page among those that move
+  int64_t words;
+  int32_t n, R, W, pages, shift, most;
+};
+
+__global__ __launch_bounds__(kLifeBlock) void life_clear(LifeArgs a, int64_t outs) {
+  const int64_t i0 = (int64_t)blockIdx.x * kLifeBlock + threadIdx.x, step = (int64_t)gridDim.x * kLifeBlock;
+  for (int64_t i = i0; i < a.words; i += step) a.marks[i] = 0;
+  for (int64_t i = i0; i < outs; i += step) a.out[i] = -1;
+  if (i0 < 2) a.counts[i0] = 0;
+}
+
+__device__ __forceinline__ void mark(Word *marks, int page) { atomicOr(marks + (page >> 6), (Word)1 << (page & 63)); }
+
+// Blocks take rows along x and their entries along y.  An entry is taken by an exchange, so a row named
+// twice is given up once.
+__global__ __launch_bounds__(kLifeBlock) void page_free_rows(LifeArgs a) {
+  __shared__ int sums[kLifeBlock / kWave];
+  int given = 0;
+  for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
+    const int r = a.rows[i];
+    if ((unsigned)r >= (unsigned)a.R) continue;
+    const int held = (int)(((int64_t)row_length(a.seq, r, a.W, a.shift) + (1 << a.shift) - 1) >> a.shift);
+    for (int j = blockIdx.y * kLifeBlock + threadIdx.x; j < held; j += gridDim.y * kLifeBlock) {
+      const int page = atomicExch(a.table + r * a.table_row + j, -1);
+      if (!is_page(page, a.pages)) continue;
+      ++given;
+      if (atomicSub(a.shares + page, 1) <= 0) mark(a.marks, page);
+    }
+  }
+  given = block_sum(given, sums);
+  if (threadIdx.x == 0 && given) atomicAdd(a.counts + 1, given);
+}
+
+__global__ __launch_bounds__(kLifeBlock) void page_mark_used(LifeArgs a) {
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    const int held = (int)(((int64_t)row_length(a.seq, r, a.W, a.shift) + (1 << a.shift) - 1) >> a.shift);
+    for (int j = blockIdx.y * kLifeBlock + threadIdx.x; j < held; j += gridDim.y * kLifeBlock) {
+      const int page = a.table[r * a.table_row + j];
+      if (is_page(page, a.pages)) mark(a.marks, page);
+    }
+  }
+}
+
+// How many of the pages below `end` are marked, counted by the whole block.
+__device__ __forceinline__ int marked_below(const LifeArgs &a, int64_t end, int *sums) {
+  int x = 0;
+  for (int64_t i = threadIdx.x; i < (end >> 6); i += kLifeBlock) x += __popcll(a.marks[i]);
+  if (threadIdx.x == 0 && (end & 63)) x += __popcll(a.marks[end >> 6] & (((Word)1 << (end & 63)) - 1));
+  return block_sum(x, sums);
+}
+
+// Goes through the marks of a block's share of the words: visit(page, marked, marked pages before it), a lane a
+// page, 64 at a time.
+template <class F>
+__device__ __forceinline__ void for_pages(const LifeArgs &a, int64_t w0, int64_t w1, int before, int *sums, F visit) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int64_t w = w0; w < w1; w += kLifeBlock) {
+    const int64_t i = w + threadIdx.x;
+    const Word bits = i < w1 ? a.marks[i] : 0;
+    int upto = __popcll(bits);
+    const int mine = upto;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(upto, o);
+      if (lane >= o) upto += x;
+    }
+    __syncthreads();
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int k = 0; k < kLifeBlock / kWave; ++k) {
+      if (k < wave) upto += sums[k];
+      all += sums[k];
+    }
+    const int start = before + upto - mine;
+    for (int k = 0; k < kWave && w + wave * kWave + k < w1; ++k) {
+      const Word b = __shfl(bits, k);
+      const int at = __shfl(start, k);
+      const int64_t page = (w + wave * kWave + k) * 64 + lane;
+      if (page < a.pages) visit((int)page, (bool)((b >> lane) & 1), at + __popcll(b & (((Word)1 << lane) - 1)));
+    }
+    before += all;
+  }
+}
+
+// Words of a block: all blocks together take them all.
+__device__ __forceinline__ void share_of(const LifeArgs &a, int64_t *w0, int64_t *w1) {
+  const int64_t per = (a.words + gridDim.x - 1) / gridDim.x;
+  *w0 = blockIdx.x * per < a.words ? blockIdx.x * per : a.words;
+  *w1 = *w0 + per < a.words ? *w0 + per : a.words;
+}
+
+__global__ __launch_bounds__(kLifeBlock) void page_free_list(LifeArgs a) {
+  __shared__ int sums[kLifeBlock / kWave];
+  int64_t w0, w1;
+  share_of(a, &w0, &w1);
+  const int before = marked_below(a, w0 * 64, sums);
+  for_pages(a, w0, w1, before, sums, [&](int page, bool marked, int rank) {
+    if (!marked) return;
+    a.shares[page] = 0;
+    if (rank < a.most) a.out[rank] = page;
+  });
+  for (int i = blockIdx.x * kLifeBlock + threadIdx.x; i < a.n; i += gridDim.x * kLifeBlock) {
+    const int r = a.rows[i];
+    if ((unsigned)r < (unsigned)a.R) a.seq[r] = 0;
+  }
+  if (blockIdx.x == gridDim.x - 1) {
+    const int all = marked_below(a, a.pages, sums);
+    if (threadIdx.x == 0) a.counts[0] = all;
+  }
+}
+
+// The k-th page in use at or behind the place where they would all end goes to the k-th
+// hole before it.
+__global__ __launch_bounds__(kLifeBlock) void page_compact_pairs(LifeArgs a) {
+  __shared__ int sums[kLifeBlock / kWave];
+  int64_t w0, w1;
+  share_of(a, &w0, &w1);
+  const int used = marked_below(a, a.pages, sums), stay = marked_below(a, used, sums);
+  const int before = marked_below(a, w0 * 64, sums);
+  for_pages(a, w0, w1, before, sums, [&](int page, bool marked, int rank) {
+    if (marked && page >= used) {
+      a.out[2 * (int64_t)(rank - stay)] = page;
+      a.rank[page] = rank - stay;
+    } else if (!marked && page < used) {
+      a.out[2 * (int64_t)(page - rank) + 1] = page;
+    }
+  });
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.counts[0] = used, a.counts[1] = used - stay;
+}
+
+__global__ __launch_bounds__(kLifeBlock) void page_compact_tables(LifeArgs a) {
+  const int used = a.counts[0], moves = a.counts[1];
+  for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
+    const int held = (int)(((int64_t)row_length(a.seq, r, a.W, a.shift) + (1 << a.shift) - 1) >> a.shift);
+    for (int j = blockIdx.y * kLifeBlock + threadIdx.x; j < held; j += gridDim.y * kLifeBlock) {
+      const int page = a.table[r * a.table_row + j];
+      if (is_page(page, a.pages) && page >= used)
+        a.table[r * a.table_row + j] = a.out[2 * (int64_t)a.rank[page] + 1];
+    }
+  }
+  const int blocks = gridDim.x * gridDim.y, block = blockIdx.y * gridDim.x + blockIdx.x;
+  for (int k = block * kLifeBlock + threadIdx.x; k < moves; k += blocks * kLifeBlock) {
+    const int from = a.out[2 * (int64_t)k], to = a.out[2 * (int64_t)k + 1];
+    a.shares[to] = a.shares[from];
+    a.shares[from] = 0;
+  }
+}
+
+// -------------------------------------------------------------------- copies
+
+constexpr int kCopyArrays = 8;
+constexpr int kCopyBytes = 16384;  // of a block's step
+
+struct CopyArray {
+  uint8_t *data;
+  int64_t page, outer_stride, inner_stride;  // bytes
+  int64_t bytes;                             // of a page
+  unsigned row, inner;                       // bytes of a row, rows of an inner run
+  int unit;                                  // bytes moved at once: 16, 4 or 1
+  int steps;                                 // of kCopyBytes
+  int dense;                                 // a page's bytes are adjacent
+};
+
+struct CopyArgs {
+  CopyArray array[kCopyArrays];
+  const int32_t *pairs;  // [n][2]
+  int64_t items;         // steps of all pairs
+  int32_t n, arrays, pages, steps;
+};
+
+template <class V>
+__device__ __forceinline__ void copy_step(const CopyArray &x, int from, int to, int64_t first) {
+  const uint8_t *src = x.data + from * x.page;
+  uint8_t *dst = x.data + to * x.page;
+  const int64_t last = first + kCopyBytes < x.bytes ? first + kCopyBytes : x.bytes;
+  constexpr int kMany = 4;
+  for (int64_t at = first + threadIdx.x * (int64_t)sizeof(V); at < last; at += kLifeBlock * (int64_t)sizeof(V) * kMany) {
+    V v[kMany];
+    int64_t off[kMany];
+#pragma unroll
+    for (int k = 0; k < kMany; ++k) {
+      const int64_t i = at + k * kLifeBlock * (int64_t)sizeof(V);
+      off[k] = i;
+      if (!x.dense) {
+        const int64_t row = i / x.row, outer = row / x.inner;
+        off[k] = outer * x.outer_stride + (row - outer * x.inner) * x.inner_stride + (i - row * x.row);
+      }
+      if (i < last) v[k] = *(const __attribute__((address_space(1))) V *)(src + off[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kMany; ++k)
+      if (at + k * kLifeBlock * (int64_t)sizeof(V) < last) *(__attribute__((address_space(1))) V *)(dst + off[k]) = v[k];
+  }
+}
+
+// A block takes 16 KB of a page of one array at a time; four 16-byte loads a thread are on their way.
+__global__ __launch_bounds__(kLifeBlock) void page_copy(CopyArgs a) {
+  for (int64_t item = blockIdx.x; item < a.items; item += gridDim.x) {
+    const int64_t i = item / a.steps;
+    int s = (int)(item - i * a.steps);
+    const int from = a.pairs[2 * i], to = a.pairs[2 * i + 1];
+    if (!is_page(from, a.pages) || !is_page(to, a.pages) || from == to) continue;
+    int k = 0;
+    while (k < a.arrays - 1 && s >= a.array[k].steps) s -= a.array[k++].steps;
+    const CopyArray &x = a.array[k];
+    const int64_t first = (int64_t)s * kCopyBytes;
+    if (x.unit == 16)
+      copy_step<u32x4>(x, from, to, first);
+    else if (x.unit == 4)
+      copy_step<unsigned>(x, from, to, first);
+    else
+      copy_step<uint8_t>(x, from, to, first);
+  }
+}
+
+}  // namespace paged
+}  // namespace slnr

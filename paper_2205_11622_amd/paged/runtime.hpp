@@ -11,8 +11,8 @@
 namespace slnr {
 
 // Workspace slots of these operators (0 to 2 belong to the sparse products).
-// Attention by pages grows with its call, so it has a slot of its own.
-enum WorkspaceSlot { kSlotAttend = 3, kSlotPages = 4 };
+// Attention by pages grows with its call, and so do the sets of pages: they have slots of their own.
+enum WorkspaceSlot { kSlotAttend = 3, kSlotPages = 4, kSlotLife = 5 };
 
 int hip_error(hipError_t e);  // records e for the calling thread; SPARSELNR_ERR_HIP
 int this_device(int *dev);

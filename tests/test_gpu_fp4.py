@@ -1,0 +1,410 @@
+"""The 4-bit cache on the GPU against its definitions in 64 bits."""
+import math
+import random
+
+import pytest
+import torch
+
+import paper_2205_11622_amd as slnr
+from tests import fp4_util as fu
+from tests import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+
+
+# ------------------------------------------------------------ rows in and out
+
+
+def rows(T, H, D, dtype, seed):
+    """K and V rows as slices of one projection, of very different size, with borders of the format among them."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, 2 * H + 1, D, generator=g) * torch.randn(T, 2 * H + 1, 1, generator=g).mul(2).exp()
+    if T > 4:
+        ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0])
+        for t, f in ((1, 1.0), (2, -0.125), (3, 64.0)):
+            x[t, :, :8] = ties * f  # every value between two codes
+            x[t, :, 8:] = 0.0
+        x[4] = 0.0
+    return x.to(dtype)
+
+
+def place(T, pages, P, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randperm(pages * P, generator=g)[:T]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D", [8, 32, 40, 64, 80, 128, 136, 256])
+@pytest.mark.parametrize("order", ["slots", "heads", "padded"])
+def test_rows_are_what_the_definition_gives(gpu, dtype, D, order):
+    T, H, P, pages = 37, 3, 8, 9
+    x = rows(T, H, D, dtype, D)
+    k, v = x[:, :H], x[:, H + 1:]
+    slots = place(T, pages, P, D)
+    slots[5], slots[9] = -1, pages * P  # left out
+    n = -(-D // 32)
+    old = torch.randint(0, 256, (2, pages, P, H, 16 * n), dtype=torch.uint8)
+    old_s = torch.randint(0, 256, (2, pages, P, H, n), dtype=torch.uint8)
+    want, want_s = old.clone(), old_s.clone()
+    for i, part in enumerate((k, v)):
+        c, e = fu.quantise(part)
+        for t in range(T):
+            if 0 <= slots[t] < pages * P:
+                want[i].view(-1, H, 16 * n)[slots[t]], want_s[i].view(-1, H, n)[slots[t]] = c[t], e[t]
+    cache = [fu.Batch4.ordered(a, order) for a in (*old, *old_s)]
+    at = [fu.Batch4._put(a, gpu) for a in cache]
+    put = x.to(gpu)
+    slnr.sparselnr_cache_append_fp4(put[:, :H], put[:, H + 1:], slots.to(gpu), at[0], at[1], at[2], at[3])
+    for got, w in zip(at, (*want, *want_s)):
+        assert torch.equal(got.cpu(), w)
+    rk, rv = slnr.sparselnr_cache_read_fp4(slots.to(gpu), *at, D, dtype)
+    for i, (got, part) in enumerate(((rk, k), (rv, v))):
+        assert got.dtype == dtype and got.shape == (T, H, D)
+        c, e = fu.quantise(part)
+        stand = fu.stand_for(c, e, D)
+        stand[5] = stand[9] = 0.0
+        assert torch.equal(got.cpu().double(), stand)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+def test_the_ends_of_the_types(gpu, dtype):
+    """Infinities, NaN, subnormals and the largest numbers."""
+    info = torch.finfo(dtype)
+    tiny = info.smallest_normal * (2.0 ** -23 if dtype == FP32 else info.eps)
+    values = [info.max, -info.max, info.max * 0.88, info.max / 2, info.smallest_normal, tiny, 3 * tiny, -tiny, math.inf,
+              -math.inf, math.nan, 0.0, -0.0, 1.0]
+    x = torch.zeros(len(values), 1, 64, dtype=torch.float64)
+    for i, y in enumerate(values):
+        x[i, 0, 3], x[i, 0, 7], x[i, 0, 40] = y, y / 4, 1.0
+    x = x.to(dtype)
+    T = len(values)
+    at = [torch.zeros(2, 8, 1, n, dtype=torch.uint8, device=gpu) for n in (32, 32, 2, 2)]
+    slots = torch.arange(T, device=gpu)
+    slnr.sparselnr_cache_append_fp4(x.to(gpu), x.to(gpu), slots, *at)
+    c, e = fu.quantise(x)
+    assert torch.equal(at[0].view(-1, 1, 32)[:T].cpu(), c) and torch.equal(at[3].view(-1, 1, 2)[:T].cpu(), e)
+    k, v = slnr.sparselnr_cache_read_fp4(slots, *at, 64, dtype)
+    stand = fu.stand_for(c, e, 64)
+    assert torch.equal(k.cpu().double().nan_to_num(5.0), stand.nan_to_num(5.0)) and torch.equal(k.isnan(), v.isnan())
+    assert k[8:11, 0, :32].isnan().all() and not k[:8].isnan().any() and not k[:, :, 32:].isnan().any()
+    assert torch.isfinite(k[:8]).all()
+
+
+@pytest.mark.parametrize("T,H", [(0, 2), (1, 1), (1, 8), (3000, 5)])
+def test_numbers_of_tokens(gpu, T, H):
+    x = rows(T, H, 64, BF16, 3)
+    pages = max(T, 1) // 16 + 1
+    at = [torch.zeros(pages, 16, H, n, dtype=torch.uint8, device=gpu) for n in (32, 32, 2, 2)]
+    slots = place(T, pages, 16, 1)
+    up = x.to(gpu)
+    slnr.sparselnr_cache_append_fp4(up[:, :H], up[:, H + 1:], slots.to(gpu), *at)
+    c, e = fu.quantise(x[:, :H])
+    assert torch.equal(at[0].view(-1, H, 32)[slots].cpu(), c) and torch.equal(at[2].view(-1, H, 2)[slots].cpu(), e)
+    k, _ = slnr.sparselnr_cache_read_fp4(slots.to(gpu), *at, 64, BF16)
+    assert torch.equal(k.cpu().double(), fu.stand_for(c, e, 64))
+    twice = slots.to(gpu).repeat(2)
+    k2, _ = slnr.sparselnr_cache_read_fp4(twice, *at, 64, BF16)
+    assert torch.equal(k2[:T], k) and torch.equal(k2[T:], k)
+
+
+# ------------------------------------------------------------- attention
+
+
+def run_attention(b, gpu, window=0, max_new=0, scale=None, with_lse=True, fill=0):
+    q, kc, vc, ks, vs, table, seq, qptr = b.upload(gpu)
+    lse = torch.full(q.shape[:2], math.nan, device=gpu) if with_lse else None
+    out = torch.full(q.shape, fill, dtype=q.dtype, device=gpu)
+    got = slnr.sparselnr_paged_attention_fp4(q, kc, vc, ks, vs, table, seq, qptr, scale=scale, window=window,
+                                             max_new=max_new, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert got is out
+    return out.cpu(), lse
+
+
+def compare(b, gpu, window=0, max_new=0, scale=None, logits=8.0):
+    out, lse = run_attention(b, gpu, window, max_new, scale)
+    fu.check(b, out, lse, b.reference(scale, window), scale, logits)
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D", [8, 32, 64, 72, 96, 128, 136, 200, 256])
+@pytest.mark.parametrize("P", [16, 64])
+def test_decode_types_and_widths(gpu, dtype, D, P):
+    b = fu.Batch4([0, 1, 15, 16, 17, 63, 200, 333], [1] * 8, 6, 2, D, P, dtype, seed=D)
+    compare(b, gpu, max_new=1)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D", [8, 32, 64, 72, 96, 128, 136, 200, 256])
+@pytest.mark.parametrize("P", [32, 64])
+def test_chunk_types_and_widths(gpu, dtype, D, P):
+    b = fu.Batch4([0, 5, 130], [70, 1, 301], 4, 2, D, P, dtype, seed=D + 1)
+    compare(b, gpu)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (3, 3), (5, 1), (7, 1), (12, 4), (16, 2), (17, 1), (40, 2), (64, 1), (128, 1)])
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_head_layouts(gpu, Hq, Hkv, new):
+    b = fu.Batch4([100, 0, 37], [new, 1, new], Hq, Hkv, 64, 16, BF16, seed=Hq)
+    compare(b, gpu, max_new=max(new, 1))
+
+
+@pytest.mark.parametrize("P", [1, 2, 8, 16, 64, 128, 1024])
+@pytest.mark.parametrize("order,scale_order", [("slots", "slots"), ("heads", "heads"), ("pairs", "heads"), ("padded", "padded"),
+                                               ("heads", "slots")])
+def test_page_sizes_and_orders(gpu, P, order, scale_order):
+    b = fu.Batch4([0, 130, 65], [1, 2, 140], 8, 2, 64, P, BF16, seed=P, order=order, scale_order=scale_order)
+    compare(b, gpu)
+
+
+@pytest.mark.parametrize("window", [1, 2, 31, 64, 100, 5000])
+@pytest.mark.parametrize("new", [1, 5, 150])
+@pytest.mark.parametrize("P", [16, 128])
+def test_windows(gpu, window, new, P):
+    b = fu.Batch4([0, 3, 400], [new, new, new], 4, 2, 96, P, FP16, seed=window)
+    compare(b, gpu, window=window)
+
+
+def test_requests_without_tokens_and_lengths_of_none(gpu):
+    b = fu.Batch4([0, 7, 0, 0, 20], [0, 0, 1, 0, 2], 4, 1, 64, 16, BF16, seed=2)
+    compare(b, gpu)
+    b = fu.Batch4([4, 9], [0, 0], 4, 1, 64, 16, BF16, seed=2)
+    out, _ = run_attention(b, gpu)
+    assert out.shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("new", [1, 4, 90])
+@pytest.mark.parametrize("P", [16, 64])
+def test_pages_that_are_not_there(gpu, new, P):
+    b = fu.Batch4([300, 64, 10], [new] * 3, 8, 2, 64, P, BF16, seed=5)
+    for j in (0, 3, 4):
+        b.table[0][j] = -1
+    b.table[1] = [-1] * len(b.table[1])  # nothing left: empty rows
+    b.table[2][0] = b.kc.shape[0]        # past the cache
+    out, lse = compare(b, gpu)
+    a, e = b.qptr[1], b.qptr[2]
+    assert (out[a:e] == 0).all() and (lse[a:e] == -math.inf).all()
+
+
+def test_a_cache_without_pages(gpu):
+    b = fu.Batch4([10], [2], 4, 2, 64, 64, BF16, seed=5)
+    q, kc, vc, ks, vs, table, seq, qptr = b.upload(gpu)
+    for n in (2, 40):
+        q = torch.ones(n, 4, 64, dtype=BF16, device=gpu)
+        out = slnr.sparselnr_paged_attention_fp4(q, kc[:0], vc[:0], ks[:0], vs[:0], table, b.ints([n + 10], gpu),
+                                                 b.ints([0, n], gpu))
+        assert (out == 0).all()
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_lengths_that_do_not_fit_stay_in_bounds(gpu, new):
+    """seq_len past the table's row ends there; more new tokens than positions: the first see nothing."""
+    b = fu.Batch4([40, 40], [new, new], 4, 2, 64, 16, FP32, seed=6, extra_w=0)
+    for name in ("ks", "vs"):
+        b.bytes[name][b.bytes[name] == 255] = 120
+    b.refresh()
+    q, kc, vc, ks, vs, table, seq, qptr = b.upload(gpu)
+    W = table.shape[1]
+    big = torch.tensor([2 ** 31 - 1, b.seq[1]], dtype=torch.int32, device=gpu)
+    out = slnr.sparselnr_paged_attention_fp4(q, kc, vc, ks, vs, table, big, qptr).cpu()
+    b.seq[0] = W * 16
+    fu.check(b, out, None, b.reference())
+    one = torch.tensor([1, 1], dtype=torch.int32, device=gpu)
+    lse = torch.empty(q.shape[:2], device=gpu)
+    out = slnr.sparselnr_paged_attention_fp4(q, kc, vc, ks, vs, table, one, qptr, lse=lse).cpu()
+    for r in range(2):
+        a, e = b.qptr[r], b.qptr[r + 1]
+        assert (out[a:e - 1] == 0).all() and (lse[a:e - 1] == -math.inf).all()
+        v = b.vc[b.table[r][0], 0].repeat_interleave(2, 0)
+        assert torch.equal(out[e - 1].double(), v)  # one key: its value
+
+
+@pytest.mark.parametrize("what", ["tokens past T", "backwards", "negative"])
+def test_offsets_that_do_not_fit_stay_in_bounds(gpu, what):
+    b = fu.Batch4([30, 30], [3, 3], 4, 2, 64, 16, BF16, seed=7)
+    q, *cache, table, seq, _ = b.upload(gpu)
+    qptr = {"tokens past T": [0, 3, 100], "backwards": [0, 6, 3], "negative": [-5, 3, 6]}[what]
+    out = torch.full(q.shape, 7.0, dtype=BF16, device=gpu)
+    slnr.sparselnr_paged_attention_fp4(q, *cache, table, seq, b.ints(qptr, gpu), out=out)
+    torch.cuda.synchronize()
+
+
+def test_rows_of_no_request_are_left(gpu):
+    b = fu.Batch4([30, 5], [2, 100], 4, 2, 64, 16, BF16, seed=8)
+    b.q = torch.cat([b.q, b.q[:5]])
+    out, _ = run_attention(b, gpu, with_lse=False, fill=7)
+    assert (out[102:] == 7).all() and not (out[:102] == 7).all(dim=2).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("new", [3, 9, 130])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("P", [16, 64])
+def test_nan_where_a_query_does_not_look(gpu, dtype, new, window, P):
+    """A NaN group of the newest tokens reaches those that see it, in its columns, and no other."""
+    b = fu.Batch4([61, 0], [new, new], 4, 2, 96, P, dtype, seed=9)
+    ref, _, _ = b.reference(window=window)
+    S, old = b.seq[0], 4
+
+    def at(j):
+        return b.table[0][j // P], j % P
+    for j, g in ((S - 1, 2), (S - 2, 1)):
+        b.bytes["vs"][(*at(j), slice(None), g)] = 255
+    if window:  # one that only the first tokens still see
+        b.bytes["vs"][(*at(old), slice(None), 0)] = 255
+    b.bytes["ks"][(*at(S - 1), 1, 1)] = 255  # key of the last token, second head
+    out, _ = run_attention(b, gpu, window=window)
+    for i, p in enumerate(range(61, S)):
+        o = out[i].double()
+        assert torch.isnan(o[2:]).all() == (p == S - 1)
+        for h in range(0, 2 if p == S - 1 else 4):
+            seen = [window > 0 and p - old < window, p >= S - 2, p >= S - 1]
+            for g in range(3):
+                got = o[h, 32 * g:32 * g + 32]
+                assert got.isnan().all() if seen[g] else (got - ref[i, h, 32 * g:32 * g + 32]).abs().max() < 0.05, (i, h, g)
+    assert (out[new:].double() - ref[new:]).abs().max() < 0.05
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("new", [1, 80])
+def test_a_query_that_is_not_finite(gpu, dtype, new):
+    b = fu.Batch4([100], [new], 4, 2, 64, 16, dtype, seed=12)
+    q = b.q.clone()
+    q[0, 1, 5], q[new - 1, 2, 40] = math.inf, math.nan
+    b.q = q
+    out, lse = run_attention(b, gpu)
+    bad = torch.zeros(new, 4, dtype=torch.bool)
+    bad[0, 1] = bad[new - 1, 2] = True
+    assert torch.equal(out.isnan().all(2), bad) and torch.equal(out.isnan().any(2), bad) and torch.equal(lse.isnan().cpu(), bad)
+
+
+def test_scores_of_any_size(gpu):
+    """Large scores (one key takes all), a scale that makes all weights alike, queries of very different size."""
+    b = fu.Batch4([200, 90], [1, 80], 4, 2, 64, 16, FP32, seed=10, amp=60.0)
+    out, _ = run_attention(b, gpu)
+    ref, _, _ = b.reference()
+    # scores up to about 2000, off by 64 * 2^-24 of the sum of their terms' magnitudes and the pieces' 2^-23: < 0.05
+    assert (out.double() - ref).abs().max() < 0.15
+    b = fu.Batch4([200, 90], [1, 80], 4, 2, 64, 16, BF16, seed=10)
+    compare(b, gpu, scale=1e-6)
+    for dtype in (BF16, FP32):
+        b = fu.Batch4([200, 90], [1, 80], 4, 2, 64, 16, dtype, seed=10)
+        b.q = (b.q.float() * torch.logspace(-30, 0, b.q.shape[0])[:, None, None]).to(dtype)
+        compare(b, gpu)
+    b.q = torch.zeros_like(b.q)
+    compare(b, gpu)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("ctx,new", [(9000, 1), (20011, 1), (9000, 3), (3000, 60), (2500, 170)])
+@pytest.mark.parametrize("P", [32, 64])
+def test_long_contexts_are_cut_and_joined(gpu, dtype, ctx, new, P):
+    b = fu.Batch4([ctx], [new], 4, 2, 64, P, dtype, seed=11)
+    compare(b, gpu, max_new=new)
+
+
+def test_chunks_of_wide_heads_in_every_type(gpu):
+    for dtype in (BF16, FP16, FP32):
+        b = fu.Batch4([700, 40], [300, 65], 6, 2, 256, 64, dtype, seed=13)
+        compare(b, gpu)
+
+
+def test_one_long_request_among_many_short_ones(gpu):
+    rng = random.Random(3)
+    ctx = [rng.randrange(0, 40) for _ in range(700)]
+    new = [rng.choice([0, 1, 1, 2]) for _ in range(700)]
+    ctx[333], new[333] = 6000, 40
+    b = fu.Batch4(ctx, new, 4, 2, 64, 16, BF16, seed=4)
+    compare(b, gpu)
+
+
+@pytest.mark.parametrize("max_new", [0, 1, 50, 1000])
+def test_the_hint_changes_nothing_but_kernels(gpu, max_new):
+    b = fu.Batch4([900, 12, 64], [1, 50, 9], 8, 2, 128, 64, FP16, seed=14)
+    compare(b, gpu, max_new=max_new)
+
+
+def test_a_cache_past_32_bits(gpu):
+    """Pages whose bytes lie beyond 4 GiB."""
+    P, H, D, pages = 64, 8, 128, 150000
+    small = fu.Batch4([500, 90], [1, 40], 16, H, D, P, BF16, seed=15)
+    n = small.kc.shape[0]
+    q, kc, vc, ks, vs, table, seq, qptr = small.upload(gpu)
+    at = torch.linspace(0, pages - 1, n, device=gpu).long()
+    big = []
+    for x in (kc, vc, ks, vs):
+        y = torch.empty(pages, *x.shape[1:], dtype=torch.uint8, device=gpu)
+        y[at] = x
+        big.append(y)
+    assert big[0].numel() > 2 ** 32
+    moved = torch.where(table >= 0, at[table.clamp(min=0).long()].int(), -1).contiguous()
+    out = slnr.sparselnr_paged_attention_fp4(q, *big, moved, seq, qptr)
+    want = slnr.sparselnr_paged_attention_fp4(q, kc, vc, ks, vs, table, seq, qptr)
+    assert torch.equal(out, want)
+    slots = (at[-3:] * P + 5).contiguous()
+    x = torch.randn(3, H, D, device=gpu).to(BF16)
+    slnr.sparselnr_cache_append_fp4(x, x, slots, *big)
+    k, v = slnr.sparselnr_cache_read_fp4(slots, *big, D, BF16)
+    c, e = fu.quantise(x.cpu())
+    assert torch.equal(k.cpu().double(), fu.stand_for(c, e, D)) and torch.equal(k, v)
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_same_bits_again_and_on_another_stream(gpu, new):
+    b = fu.Batch4([5000, 333, 64], [new, 1, new], 8, 2, 128, 64, BF16, seed=16)
+    up = b.upload(gpu)
+    want = slnr.sparselnr_paged_attention_fp4(*up)
+    assert torch.equal(want, slnr.sparselnr_paged_attention_fp4(*up))
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    out = torch.empty_like(want)
+    slnr.sparselnr_paged_attention_fp4(*up, out=out, stream=stream)
+    stream.synchronize()
+    assert torch.equal(out, want)
+    with torch.cuda.stream(stream):
+        got = slnr.sparselnr_paged_attention_fp4(*up)
+    stream.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_a_captured_step_beside_eager_calls(gpu):
+    """Append and attention of a step, captured after one eager step, replayed between calls of other sizes."""
+    b = fu.Batch4([4000, 90], [2, 2], 8, 2, 128, 64, BF16, seed=17)
+    big = fu.Batch4([700], [900], 8, 8, 128, 64, BF16, seed=18)
+    q, kc, vc, ks, vs, table, seq, qptr = b.upload(gpu)
+    up = big.upload(gpu)
+    slots = torch.tensor([b.table[r][p // 64] * 64 + p % 64 for r, s in enumerate(b.seq) for p in (s - 2, s - 1)],
+                         device=gpu)
+    new = torch.randn(4, 2, 128, device=gpu, generator=torch.Generator(device=gpu).manual_seed(2)).to(BF16)
+    stream = torch.cuda.Stream()
+
+    def step():
+        slnr.sparselnr_cache_append_fp4(new, new, slots, kc, vc, ks, vs)
+        return slnr.sparselnr_paged_attention_fp4(q, kc, vc, ks, vs, table, seq, qptr)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step()
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = step()
+    with torch.cuda.stream(stream):
+        for i in range(3):
+            q.normal_()
+            new.normal_()
+            graph.replay()
+            slnr.sparselnr_paged_attention_fp4(*up)
+            out.zero_()
+            graph.replay()
+            got = out.clone()
+            want = step()
+            stream.synchronize()
+            assert torch.equal(got, want), i
+    b.q = q.cpu()
+    for name, x in zip(("k", "v", "ks", "vs"), (kc, vc, ks, vs)):
+        b.bytes[name] = x.cpu()
+    b.refresh()
+    fu.check(b, got.cpu(), None, b.reference())
