@@ -26,37 +26,113 @@ __device__ __forceinline__ void split_weight(float e, typename Type<V4>::Vec out
   }
 }
 
-// Loads from device memory: see load8_global.
+// Loads from device memory (see load8_global), and those of what is read once.
 template <class V>
 __device__ __forceinline__ V load_global(const uint8_t *p) {
   return *(const __attribute__((address_space(1))) V *)p;
 }
+template <class V>
+__device__ __forceinline__ V load_once(const uint8_t *p) {
+  return __builtin_nontemporal_load((const __attribute__((address_space(1))) V *)p);
+}
+
+// ------------------------------------------------------------- split of the work
+//
+// The steps of all tiles of a KV head, one request after the other, are one line of `all` steps that
+// `n` blocks share evenly, so that all end at the same time: block i takes the steps from all i / n to
+// all (i + 1) / n, which are the end of a tile, whole tiles and the beginning of one.  A tile that is
+// cut has pieces in the blocks i0 .. i1; the first is the last thing that block i0 does, the others are the first
+// thing that theirs do, so two places a block hold all pieces there are.
+template <int NT>
+struct Line {
+  long long before[NT];  // steps before this thread's requests
+  long long work[NT / kWave];
+};
+
+// The steps of a KV head.  count(r, tiles, steps) gives a request's tiles and the steps of each.
+template <int NT, class F>
+__device__ __forceinline__ long long line_scan(Line<NT> &sh, const AttendArgs &a, int per, F count) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int r0 = imin(tid * per, a.R), r1 = imin(r0 + per, a.R);
+  long long w = 0;
+  for (int r = r0; r < r1; ++r) {
+    int tiles, steps;
+    count(r, tiles, steps);
+    w += (long long)tiles * imax(steps, 1);
+  }
+  long long upto = w;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 63) sh.work[wave] = upto;
+  __syncthreads();
+  long long all = 0;
+#pragma unroll
+  for (int i = 0; i < NT / kWave; ++i) {
+    if (i < wave) upto += sh.work[i];
+    all += sh.work[i];
+  }
+  sh.before[tid] = upto - w;
+  __syncthreads();
+  return all;
+}
+
+// Whole numbers of a line: up to 2^28 rows of up to 2^23 steps, times n < 2^12, fit 64 bits.
+__device__ __forceinline__ int block_of(long long step, int n, long long all) {
+  return (int)(((step + 1) * n - 1) / all);
+}
 
 // --------------------------------------------------------------- few rows
 //
-// attend_few_fp4: as attend_few, a block of four waves takes one piece of a tile of 16 rows, here in tiles
-// of 64 keys a wave.  A lane loads 16 bytes of K, which are one group of a key and,
+// attend_few_fp4: as attend_few, tiles of 16 rows and blocks of four waves, each of which walks every fourth
+// tile of 64 keys.  A lane loads 16 bytes of K, which are one group of a key and,
 // with its exponent, an operand of a product over 128 dimensions; the query's pieces
 // are the other.  V goes through LDS 32 keys at a time.
 constexpr int kFew4Keys = 64;                        // of a wave's tile
 constexpr int kFew4Step = kFew4Keys * kFewWaves;     // of a block's step
 
+// A tile of V in LDS (see Tile) whose 16-byte chunks are permuted for reads of 16 columns: LDS moves 128 bytes
+// a cycle, which are two chunks of four rows in a read and one of eight rows in a write.  The permutation is an exclusive or and the same
+// 16 rows on, so a lane's addresses differ from its first ones in single bits.
+template <int DP>
+struct Tile16 {
+  static constexpr int kRowBytes = 2 * DP;
+  static __device__ __forceinline__ unsigned chunk(int row) {
+    return ((row & 3) << 1) | ((row >> 2) & 1) | (DP >= 128 ? row & 8 : 0);
+  }
+  // Columns column .. + 7 (a multiple of 8) of row `row` < 16; those 8 i on: ^ (i << 4).
+  static __device__ __forceinline__ unsigned write_first(int row, int column) {
+    return row * kRowBytes + (((column >> 3) ^ chunk(row)) << 4);
+  }
+  // Keys 4 (lane >> 4) .. + 3 of column lane & 15, by a transposing read; columns 16 i on: ^ (i << 5).
+  static __device__ __forceinline__ unsigned read_first(int lane) {
+    const int row = (lane >> 4) * 4 + ((lane >> 2) & 3), column = (lane & 3) * 4;
+    return row * kRowBytes + (((column >> 3) ^ chunk(row)) << 4) + (column & 7) * 2;
+  }
+};
+
 template <class T, int DP>
 struct Few4Shared {
   typedef typename Four<T>::V4 V4;
   union {
-    V4 v[kFewWaves][32 * Tile<V4, DP>::kStride];
+    alignas(512) V4 v[kFewWaves][32 * DP];
     float o[kFewWaves][kFewRows * DP];
   };
   float m[kFewWaves][kFewRows], l[kFewWaves][kFewRows];
-  Split<kFewBlock> split;
+  Line<kFewBlock> line;
 };
 
+// Blocks of a compute unit that the registers leave room for.
+template <class T, int DP>
+constexpr int kFew4PerCu = DP == 256 ? 1 : 2;
+
 template <class T, int DP, bool ONE_PAGE>
-__global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
+__global__ __launch_bounds__(kFewBlock, (kFew4PerCu<T, DP>)) void attend_few_fp4(AttendFp4Args a) {
   typedef typename Four<T>::V4 V4;
   typedef typename Type<V4>::Vec Vec;
-  typedef Tile<V4, DP> L;
+  typedef Tile16<DP> L;
   constexpr int NQ = Four<T>::kQ, NP = Four<T>::kP;
   constexpr int DT = DP / 16;               // tiles of output columns
   constexpr int KR = DP == 256 ? 2 : 1;     // operands of a key
@@ -66,7 +142,8 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
   extern __shared__ __align__(16) char raw[];
   Few4Shared<T, DP> &sh = *reinterpret_cast<Few4Shared<T, DP> *>(raw);
   const float sc = score_unit<T>(a);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // a scalar: so are its tiles, their addresses and conditions
   const int col = lane & 15, grp = lane >> 4;
   const int P = 1 << a.shift;
   auto count = [&](int r, int &tiles, int &steps) {
@@ -76,17 +153,49 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
     const int lo = (a.window ? imax(q.S - q.n - a.window + 1, 0) : 0) & -kFew4Keys;
     steps = (q.S - lo + kFew4Step - 1) / kFew4Step;
   };
-  split_scan<kFewBlock>(sh.split, a, 1, count);
-  const int total = sh.split.total;
-  if (blockIdx.x == 0 && tid == 0) a.meta[0] = sh.split.total_split * a.Hkv;
+  const int per = (a.R + kFewBlock - 1) / kFewBlock;
+  const long long all = line_scan<kFewBlock>(sh.line, a, per, count);
+  const int h = (int)(blockIdx.x % (unsigned)a.Hkv), me = (int)(blockIdx.x / (unsigned)a.Hkv);
+  const int blocks = (int)(gridDim.x / (unsigned)a.Hkv), n = all < blocks ? (int)all : blocks;
+  int32_t *record = a.meta + (int64_t)blockIdx.x * kMeta;  // of the tile that begins here and goes on in other blocks
+  if (tid == 0) record[0] = 0;
+  if (me >= n) return;
+  long long u = all * me / n;
+  const long long u_end = all * (me + 1) / n;
+  // the request of step u: of the last thread that begins at or before it
+  int r = 0, r_tiles, r_steps;
+  long long r_begin;
+  {
+    int x = 0, y = kFewBlock - 1;
+    while (x < y) {
+      const int mid = (x + y + 1) >> 1;
+      if (sh.line.before[mid] <= u)
+        x = mid;
+      else
+        y = mid - 1;
+    }
+    r = x * per;
+    r_begin = sh.line.before[x];
+  }
 
-  for (unsigned p = blockIdx.x; p < (unsigned)total * (unsigned)a.Hkv; p += gridDim.x) {
-    const int h = (int)(p % (unsigned)a.Hkv);
-    const Piece pc = split_find<kFewBlock>(sh.split, a, (int)(p / (unsigned)a.Hkv), count);
-    if (pc.r < 0) continue;
-    const int part = pc.part, np = pc.np, slot = pc.slot;
-    const Request rq = request_of(a, pc.r);
-    const int first = pc.tile * kFewRows;  // of the request's rows
+  for (; u < u_end && r < a.R;) {
+    count(r, r_tiles, r_steps);
+    const int units = imax(r_steps, 1);  // of a tile
+    if (u >= r_begin + (long long)r_tiles * units) {
+      r_begin += (long long)r_tiles * units;
+      ++r;
+      continue;
+    }
+    const int tile_of = (int)((u - r_begin) / units);
+    const long long begin = r_begin + (long long)tile_of * units;
+    const int from = (int)(u - begin), to = (int)(u_end - begin < units ? u_end - begin : units);
+    u = begin + to;
+    const bool split = from > 0 || to < units;
+    const int i0 = split ? block_of(begin, n, all) : me;
+    const int np = split ? block_of(begin + units - 1, n, all) - i0 + 1 : 1;
+    const int slot = !split ? -1 : 2 * me + (me == i0);
+    const Request rq = request_of(a, r);
+    const int first = tile_of * kFewRows;  // of the request's rows
     const int rows = imin(rq.n * a.G - first, kFewRows);
     const int row0 = rq.first * a.G + first;
     const int pos_first = rq.S - rq.n + first / a.G;
@@ -95,8 +204,8 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
     const int hi = imin(pos_last + 1, rq.S);
     const int tiles = hi > lo ? (hi - lo + kFew4Keys - 1) / kFew4Keys : 0;
     const int steps = (tiles + kFewWaves - 1) / kFewWaves;
-    const int s0 = (int)((long long)steps * part / np), s1 = (int)((long long)steps * (part + 1) / np);
-    const int32_t *table = a.table + (int64_t)pc.r * a.table_row;
+    const int s0 = (int)((long long)steps * from / units), s1 = (int)((long long)steps * to / units);
+    const int32_t *table = a.table + (int64_t)r * a.table_row;
 
     // ------------------------------------------------ the queries, as columns
     // Product m of a key's operand c has piece m / KR for 128 columns and more; for 64 the
@@ -136,6 +245,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
     }
 
     // ------------------------------------------------ walk of the keys
+    __builtin_amdgcn_sched_barrier(0);  // the first keys' registers are not wanted before: the pieces take many
     f32x4 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i) o[i] = f32x4{0, 0, 0, 0};
@@ -144,9 +254,9 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
     // Of 64 keys: 16 of each of four parts, four lanes a key.
     struct Keys {
       u32x4 k[4][KR];
-      unsigned k_scale[4][KR];
+      uint8_t k_scale[4][KR];  // bytes: made words where they are loaded, they would be waited for there
       unsigned v[4][VW];
-      unsigned v_scale[4][VS];
+      uint8_t v_scale[4][VS];
       unsigned long long live;  // bit: this key is there
     };
     // The page of key `lane` of a tile (ONE_PAGE: of all of them); -1 where there is none.
@@ -163,48 +273,44 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
     const int kg = DP == 64 ? grp & 1 : grp;  // this lane's group of the key's first operand
     const int v0 = grp * (DP / 4);            // this lane's first column of V
     const uint8_t *zero = (const uint8_t *)kZeroRow;
-    auto load = [&](Keys &x, int base, int found) {
+    // ONE_PAGE: a tile's address is a scalar, to which a lane adds 32 bits.  Rows that are not there are read
+    // from a page that is, and zeroed or not looked at: a load then has no condition.
+    const bool any = a.pages > 0;
+    const uint8_t *k_head = any ? (const uint8_t *)a.k + h * a.k_head : zero;
+    const uint8_t *v_head = any ? (const uint8_t *)a.v + h * a.v_head : zero;
+    const uint8_t *ks_head = any ? a.ks + h * a.ks_head : zero;
+    const uint8_t *vs_head = any ? a.vs + h * a.vs_head : zero;
+    const int k_row = any ? (int)a.k_slot : 0, v_row = any ? (int)a.v_slot : 0;
+    const int ks_row = any ? (int)a.ks_slot : 0, vs_row = any ? (int)a.vs_slot : 0;
+    unsigned k_at[KR], ks_at[KR], v_at[(VW + 3) / 4], vs_at[VS];
+    if constexpr (ONE_PAGE) {
+#pragma unroll
+      for (int c = 0; c < KR; ++c) {
+        const int g = kg + c * 4 < a.groups ? kg + c * 4 : 0;
+        k_at[c] = col * k_row + g * kGroupBytes, ks_at[c] = col * ks_row + g;
+      }
+#pragma unroll
+      for (int i = 0; i < (VW + 3) / 4; ++i) v_at[i] = col * v_row + (v0 + i * 32 < a.groups * kGroup ? v0 / 2 + i * 16 : 0);
+#pragma unroll
+      for (int i = 0; i < VS; ++i) vs_at[i] = col * vs_row + (v0 / kGroup + i < a.groups ? v0 / kGroup + i : 0);
+    }
+    auto load_k = [&](Keys &x, int base, int found) {
       if constexpr (ONE_PAGE) {
         const int page = __builtin_amdgcn_readfirstlane(found);
         const int keys = end - base;
         x.live = page < 0 ? 0 : keys >= kFew4Keys ? ~0ull : (1ull << keys) - 1;
-        const int64_t in = base & (P - 1);
-        const bool ok = page >= 0;
-        // rows of the page behind the last key are read too, and zeroed
-        const uint8_t *kp = ok ? (const uint8_t *)a.k + page * a.k_page + in * a.k_slot + h * a.k_head : zero;
-        const uint8_t *vp = ok ? (const uint8_t *)a.v + page * a.v_page + in * a.v_slot + h * a.v_head : zero;
-        const uint8_t *ksp = ok ? a.ks + page * a.ks_page + in * a.ks_slot + h * a.ks_head : zero;
-        const uint8_t *vsp = ok ? a.vs + page * a.vs_page + in * a.vs_slot + h * a.vs_head : zero;
-        const int k_row = ok ? (int)a.k_slot : 0, v_row = ok ? (int)a.v_slot : 0;
-        const int ks_row = ok ? (int)a.ks_slot : 0, vs_row = ok ? (int)a.vs_slot : 0;
+        const int in = base & (P - 1);
+        const int64_t pg = any ? imax(page, 0) : 0;
+        const uint8_t *kp = k_head + pg * a.k_page + (int64_t)in * k_row;
+        const uint8_t *ksp = ks_head + pg * a.ks_page + (int64_t)in * ks_row;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
 #pragma unroll
           for (int c = 0; c < KR; ++c) {
-            const int g = kg + c * 4;
-            const bool in_row = g < a.groups;
-            x.k[s][c] = load_global<u32x4>(kp + (unsigned)((s * 16 + col) * k_row + (in_row ? g * kGroupBytes : 0)));
-            x.k_scale[s][c] = load_global<uint8_t>(ksp + (unsigned)((s * 16 + col) * ks_row + (in_row ? g : 0)));
+            x.k[s][c] = load_once<u32x4>(kp + k_at[c]);
+            x.k_scale[s][c] = load_once<uint8_t>(ksp + ks_at[c]);
           }
-          const bool in_row = v0 < a.groups * kGroup;
-          const uint8_t *vr = vp + (unsigned)((s * 16 + col) * v_row + (in_row ? v0 / 2 : 0));
-          if constexpr (VW == 2) {
-            const u32x2 w = load_global<u32x2>(vr);
-            x.v[s][0] = w[0], x.v[s][1] = w[1];
-          } else {
-#pragma unroll
-            for (int i = 0; i < VW; i += 4) {
-              const bool there = DP < 256 || i == 0 || v0 + i * 8 < a.groups * kGroup;
-              const u32x4 w = load_global<u32x4>(vr + (there ? i * 4 : 0));
-#pragma unroll
-              for (int j = 0; j < 4; ++j) x.v[s][i + j] = w[j];
-            }
-          }
-#pragma unroll
-          for (int i = 0; i < VS; ++i) {
-            const int g = v0 / kGroup + i;
-            x.v_scale[s][i] = load_global<uint8_t>(vsp + (unsigned)((s * 16 + col) * vs_row + (g < a.groups ? g : 0)));
-          }
+          kp += 16 * k_row, ksp += 16 * ks_row;
         }
       } else {
         x.live = __builtin_amdgcn_ballot_w64(found >= 0);
@@ -214,23 +320,55 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
           const bool ok = page >= 0;
           const int64_t in = (base + s * 16 + col) & (P - 1);
           const uint8_t *kp = (const uint8_t *)a.k + page * a.k_page + in * a.k_slot + h * a.k_head;
-          const uint8_t *vp = (const uint8_t *)a.v + page * a.v_page + in * a.v_slot + h * a.v_head;
           const uint8_t *ksp = a.ks + page * a.ks_page + in * a.ks_slot + h * a.ks_head;
-          const uint8_t *vsp = a.vs + page * a.vs_page + in * a.vs_slot + h * a.vs_head;
 #pragma unroll
           for (int c = 0; c < KR; ++c) {
             const int g = kg + c * 4;
             const bool in_row = ok && g < a.groups;
-            x.k[s][c] = load_global<u32x4>(in_row ? kp + g * kGroupBytes : zero);
-            x.k_scale[s][c] = load_global<uint8_t>(in_row ? ksp + g : zero);
+            x.k[s][c] = load_once<u32x4>(in_row ? kp + g * kGroupBytes : zero);
+            x.k_scale[s][c] = load_once<uint8_t>(in_row ? ksp + g : zero);
           }
+        }
+      }
+    };
+    auto load_v = [&](Keys &x, int base, int found) {
+      if constexpr (ONE_PAGE) {
+        const int in = base & (P - 1);
+        const int64_t pg = any ? imax(__builtin_amdgcn_readfirstlane(found), 0) : 0;
+        const uint8_t *vp = v_head + pg * a.v_page + (int64_t)in * v_row;
+        const uint8_t *vsp = vs_head + pg * a.vs_page + (int64_t)in * vs_row;
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
           if constexpr (VW == 2) {
-            const u32x2 w = load_global<u32x2>(ok && v0 < a.groups * kGroup ? vp + v0 / 2 : zero);
+            const u32x2 w = load_once<u32x2>(vp + v_at[0]);
             x.v[s][0] = w[0], x.v[s][1] = w[1];
           } else {
 #pragma unroll
             for (int i = 0; i < VW; i += 4) {
-              const u32x4 w = load_global<u32x4>(ok && v0 + i * 8 < a.groups * kGroup ? vp + v0 / 2 + i * 4 : zero);
+              const u32x4 w = load_once<u32x4>(vp + v_at[i / 4]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) x.v[s][i + j] = w[j];
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < VS; ++i) x.v_scale[s][i] = load_once<uint8_t>(vsp + vs_at[i]);
+          vp += 16 * v_row, vsp += 16 * vs_row;
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const int page = __shfl(found, s * 16 + col);
+          const bool ok = page >= 0;
+          const int64_t in = (base + s * 16 + col) & (P - 1);
+          const uint8_t *vp = (const uint8_t *)a.v + page * a.v_page + in * a.v_slot + h * a.v_head;
+          const uint8_t *vsp = a.vs + page * a.vs_page + in * a.vs_slot + h * a.vs_head;
+          if constexpr (VW == 2) {
+            const u32x2 w = load_once<u32x2>(ok && v0 < a.groups * kGroup ? vp + v0 / 2 : zero);
+            x.v[s][0] = w[0], x.v[s][1] = w[1];
+          } else {
+#pragma unroll
+            for (int i = 0; i < VW; i += 4) {
+              const u32x4 w = load_once<u32x4>(ok && v0 + i * 8 < a.groups * kGroup ? vp + v0 / 2 + i * 4 : zero);
 #pragma unroll
               for (int j = 0; j < 4; ++j) x.v[s][i + j] = w[j];
             }
@@ -238,7 +376,7 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
 #pragma unroll
           for (int i = 0; i < VS; ++i) {
             const int g = v0 / kGroup + i;
-            x.v_scale[s][i] = load_global<uint8_t>(ok && g < a.groups ? vsp + g : zero);
+            x.v_scale[s][i] = load_once<uint8_t>(ok && g < a.groups ? vsp + g : zero);
           }
         }
       }
@@ -248,26 +386,44 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
       return (pos_first != pos_last && tile + kFew4Keys - 1 > pos_first) || (a.window && tile <= pos_last - a.window);
     };
     bool odd = false;
-    V4 *vt = sh.v[wave];
-    auto work = [&](Keys &k, int tile) {
+    const unsigned to_first = lds_address(sh.v[wave]) + L::write_first(col, v0);
+    const unsigned from_first = lds_address(sh.v[wave]) + L::read_first(lane);
+    Keys k;
+    int base = lo + (s0 * kFewWaves + wave) * kFew4Keys;
+    int next = find(base + kFew4Step);
+    if (base < end) {
+      const int found = find(base);
+      load_k(k, base, found);
+      load_v(k, base, found);
+    }
+    while (base < end) {
+      const int tile = base;
+      base += kFew4Step;
+      const int found = next;
+      next = find(base + kFew4Step);
       // S^T = K Q^T
       f32x4 x[4];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        x[s] = f32x4{0, 0, 0, 0};
+      for (int s = 0; s < 4; ++s) x[s] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < NM; ++i)
+      for (int i = 0; i < NM; ++i)
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
           x[s] = fp4_dot16(k.k[s][i % KR], k.k_scale[s][i % KR], q[i], q_scale[i], x[s]);
-        if constexpr (sizeof(T) == 4) x[s] *= a.scale2;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) x[s] *= a.scale2;
       }
       // V that is not there, or not in the row, is zero; a NaN that some rows see and others do not must not
       // reach the latter through 0 * NaN, so it is taken out of the product and added at the end.
       const bool mixed = is_mixed(tile);
-      if (k.live != ~0ull || mixed || a.groups * kGroup != DP) {
+      const unsigned long long live = k.live;
+      if (live != ~0ull || mixed || a.groups * kGroup != DP) {
         bool bad = false;
+        const unsigned long long mine = live >> col;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          const bool there = (k.live >> (s * 16 + col)) & 1;
+          const bool there = (unsigned)(mine >> (32 * (s >> 1))) & (1u << (16 * (s & 1)));
 #pragma unroll
           for (int i = 0; i < VS; ++i) {
             const bool keep = there && v0 + i * kGroup < a.groups * kGroup;
@@ -281,27 +437,38 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
           }
         }
         if (__builtin_amdgcn_ballot_w64(bad)) odd = true;
-        if (k.live != ~0ull || mixed) {
+      }
+      load_k(k, base, found);  // the next tile's keys are on their way from here on, its V from below
+
+      if (live != ~0ull || mixed) {
+        // bit: this lane's query sees the key; the lane's keys begin at 4 grp
+        unsigned long long seen = live;
+        if (mixed) {
+          const int most = pos - tile, least = a.window ? most - a.window : -1;
+          seen &= most < 0 ? 0 : most >= 63 ? ~0ull : (2ull << most) - 1;
+          seen &= least < 0 ? ~0ull : least >= 63 ? 0 : ~0ull << (least + 1);
+        }
+        seen >>= 4 * grp;
 #pragma unroll
-          for (int s = 0; s < 4; ++s)
+        for (int s = 0; s < 4; ++s) {
+          const unsigned bits = (unsigned)(seen >> (32 * (s >> 1)));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int key = s * 16 + grp * 4 + i;
-              bool seen = (k.live >> key) & 1;
-              if (mixed) seen = seen && tile + key <= pos && (!a.window || tile + key > pos - a.window);
-              x[s][i] = seen ? x[s][i] : kNegInf;
-            }
+          for (int i = 0; i < 4; ++i) x[s][i] = bits & (1u << (16 * (s & 1) + i)) ? x[s][i] : kNegInf;
         }
       }
       float top = x[0][0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
       top = max_across_16(top);
-      const float mn = fmaxf(m, top);
-      const float ms = mn == kNegInf ? 0.0f : mn * sc;  // nothing seen yet: exp2(-inf - 0) = 0
-      const float fade = exp2_of(m * sc - ms);          // 0 at the first key seen
-      m = mn;
-      l *= fade;
+      if (__builtin_amdgcn_ballot_w64(top > m)) {  // seldom behind the first tiles
+        const float mn = fmaxf(m, top);
+        const float fade = mn == kNegInf ? 1.0f : exp2_of((m - mn) * sc);  // 0 at the first key seen
+        m = mn;
+        l *= fade;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] *= fade;
+      }
+      const float ms = m == kNegInf ? 0.0f : m * sc;  // nothing seen yet: exp2(-inf - 0) = 0
       Vec pv[2][NP];
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
@@ -311,52 +478,41 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
         split_weight<V4, NP>(e, pv[i >> 3], i & 7);
       }
 #pragma unroll
-      for (int i = 0; i < DT; ++i) o[i] *= fade;
-#pragma unroll
       for (int half = 0; half < 2; ++half) {
+        // the addresses made of these here take an instruction each, kept ones a register
+        unsigned to = to_first, from = from_first;
+        asm("" : "+v"(to), "+v"(from));
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int i = 0; i < VW; ++i)
-            store8<V4>(vt + L::at(s * 16 + col, v0 + i * 8),
-                       eight_of<V4>(k.v[half * 2 + s][i], scale_of(k.v_scale[half * 2 + s][i * VS / VW])));
+            *(__attribute__((address_space(3))) Vec *)(uintptr_t)((to ^ (i << 4)) + s * 16 * L::kRowBytes) =
+                eight_of<V4>(k.v[half * 2 + s][i], scale_of(k.v_scale[half * 2 + s][i * VS / VW]));
+        if (half == 1) load_v(k, base, found);
         __builtin_amdgcn_wave_barrier();
+        union {
+          Vec v;
+          i16x4 h[2];
+        } w[DT];
 #pragma unroll
         for (int i = 0; i < DT; ++i) {
-          union {
-            Vec v;
-            V4 t[8];
-          } w;
-          L::read4(vt, grp * 4, i * 16, lane, w.t);
-          L::read4(vt, 16 + grp * 4, i * 16, lane, w.t + 4);
+          w[i].h[0] = lds_read_transposed(from ^ (i << 5));
+          w[i].h[1] = lds_read_transposed((from ^ (i << 5)) + 16 * L::kRowBytes);
+        }
 #pragma unroll
-          for (int p = 0; p < NP; ++p) o[i] = Type<V4>::dot16(w.v, pv[half][p], o[i]);
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int p = 0; p < NP; ++p) o[i] = Type<V4>::dot16(w[i].v, pv[half][p], o[i]);
+        // operands ahead of the products
+        constexpr int kAhead = DT < 4 ? DT : 4;
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 2 * kAhead, 2);
+#pragma unroll
+        for (int i = 0; i < DT - kAhead; ++i) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, NP, 2);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 2);
         }
-      }
-    };
-    int base = lo + (s0 * kFewWaves + wave) * kFew4Keys;
-    if (base < end) {
-      Keys one, two;
-      int next = find(base + kFew4Step);
-      load(one, base, find(base));
-      for (;;) {
-        const bool more = base + kFew4Step < end;
-        if (more) {
-          load(two, base + kFew4Step, next);
-          next = find(base + 2 * kFew4Step);
-        }
-        work(one, base);
-        base += kFew4Step;
-        if (!more) break;
-        const bool again = base + kFew4Step < end;
-        if (again) {
-          load(one, base + kFew4Step, next);
-          next = find(base + 2 * kFew4Step);
-        }
-        work(two, base);
-        base += kFew4Step;
-        if (!again) break;
+        __builtin_amdgcn_sched_group_barrier(kMfma, NP * kAhead, 2);
       }
     }
     if (odd) {  // rare
@@ -432,13 +588,83 @@ __global__ __launch_bounds__(kFewBlock) void attend_few_fp4(AttendFp4Args a) {
           a.lse[(int64_t)t * a.Hq + hd] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
       }
     }
-    if (slot >= 0 && tid == 0) {
-      int32_t *mt = a.meta + (1 + (int64_t)slot * a.Hkv + h) * kMeta;
-      mt[0] = part == 0 ? np : 0;
-      mt[1] = row0;
-      mt[2] = rows;
-      mt[3] = h;
+    if (slot >= 0 && me == i0 && tid == 0) {
+      record[0] = np;
+      record[1] = row0;
+      record[2] = rows;
     }
+    __syncthreads();
+  }
+}
+
+// Adds the pieces of one row of a tile that is cut up (see join_few): of the tile that begins in block i0 of
+// a KV head, at places 2 i0 + 1, 2 (i0 + 1), 2 (i0 + 2), ...  A block takes one of the n * Hkv records and every
+// gridDim.y-th row.
+template <class T, int DP>
+__global__ __launch_bounds__(kJoinBlock) void join_few_fp4(AttendArgs a) {
+  constexpr int kLanes = DP / 4;              // threads of a row
+  constexpr int kSide = kJoinBlock / kLanes;  // pieces side by side
+  __shared__ float acc[kSide][DP];
+  __shared__ float weight[kJoinBlock];
+  __shared__ float red[2][kJoinBlock / kWave];
+  const float sc = score_unit<T>(a);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t *record = a.meta + (int64_t)blockIdx.x * kMeta;
+  const int np = record[0], row0 = record[1], rows = record[2];
+  if (np <= 1) return;
+  const int h = (int)(blockIdx.x % (unsigned)a.Hkv);
+  const int64_t i0 = blockIdx.x / (unsigned)a.Hkv;
+  constexpr int64_t kSize = (int64_t)kFewRows * (DP + 2);
+  auto piece = [&](int j) { return a.part + ((2 * (i0 + j) + (j == 0)) * a.Hkv + h) * kSize; };
+  for (int i = blockIdx.y; i < rows; i += gridDim.y) {
+    const int ml = kFewRows * DP + i * 2;
+    float mx = kNegInf;
+    for (int j = tid; j < np; j += kJoinBlock) mx = fmaxf(mx, piece(j)[ml]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+    if (lane == 0) red[0][wave] = mx;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kJoinBlock / kWave; ++w) mx = fmaxf(mx, red[0][w]);
+    const int c = (tid % kLanes) * 4, g = tid / kLanes;
+    f32x4 o{0, 0, 0, 0};
+    float sum = 0.0f;
+    for (int j0 = 0; j0 < np; j0 += kJoinBlock) {
+      const int j = j0 + tid;
+      float w = 0.0f;
+      if (j < np) {
+        const float mj = piece(j)[ml];
+        w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
+        sum += w == 0.0f ? 0.0f : w * piece(j)[ml + 1];
+      }
+      __syncthreads();
+      weight[tid] = w;
+      __syncthreads();
+      const int n = imin(np - j0, kJoinBlock);
+#pragma unroll 8
+      for (int k = g; k < n; k += kSide) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(piece(j0 + k) + i * DP + c);
+        const float f = weight[k];
+        if (f != 0.0f) o += x * f;
+      }
+    }
+#pragma unroll
+    for (int k = 32; k; k >>= 1) sum += __shfl_xor(sum, k);
+    if (lane == 0) red[1][wave] = sum;
+    *reinterpret_cast<f32x4 *>(&acc[g][c]) = o;
+    __syncthreads();
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinBlock / kWave; ++w) sum += red[1][w];
+    const int row = row0 + i, t = row / a.G, hd = h * a.G + row % a.G;
+    const int64_t at = (int64_t)t * a.Hq + hd;
+    if (tid < a.D) {
+      float v = 0.0f;
+#pragma unroll
+      for (int k = 0; k < kSide; ++k) v += acc[k][tid];
+      ((T *)a.out)[at * a.D + tid] = (T)(mx == kNegInf ? 0.0f : v / sum);
+    }
+    if (tid == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
     __syncthreads();
   }
 }

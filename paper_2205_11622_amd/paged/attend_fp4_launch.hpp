@@ -23,24 +23,17 @@ int launch_fp4(F *fn, dim3 grid, int block, size_t lds, const Launch &l, const A
 
 template <class T, int DP, bool ONE_PAGE>
 int run_few_fp4(const Launch &l, AttendFp4Args a, int most_rows) {
-  a.target = l.cus * kFewPerCu;
-  const int64_t requests = a.R < a.T ? a.R : a.T;  // that have tokens, at most
-  int64_t tiles = (int64_t)a.T * a.G / kFewRows + requests;
-  // Beside attend_many_fp4: only what is left of a request has tiles here.
-  const int64_t left = requests * ((kFew4MostRows<T, DP> + kFewRows - 1) / kFewRows);
-  if (a.few <= kFew4MostRows<T, DP> && tiles > left) tiles = left;
-  const int64_t pieces = tiles * a.Hkv + a.target;
-  static_assert(kFewRows * (DP + 2) <= kFewValues, "fits the workspace");
-  const int64_t slots = few_slots(a.target);
+  // as many blocks as there is room for, the same for each KV head
+  static_assert(kFew4PerCu<T, DP> <= kFewPerCu && kFewRows * (DP + 2) <= kFewValues, "fits the workspace");
+  const int64_t room = (int64_t)l.cus * kFew4PerCu<T, DP>;
+  const int64_t n = room / a.Hkv > 0 ? room / a.Hkv : 1;
   HeldWorkspace ws;
-  int rc = partials(l, slots, a, &ws);
+  int rc = partials(l, few_slots(room > a.Hkv ? room : a.Hkv), a, &ws);
   if (rc != SPARSELNR_OK) return rc;
-  const int64_t most = (int64_t)l.cus * 8;
-  const unsigned grid = (unsigned)(pieces < most ? pieces : most);
-  rc = launch_fp4(attend_few_fp4<T, DP, ONE_PAGE>, dim3(grid), kFewBlock, sizeof(Few4Shared<T, DP>), l, a);
-  if (rc != SPARSELNR_OK) return rc;
-  const unsigned side = most_rows < kFewRows ? most_rows : kFewRows;  // about 8000 blocks in all
-  return launch(join_few<T, DP>, dim3((unsigned)(slots < 8192 / side ? slots : 8192 / side), side), kJoinBlock, 0, l, a);
+  rc = launch_fp4(attend_few_fp4<T, DP, ONE_PAGE>, dim3((unsigned)(n * a.Hkv)), kFewBlock, sizeof(Few4Shared<T, DP>), l, a);
+  if (rc != SPARSELNR_OK || n == 1) return rc;
+  return launch(join_few_fp4<T, DP>, dim3((unsigned)(n * a.Hkv), (unsigned)(most_rows < kFewRows ? most_rows : kFewRows)),
+                kJoinBlock, 0, l, a);
 }
 
 template <class T, int DP, bool ONE_PAGE>
