@@ -723,7 +723,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
   extern __shared__ __align__(16) char raw[];
   Many4SharedOf<T, DP, NW> &sh = *reinterpret_cast<Many4SharedOf<T, DP, NW> *>(raw);
   const float sc = score_unit<T>(a);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int P = 1 << a.shift;
   auto count = [&](int r, int &tiles, int &steps) {
@@ -760,9 +760,6 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
     const int rho = have_row ? mine : first;
     const int tok = rq.first + rho / a.G, head = h * a.G + rho % a.G;
     const int pos = before + rho / a.G;
-    const int wave_rows = imin(rows - wave * 32, 32);
-    const int wave_first = wave_rows > 0 ? before + (first + wave * 32) / a.G : 0;
-    const int wave_last = wave_rows > 0 ? before + (first + wave * 32 + wave_rows - 1) / a.G : -1;
     u32x6 q[KS][NQ];
     int q_scale[KS][NQ];
     {
@@ -792,15 +789,22 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
     // ------------------------------------------------ K and V into LDS
     const int n = t1 - t0;          // tiles of this piece
     const int k0 = lo + t0 * kManyKeys;
+    // Tiles from `tail` on some of the block's rows see a part of only, and with a window those before `head`.
+    const int tail = imin(imax((pos_first + 1 - k0) >> 6, 0), n);
+    const int head_end = a.window ? imin(imax(((pos_last - a.window - k0) >> 6) + 1, 0), n) : 0;
+    auto mixed = [&](int i) { return i >= tail || i < head_end; };
     // The table's entry for key `lane` of tile i (ONE_PAGE: for all of them), or of the
     // last key there is (there is one wherever this is called), and the page it stands for.
     auto find = [&](int i) {
       return table[imin(k0 + i * kManyKeys + (ONE_PAGE ? 0 : lane), hi - 1) >> a.shift];
     };
     auto valid = [&](int i, int page) {
-      if constexpr (ONE_PAGE) page = __builtin_amdgcn_readfirstlane(page);
-      const bool in = k0 + i * kManyKeys + (ONE_PAGE ? 0 : lane) < hi;
-      return in && (unsigned)page < (unsigned)a.pages ? page : -1;
+      if constexpr (ONE_PAGE) {
+        page = __builtin_amdgcn_readfirstlane(page);
+        return i < n && (unsigned)page < (unsigned)a.pages ? page : -1;
+      } else {
+        return k0 + i * kManyKeys + lane < hi && (unsigned)page < (unsigned)a.pages ? page : -1;
+      }
     };
     auto live_of = [&](int i, int page) -> unsigned long long {  // bit: this key is there
       if constexpr (ONE_PAGE) {
@@ -810,10 +814,13 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
         return __builtin_amdgcn_ballot_w64(page >= 0);
       }
     };
-    // a tile of which some of the block's rows see a part only
-    auto mixed = [&](int i) {
-      const int b = k0 + i * kManyKeys;
-      return b + kManyKeys - 1 > pos_first || (a.window && b <= pos_last - a.window);
+    // Few tiles are anything but 64 keys that are there and that all rows see: what the others need has its
+    // scalars worked out where it is needed only.
+    auto plain = [&](int i, int page) {
+      if constexpr (ONE_PAGE)
+        return page >= 0 && !mixed(i);
+      else
+        return __builtin_amdgcn_ballot_w64(page >= 0) == ~0ull && !mixed(i);
     };
     const int c_of = tid % NC, row_of = tid / NC;
     const int g_of = c_of * CB / kGroupBytes;  // group of this thread's chunks
@@ -831,20 +838,21 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
     const int64_t ks_page = any ? a.ks_page : 0, ks_slot = any ? a.ks_slot : 0;
     const int64_t vs_page = any ? a.vs_page : 0, vs_slot = any ? a.vs_slot : 0;
     const unsigned c_at = in_row ? c_of * CB : 0, s_at = in_row ? g_of : 0;
+    // ONE_PAGE: this lane's first row of page 0, to which a tile adds a scalar (see one_page: strides are 32 bits)
+    const uint8_t *k_lane = k_head + row_of * k_slot + c_at, *v_lane = v_head + row_of * v_slot + c_at;
+    const uint8_t *ks_lane = ks_head + row_of * ks_slot + s_at, *vs_lane = vs_head + row_of * vs_slot + s_at;
     Chunk kr[CH], vr[CH];
-    unsigned kb[CH], vb[CH];
-    auto load = [&](Chunk r[CH], unsigned b[CH], int i, int page, const uint8_t *base, int64_t page_stride,
+    uint8_t kb[CH], vb[CH];  // bytes: made words where they are loaded, they would be waited for there
+    auto load = [&](Chunk r[CH], uint8_t b[CH], int i, int page, const uint8_t *base, int64_t page_stride,
                     int64_t slot_stride, const uint8_t *s_base, int64_t s_page, int64_t s_slot) {
       if constexpr (ONE_PAGE) {
-        const int in = (k0 + i * kManyKeys) & (P - 1);
-        const uint8_t *src = base + imax(page, 0) * page_stride + in * slot_stride;
-        const uint8_t *s_src = s_base + imax(page, 0) * s_page + in * s_slot;
+        const unsigned in = (k0 + i * kManyKeys) & (P - 1), pg = imax(page, 0);
+        const uint8_t *src = base + ((uint64_t)pg * (unsigned)page_stride + in * (unsigned)slot_stride);
+        const uint8_t *s_src = s_base + ((uint64_t)pg * (unsigned)s_page + in * (unsigned)s_slot);
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-          r[c] = load_global<Chunk>(src + ((unsigned)row_of * (unsigned)slot_stride + c_at));
-          b[c] = load_global<uint8_t>(s_src + ((unsigned)row_of * (unsigned)s_slot + s_at));
-          src += RS * slot_stride;
-          s_src += RS * s_slot;
+          r[c] = load_global<Chunk>(src + c * RS * (int)slot_stride);
+          b[c] = load_global<uint8_t>(s_src + c * RS * (int)s_slot);
         }
       } else {
 #pragma unroll
@@ -858,26 +866,28 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
       }
     };
     auto load_k = [&](int i, int page) {
-      load(kr, kb, i, page, k_head, k_page, k_slot, ks_head, ks_page, ks_slot);
+      load(kr, kb, i, page, ONE_PAGE ? k_lane : k_head, k_page, k_slot, ONE_PAGE ? ks_lane : ks_head, ks_page, ks_slot);
     };
     auto load_v = [&](int i, int page) {
-      load(vr, vb, i, page, v_head, v_page, v_slot, vs_head, vs_page, vs_slot);
+      load(vr, vb, i, page, ONE_PAGE ? v_lane : v_head, v_page, v_slot, ONE_PAGE ? vs_lane : vs_head, vs_page, vs_slot);
     };
     // Rows that are not there become zeros, and V of a tile of which some rows see a part
     // only loses its NaN (kept for those who see them: see the end of the walk).
     const bool whole_rows = a.groups == G16;
-    auto clean = [&](Chunk r[CH], unsigned b[CH], unsigned long long live) {
-      if (live != ~0ull || !whole_rows) {
+    auto clean = [&](Chunk r[CH], uint8_t b[CH], unsigned long long live) {
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          const bool keep = in_row && ((live >> (c * RS + row_of)) & 1);
-          r[c] = keep ? r[c] : Chunk(0);
-          b[c] = keep ? b[c] : 127;
-        }
+      for (int c = 0; c < CH; ++c) {
+        const bool keep = in_row && ((live >> (c * RS + row_of)) & 1);
+        r[c] = keep ? r[c] : Chunk(0);
+        b[c] = keep ? b[c] : (uint8_t)127;
       }
     };
-    auto clean_v = [&](int i, unsigned long long live) {
-      clean(vr, vb, live);
+    auto clean_k = [&](int i, int page) {
+      if (!whole_rows || !plain(i, page)) clean(kr, kb, live_of(i, page));
+    };
+    auto clean_v = [&](int i, int page) {
+      if (whole_rows && plain(i, page)) return;
+      clean(vr, vb, live_of(i, page));
       if (mixed(i)) {
         bool bad = false;
 #pragma unroll
@@ -885,7 +895,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
           const bool nan = vb[c] == kNanScale;
           bad |= nan;
           vr[c] = nan ? Chunk(0) : vr[c];
-          vb[c] = nan ? 127 : vb[c];
+          vb[c] = nan ? (uint8_t)127 : vb[c];
         }
         if (__builtin_amdgcn_ballot_w64(bad)) sh.odd = 1;
       }
@@ -899,7 +909,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
         const int row = c * RS + row_of;
         const int at = c_of * CB;
         *reinterpret_cast<Chunk *>(&sh.k[buffer][row * RB + ((g_of ^ swizzle(row)) << 4) + (at & 15)]) = kr[c];
-        if (at % kGroupBytes == 0) sh.k_scale[buffer][row * SB + g_of] = (uint8_t)kb[c];
+        if (at % kGroupBytes == 0) sh.k_scale[buffer][row * SB + g_of] = kb[c];
       }
     };
     auto store_v = [&](int buffer) {
@@ -954,20 +964,22 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
       for (int c = 0; c < KS; ++c)
 #pragma unroll
         for (int w = 0; w < NQ; ++w)
+          {
 #pragma unroll
-          for (int s = 0; s < 2; ++s)
-            x[s] = c & 1 ? fp4_dot32<2>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s])
-                         : fp4_dot32<0>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s]);
+            for (int s = 0; s < 2; ++s)
+              x[s] = c & 1 ? fp4_dot32<2>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s])
+                           : fp4_dot32<0>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s]);
+            asm volatile("" : "+v"(x[0]), "+v"(x[1]));  // two products that do not wait for one another, in turn
+          }
       if constexpr (sizeof(T) == 4) x[0] *= a.scale2, x[1] *= a.scale2;
     };
 
     // P^T of tile i out of S^T, and what was summed so far brought to its maximum
-    auto weights = [&](int i, unsigned long long live) {
-      const int b = k0 + i * kManyKeys;
-      if (live != ~0ull || b + kManyKeys - 1 > wave_first || (a.window && b <= wave_last - a.window)) {
+    auto weights = [&](int i, int page) {
+      if (!plain(i, page)) {
         // bit: this lane's query sees the key; the lane's keys begin at 4 half
-        const int most = pos - b, least = a.window ? most - a.window : -1;
-        unsigned long long seen = live;
+        const int b = k0 + i * kManyKeys, most = pos - b, least = a.window ? most - a.window : -1;
+        unsigned long long seen = live_of(i, page);
         seen &= most < 0 ? 0 : most >= 63 ? ~0ull : (2ull << most) - 1;
         seen &= least < 0 ? ~0ull : least >= 63 ? 0 : ~0ull << (least + 1);
         seen >>= 4 * half;
@@ -1041,17 +1053,16 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
     if (tid == 0) sh.odd = 0;
     sync();
     if (n > 0) {
-      const int page0 = valid(0, find(0));
-      int v_pg = valid(1, find(1)), k_pg = valid(2, find(2));  // pages of stage i + 1 (V, K), while stage i is at hand
+      int pg = valid(0, find(0));  // page of tile i
+      int v_pg = valid(1, find(1)), k_pg = valid(2, find(2));  // of stage i + 1 (V, K), while stage i is at hand
       int next_pg = find(3);  // not looked at before its time: that would wait for the loads before it
-      unsigned long long live = live_of(0, page0), live1 = live_of(1, v_pg), live2 = live_of(2, k_pg);
-      load_k(0, page0);
-      clean(kr, kb, live);
+      load_k(0, pg);
+      clean_k(0, pg);
       store_k(0);
       load_k(1, v_pg);
-      load_v(0, page0);
-      clean(kr, kb, live1);
-      clean_v(0, live);
+      load_v(0, pg);
+      clean_k(1, v_pg);
+      clean_v(0, pg);
       sync();
       if (late) sync();
       for (int i = 0; i < n; ++i) {
@@ -1065,12 +1076,10 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
         if (i > 0) values(i - 1);
         sync();
         // among the softmax: what the stage on its way needs before it goes to LDS, and the next one's pages
-        weights(i, live);
-        if (live2 != ~0ull || !whole_rows) clean(kr, kb, live2);
-        if (live1 != ~0ull || !whole_rows || mixed(i + 1)) clean_v(i + 1, live1);
-        v_pg = k_pg;
-        k_pg = valid(i + 3, next_pg);
-        live = live1, live1 = live2, live2 = live_of(i + 3, k_pg);
+        weights(i, pg);
+        clean_k(i + 2, k_pg);
+        clean_v(i + 1, v_pg);
+        pg = v_pg, v_pg = k_pg, k_pg = valid(i + 3, next_pg);
         next_pg = find(i + 4);
         sync();
       }

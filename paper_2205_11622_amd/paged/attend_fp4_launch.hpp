@@ -67,9 +67,10 @@ int run_attend_fp4(const Launch &l, AttendFp4Args a, int64_t max_new) {
 
 template <class T, int DP>
 int attend_fp4_width(const Launch &l, const AttendFp4Args &a, int64_t max_new) {
-  // a tile of 64 keys within one page, its rows within 32 bits of bytes
-  const int64_t most = 1 << 24;
-  const bool one_page = a.shift >= 6 && a.k_slot < most && a.v_slot < most && a.ks_slot < most && a.vs_slot < most;
+  // a tile of 64 keys within one page, the page's bytes and the pages' strides within 32 bits
+  const int64_t row = 1 << 19, page = (int64_t)1 << 32;
+  const bool one_page = a.shift >= 6 && a.k_slot < row && a.v_slot < row && a.ks_slot < row && a.vs_slot < row &&
+                        a.k_page < page && a.v_page < page && a.ks_page < page && a.vs_page < page;
   return one_page ? run_attend_fp4<T, DP, true>(l, a, max_new) : run_attend_fp4<T, DP, false>(l, a, max_new);
 }
 
