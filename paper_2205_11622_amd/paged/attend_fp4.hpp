@@ -722,7 +722,6 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
   typedef typename Words<CB>::V Chunk;
   extern __shared__ __align__(16) char raw[];
   Many4SharedOf<T, DP, NW> &sh = *reinterpret_cast<Many4SharedOf<T, DP, NW> *>(raw);
-  const float sc = score_unit<T>(a);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, half = lane >> 5;
   const int P = 1 << a.shift;
@@ -772,7 +771,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
           const int d = c * 64 + half * 32 + i * 8;
           const typename Type<T>::Vec in = load8_global<T>(have_row && d < a.D ? src + d : (const T *)kZeroRow);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[i * 8 + j] = (float)in[j];
+          for (int j = 0; j < 8; ++j) x[i * 8 + j] = (float)in[j] * a.scale2;  // scores come out as exponents of two
         }
         const Query<NQ> s = split_query<NQ>(x);
 #pragma unroll
@@ -785,6 +784,9 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
     float m = kNegInf, l = 0.0f;
+    f32x16 low;  // -m in all of them, 0 before the first key: the products of a tile begin from it
+#pragma unroll
+    for (int j = 0; j < 16; ++j) low[j] = 0.0f;
 
     // ------------------------------------------------ K and V into LDS
     const int n = t1 - t0;          // tiles of this piece
@@ -909,7 +911,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
         const int row = c * RS + row_of;
         const int at = c_of * CB;
         *reinterpret_cast<Chunk *>(&sh.k[buffer][row * RB + ((g_of ^ swizzle(row)) << 4) + (at & 15)]) = kr[c];
-        if (at % kGroupBytes == 0) sh.k_scale[buffer][row * SB + g_of] = kb[c];
+        sh.k_scale[buffer][row * SB + g_of] = kb[c];  // all threads of a group the same: no condition, no other block
       }
     };
     auto store_v = [&](int buffer) {
@@ -938,7 +940,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
     f32x16 x[2];
     Vec pv[4][NP];
 
-    // S^T = K Q^T of tile i
+    // S^T = K Q^T of tile i, less the maximum so far
     auto scores = [&](int i) {
       const int buffer = i & 1;
       u32x4 k[2][KS];
@@ -956,22 +958,15 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
         for (int c = 0; c < KS; ++c)
           k[s][c] = *reinterpret_cast<const u32x4 *>(&sh.k[buffer][row * RB + (((c * 2 + half) ^ swizzle(row)) << 4)]);
       }
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) x[s][j] = 0.0f;
+      x[0] = low, x[1] = low;
 #pragma unroll
       for (int c = 0; c < KS; ++c)
 #pragma unroll
         for (int w = 0; w < NQ; ++w)
-          {
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-              x[s] = c & 1 ? fp4_dot32<2>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s])
-                           : fp4_dot32<0>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s]);
-            asm volatile("" : "+v"(x[0]), "+v"(x[1]));  // two products that do not wait for one another, in turn
-          }
-      if constexpr (sizeof(T) == 4) x[0] *= a.scale2, x[1] *= a.scale2;
+          for (int s = 0; s < 2; ++s)
+            x[s] = c & 1 ? fp4_dot32<2>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s])
+                         : fp4_dot32<0>(k[s][c], (int)e[s][c >> 1], q[c][w], q_scale[c][w], x[s]);
     };
 
     // P^T of tile i out of S^T, and what was summed so far brought to its maximum
@@ -994,18 +989,24 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
 #pragma unroll
       for (int j = 1; j < 32; ++j) top = fmaxf(top, x[j >> 4][j & 15]);
       top = max_across_32(top);
-      if (__builtin_amdgcn_ballot_w64((top - m) * sc > kLag<T, DP>)) {
-        const float mn = fmaxf(m, top);
-        const float fade = mn == kNegInf ? 1.0f : exp2_of((m - mn) * sc);
+      const bool none = m == kNegInf;
+      if (__builtin_amdgcn_ballot_w64(top > (none ? kNegInf : kLag<T, DP>))) {
+        const float up = none ? top : fmaxf(top, 0.0f);  // by how much the maximum rises
+        const float mn = none ? top : m + up;
+        const float fade = mn == kNegInf ? 1.0f : exp2_of(m - mn);
         l *= fade;
 #pragma unroll
         for (int c = 0; c < DT; ++c) o[c] *= fade;
         m = mn;
+        const float less = mn == kNegInf ? 0.0f : up;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j >> 4][j & 15] -= less;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) low[j] = mn == kNegInf ? 0.0f : -mn;
       }
-      const float ms = m == kNegInf ? 0.0f : m * sc;
 #pragma unroll
       for (int j = 0; j < 32; ++j) {
-        const float e = exp2_of(__builtin_fmaf(x[j >> 4][j & 15], sc, -ms));
+        const float e = exp2_of(x[j >> 4][j & 15]);
         l += e;
         // the weights go to the matrix cores in the type of V, their sum stays in fp32
         split_weight<V4, NP>(e, pv[j >> 3], j & 7);
@@ -1024,9 +1025,8 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
       for (int s = 0; s < 4; ++s)
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-          const unsigned to = (at ^ (c << 6)) + s * 16 * L::kRowBytes;
-          v[s][c].h[0] = lds_read_transposed(to);
-          v[s][c].h[1] = lds_read_transposed((to ^ L::kEight) + 8 * L::kRowBytes);
+          v[s][c].h[0] = lds_read_transposed((at ^ (c << 6)) + s * 16 * L::kRowBytes);
+          v[s][c].h[1] = lds_read_transposed((at ^ (c << 6) ^ L::kEight) + (s * 16 + 8) * L::kRowBytes);
         }
 #pragma unroll
       for (int s = 0; s < 4; ++s)
@@ -1034,14 +1034,6 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
         for (int w = 0; w < NP; ++w)
 #pragma unroll
           for (int c = 0; c < DT; ++c) o[c] = Type<V4>::dot32(v[s][c].v, pv[s][w], o[c]);
-      __builtin_amdgcn_sched_group_barrier(kDsRead, 8, 1);
-#pragma unroll
-      for (int c = 0; c < 4 * DT - 4; ++c) {
-        __builtin_amdgcn_sched_group_barrier(kMfma, NP, 1);
-        __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
-      }
-      __builtin_amdgcn_sched_group_barrier(kMfma, 4 * NP, 1);
-      __builtin_amdgcn_sched_barrier(0);
     };
 
     // ------------------------------------------------ the walk, in two phases a tile
@@ -1065,22 +1057,48 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
       clean_v(0, pg);
       sync();
       if (late) sync();
-      for (int i = 0; i < n; ++i) {
-        scores(i);
-        // stage i: K of tile i + 1, V of tile i
+      // Stage i, K of tile i + 1 and V of tile i, goes to LDS among the products of tile i, and the next stage's loads set off.
+      auto stage = [&](int i) {
         store_k((i + 1) & 1);
         store_v(i & 1);
         load_k(i + 2, k_pg);
         load_v(i + 1, v_pg);
-        __builtin_amdgcn_sched_barrier(0);
-        if (i > 0) values(i - 1);
-        sync();
-        // among the softmax: what the stage on its way needs before it goes to LDS, and the next one's pages
+      };
+      // The softmax, and among it what the stage on its way needs before it goes to LDS, and the next one's pages.
+      auto softmax = [&](int i) {
         weights(i, pg);
         clean_k(i + 2, k_pg);
         clean_v(i + 1, v_pg);
         pg = v_pg, v_pg = k_pg, k_pg = valid(i + 3, next_pg);
         next_pg = find(i + 4);
+      };
+      scores(0);
+      stage(0);
+      sync();
+      softmax(0);
+      sync();
+      for (int i = 1; i < n; ++i) {
+        values(i - 1);
+        stage(i);
+        scores(i);
+        // four operands of V ahead of its products, K's behind them
+        constexpr int kValues = 4 * DT;
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 8, 1);
+#pragma unroll
+        for (int c = 0; c < kValues - 4; ++c) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, NP, 1);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 1);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          __builtin_amdgcn_sched_group_barrier(kMfma, NP, 1);
+          __builtin_amdgcn_sched_group_barrier(kDsRead, (KS + 1) / 2, 1);
+        }
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 2 + 2 * KS, 1);
+        __builtin_amdgcn_sched_group_barrier(kMfma, 2 * KS * NQ, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        sync();
+        softmax(i);
         sync();
       }
       values(n - 1);
@@ -1147,7 +1165,7 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
           }
         }
       if (half == 0 && a.lse)
-        a.lse[(int64_t)tok * a.Hq + head] = m == kNegInf ? kNegInf : m * (sc * kLn2) + __logf(l);
+        a.lse[(int64_t)tok * a.Hq + head] = m == kNegInf ? kNegInf : m * kLn2 + __logf(l);
     }
   }
 }

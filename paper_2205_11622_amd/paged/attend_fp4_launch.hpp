@@ -49,6 +49,7 @@ int run_many_fp4(const Launch &l, AttendFp4Args a) {
   rc = launch_fp4(attend_many_fp4<T, DP, NW, ONE_PAGE>, dim3((unsigned)(pieces < most ? pieces : most)), NW * kWave,
                   sizeof(Many4SharedOf<T, DP, NW>), l, a);
   if (rc != SPARSELNR_OK) return rc;
+  a.scale2 = 1.0f;  // its maxima are exponents of two already
   return launch(join_many<T, DP, ROWS>, dim3((unsigned)l.cus, ROWS / kJoinRows), kJoinBlock, 0, l, a);
 }
 
