@@ -9,6 +9,7 @@ namespace {
 using namespace slnr;
 using namespace slnr::paged;
 
+
 // Blocks for `n` things of a thread each, at most `most`.
 unsigned blocks_for(int64_t n, int64_t most) {
   const int64_t b = (n + kLifeBlock - 1) / kLifeBlock;
@@ -25,16 +26,24 @@ int check_table(const int32_t *table, int64_t table_stride, const int32_t *seq_l
   return SPARSELNR_OK;
 }
 
-// The marks of `pages` pages and, behind them, a number for each.
-int life_workspace(const Launch &l, LifeArgs &a, bool ranks, HeldWorkspace *ws) {
-  a.words = ((int64_t)a.pages + 63) / 64;
+// The marks of the pages and, behind them, `more` numbers.
+int life_workspace(const Launch &l, LifeArgs &a, int64_t more, HeldWorkspace *ws, int32_t **numbers) {
   const size_t marks = (size_t)(a.words < 1 ? 1 : a.words) * sizeof(Word);
-  const int rc = hold_workspace(l.dev, l.stream, marks + (size_t)a.pages * sizeof(int32_t), kSlotLife, ws);
+  const int rc = hold_workspace(l.dev, l.stream, marks + (size_t)more * sizeof(int32_t), kSlotLife, ws);
   if (rc != SPARSELNR_OK) return rc;
   a.marks = (Word *)ws->ptr;
-  a.rank = ranks ? (int32_t *)((char *)ws->ptr + marks) : nullptr;
+  *numbers = (int32_t *)((char *)ws->ptr + marks);
   return SPARSELNR_OK;
 }
+
+// One block does it all where the entries and an eighth of the pages are no more than 4096.  Time on the GPU in
+// us, one block | several launches, free and compact, for entries of pages: 256 of 2048 4.0 | 8.6 and
+// 4.3 | 9.5; 2048 of 4096 6.7 | 9.1 and 6.4 | 11.0; 4096 of 8192 11.1 | 9.7 and 9.7 | 11.9; 8192 of 16384 19.9 | 10.1
+// and 17.2 | 12.4; 256 of 65536 10.9 | 9.5 and 16.4 | 11.2.
+constexpr int64_t kOneMost = 4096;
+static_assert(kOneMost * 8 <= kOneBlock * (int64_t)64, "a thread has a word of marks");
+
+bool one_block(const LifeArgs &a, int64_t rows) { return rows * a.W + a.pages / 8 <= kOneMost; }
 
 // Rows along x, up to eight blocks to a long one.
 dim3 grid_of_rows(int64_t rows, int64_t W) {
@@ -43,8 +52,8 @@ dim3 grid_of_rows(int64_t rows, int64_t W) {
 
 // Blocks that go through the marks; each of them counts all marks before its own.
 unsigned grid_of_words(const LifeArgs &a) {
-  const int64_t b = (a.words + 63) / 64;
-  return (unsigned)(b < 1 ? 1 : b > 256 ? 256 : b);
+  const int64_t b = (a.words + 15) / 16;
+  return (unsigned)(b < 1 ? 1 : b > 512 ? 512 : b);
 }
 
 }  // namespace
@@ -89,16 +98,22 @@ int sparselnr_page_free(const int32_t *rows, int32_t *table, int64_t table_strid
   a.out = freed, a.counts = counts;
   a.n = (int32_t)n, a.R = (int32_t)R, a.W = (int32_t)W, a.pages = (int32_t)pages, a.most = (int32_t)most;
   a.shift = page_shift(page_size);
+  a.words = (pages + 63) / 64;
+  if (one_block(a, n)) {
+    hipLaunchKernelGGL(page_free_one, dim3(1), dim3(kOneBlock), 0, (hipStream_t)stream, a);
+    return launched();
+  }
   Launch l;
   if ((rc = current(&l, stream)) != SPARSELNR_OK) return rc;
+  const dim3 block(kLifeBlock), rows_grid = grid_of_rows(n, W);
+  const int blocks = (int)(rows_grid.x * rows_grid.y);
   HeldWorkspace ws;
-  if ((rc = life_workspace(l, a, false, &ws)) != SPARSELNR_OK) return rc;
-  const dim3 block(kLifeBlock);
+  if ((rc = life_workspace(l, a, blocks, &ws, &a.given)) != SPARSELNR_OK) return rc;
   hipLaunchKernelGGL(life_clear, dim3(blocks_for(most > a.words ? most : a.words, 1024)), block, 0, l.stream, a, most);
   if ((rc = launched()) != SPARSELNR_OK) return rc;
-  hipLaunchKernelGGL(page_free_rows, grid_of_rows(n, W), block, 0, l.stream, a);
+  hipLaunchKernelGGL(page_free_rows, rows_grid, block, 0, l.stream, a);
   if ((rc = launched()) != SPARSELNR_OK) return rc;
-  hipLaunchKernelGGL(page_free_list, dim3(grid_of_words(a)), block, 0, l.stream, a);
+  hipLaunchKernelGGL(page_free_list, dim3(grid_of_words(a)), block, 0, l.stream, a, blocks);
   return launched();
 }
 
@@ -114,10 +129,15 @@ int sparselnr_page_compact(int32_t *table, int64_t table_stride, const int32_t *
   a.out = pairs, a.counts = counts;
   a.R = (int32_t)R, a.W = (int32_t)W, a.pages = (int32_t)pages, a.most = (int32_t)(pages / 2);
   a.shift = page_shift(page_size);
+  a.words = (pages + 63) / 64;
+  if (one_block(a, R)) {
+    hipLaunchKernelGGL(page_compact_one, dim3(1), dim3(kOneBlock), 0, (hipStream_t)stream, a);
+    return launched();
+  }
   Launch l;
   if ((rc = current(&l, stream)) != SPARSELNR_OK) return rc;
   HeldWorkspace ws;
-  if ((rc = life_workspace(l, a, true, &ws)) != SPARSELNR_OK) return rc;
+  if ((rc = life_workspace(l, a, a.words, &ws, &a.before)) != SPARSELNR_OK) return rc;
   const dim3 block(kLifeBlock), rows = grid_of_rows(R, W);
   const int64_t outs = 2 * (int64_t)a.most;
   hipLaunchKernelGGL(life_clear, dim3(blocks_for(outs > a.words ? outs : a.words, 1024)), block, 0, l.stream, a, outs);

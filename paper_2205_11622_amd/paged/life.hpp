@@ -125,7 +125,8 @@ struct LifeArgs {
   int32_t *seq, *shares;  // [R], [pages]
   int32_t *out, *counts;  // freed pages [most], or pairs [most][2]; counts [2]
   Word *marks;            // [words]
-  int32_t *rank;          // [pages] (compact): number of a page among those that move
+  int32_t *before;        // [words] (compact): marked pages before a word's
+  int32_t *given;         // [blocks] (free): entries that a block of page_free_rows gave up
   int64_t words;
   int32_t n, R, W, pages, shift, most;
 };
@@ -134,34 +135,43 @@ __global__ __launch_bounds__(kLifeBlock) void life_clear(LifeArgs a, int64_t out
   const int64_t i0 = (int64_t)blockIdx.x * kLifeBlock + threadIdx.x, step = (int64_t)gridDim.x * kLifeBlock;
   for (int64_t i = i0; i < a.words; i += step) a.marks[i] = 0;
   for (int64_t i = i0; i < outs; i += step) a.out[i] = -1;
-  if (i0 < 2) a.counts[i0] = 0;
 }
 
 __device__ __forceinline__ void mark(Word *marks, int page) { atomicOr(marks + (page >> 6), (Word)1 << (page & 63)); }
 
-// Blocks take rows along x and their entries along y.  An entry is taken by an exchange, so a row named
-// twice is given up once.
+__device__ __forceinline__ int pages_held(const LifeArgs &a, int r) {
+  return (int)(((int64_t)row_length(a.seq, r, a.W, a.shift) + (1 << a.shift) - 1) >> a.shift);
+}
+
+// Takes an entry by an exchange, so a row named twice is given up once: was it a page?  The page is marked if no
+// row is left that holds it.
+template <class M>
+__device__ __forceinline__ bool give_up(const LifeArgs &a, int r, int j, M mark_it) {
+  const int page = atomicExch(a.table + r * a.table_row + j, -1);
+  if (!is_page(page, a.pages)) return false;
+  if (atomicSub(a.shares + page, 1) <= 0) mark_it(page);
+  return true;
+}
+
+// Blocks take rows along x and their entries along y.  A block writes down what it gave up: one counter for all
+// of them costs 7 ns a block, 10 of 15 us for 1400 blocks.
 __global__ __launch_bounds__(kLifeBlock) void page_free_rows(LifeArgs a) {
   __shared__ int sums[kLifeBlock / kWave];
   int given = 0;
   for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
     const int r = a.rows[i];
     if ((unsigned)r >= (unsigned)a.R) continue;
-    const int held = (int)(((int64_t)row_length(a.seq, r, a.W, a.shift) + (1 << a.shift) - 1) >> a.shift);
-    for (int j = blockIdx.y * kLifeBlock + threadIdx.x; j < held; j += gridDim.y * kLifeBlock) {
-      const int page = atomicExch(a.table + r * a.table_row + j, -1);
-      if (!is_page(page, a.pages)) continue;
-      ++given;
-      if (atomicSub(a.shares + page, 1) <= 0) mark(a.marks, page);
-    }
+    const int held = pages_held(a, r);
+    for (int j = blockIdx.y * kLifeBlock + threadIdx.x; j < held; j += gridDim.y * kLifeBlock)
+      given += give_up(a, r, j, [&](int page) { mark(a.marks, page); });
   }
   given = block_sum(given, sums);
-  if (threadIdx.x == 0 && given) atomicAdd(a.counts + 1, given);
+  if (threadIdx.x == 0) a.given[blockIdx.y * gridDim.x + blockIdx.x] = given;
 }
 
 __global__ __launch_bounds__(kLifeBlock) void page_mark_used(LifeArgs a) {
   for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
-    const int held = (int)(((int64_t)row_length(a.seq, r, a.W, a.shift) + (1 << a.shift) - 1) >> a.shift);
+    const int held = pages_held(a, r);
     for (int j = blockIdx.y * kLifeBlock + threadIdx.x; j < held; j += gridDim.y * kLifeBlock) {
       const int page = a.table[r * a.table_row + j];
       if (is_page(page, a.pages)) mark(a.marks, page);
@@ -177,14 +187,16 @@ __device__ __forceinline__ int marked_below(const LifeArgs &a, int64_t end, int 
   return block_sum(x, sums);
 }
 
-// Goes through the marks of a block's share of the words: visit(page, marked, marked pages before it), a lane a
-// page, 64 at a time.
+// Goes through the marks of a block's share of the words: visit(page, marked, marked pages before it).  A thread
+// takes a word and counts what lies before it, then a wave takes the words in turn, a lane a page.
 template <class F>
-__device__ __forceinline__ void for_pages(const LifeArgs &a, int64_t w0, int64_t w1, int before, int *sums, F visit) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ void for_pages(const LifeArgs &a, int64_t w0, int64_t w1, int before, F visit) {
+  __shared__ Word words[kLifeBlock];
+  __shared__ int starts[kLifeBlock], sums[kLifeBlock / kWave];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   for (int64_t w = w0; w < w1; w += kLifeBlock) {
-    const int64_t i = w + threadIdx.x;
-    const Word bits = i < w1 ? a.marks[i] : 0;
+    const int n = (int)(w1 - w < kLifeBlock ? w1 - w : kLifeBlock);
+    const Word bits = tid < n ? a.marks[w + tid] : 0;
     int upto = __popcll(bits);
     const int mine = upto;
 #pragma unroll
@@ -192,7 +204,6 @@ __device__ __forceinline__ void for_pages(const LifeArgs &a, int64_t w0, int64_t
       const int x = __shfl_up(upto, o);
       if (lane >= o) upto += x;
     }
-    __syncthreads();
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     int all = 0;
@@ -201,14 +212,16 @@ __device__ __forceinline__ void for_pages(const LifeArgs &a, int64_t w0, int64_t
       if (k < wave) upto += sums[k];
       all += sums[k];
     }
-    const int start = before + upto - mine;
-    for (int k = 0; k < kWave && w + wave * kWave + k < w1; ++k) {
-      const Word b = __shfl(bits, k);
-      const int at = __shfl(start, k);
-      const int64_t page = (w + wave * kWave + k) * 64 + lane;
-      if (page < a.pages) visit((int)page, (bool)((b >> lane) & 1), at + __popcll(b & (((Word)1 << lane) - 1)));
+    words[tid] = bits;
+    starts[tid] = before + upto - mine;
+    __syncthreads();
+    for (int k = wave; k < n; k += kLifeBlock / kWave) {
+      const Word b = words[k];
+      const int64_t page = (w + k) * 64 + lane;
+      if (page < a.pages) visit((int)page, (bool)((b >> lane) & 1), starts[k] + __popcll(b & (((Word)1 << lane) - 1)));
     }
     before += all;
+    __syncthreads();
   }
 }
 
@@ -219,12 +232,12 @@ __device__ __forceinline__ void share_of(const LifeArgs &a, int64_t *w0, int64_t
   *w1 = *w0 + per < a.words ? *w0 + per : a.words;
 }
 
-__global__ __launch_bounds__(kLifeBlock) void page_free_list(LifeArgs a) {
+__global__ __launch_bounds__(kLifeBlock) void page_free_list(LifeArgs a, int blocks) {
   __shared__ int sums[kLifeBlock / kWave];
   int64_t w0, w1;
   share_of(a, &w0, &w1);
   const int before = marked_below(a, w0 * 64, sums);
-  for_pages(a, w0, w1, before, sums, [&](int page, bool marked, int rank) {
+  for_pages(a, w0, w1, before, [&](int page, bool marked, int rank) {
     if (!marked) return;
     a.shares[page] = 0;
     if (rank < a.most) a.out[rank] = page;
@@ -235,7 +248,10 @@ __global__ __launch_bounds__(kLifeBlock) void page_free_list(LifeArgs a) {
   }
   if (blockIdx.x == gridDim.x - 1) {
     const int all = marked_below(a, a.pages, sums);
-    if (threadIdx.x == 0) a.counts[0] = all;
+    int given = 0;
+    for (int i = threadIdx.x; i < blocks; i += kLifeBlock) given += a.given[i];
+    given = block_sum(given, sums);
+    if (threadIdx.x == 0) a.counts[0] = all, a.counts[1] = given;
   }
 }
 
@@ -247,30 +263,146 @@ __global__ __launch_bounds__(kLifeBlock) void page_compact_pairs(LifeArgs a) {
   share_of(a, &w0, &w1);
   const int used = marked_below(a, a.pages, sums), stay = marked_below(a, used, sums);
   const int before = marked_below(a, w0 * 64, sums);
-  for_pages(a, w0, w1, before, sums, [&](int page, bool marked, int rank) {
-    if (marked && page >= used) {
+  for_pages(a, w0, w1, before, [&](int page, bool marked, int rank) {
+    if (marked && page >= used)
       a.out[2 * (int64_t)(rank - stay)] = page;
-      a.rank[page] = rank - stay;
-    } else if (!marked && page < used) {
+    else if (!marked && page < used)
       a.out[2 * (int64_t)(page - rank) + 1] = page;
-    }
+    if ((page & 63) == 0) a.before[page >> 6] = rank - stay;
   });
   if (blockIdx.x == 0 && threadIdx.x == 0) a.counts[0] = used, a.counts[1] = used - stay;
+}
+
+// The number of a page among those that move.
+__device__ __forceinline__ int move_of(const Word *marks, const int32_t *before, int page) {
+  return before[page >> 6] + __popcll(marks[page >> 6] & (((Word)1 << (page & 63)) - 1));
 }
 
 __global__ __launch_bounds__(kLifeBlock) void page_compact_tables(LifeArgs a) {
   const int used = a.counts[0], moves = a.counts[1];
   for (int r = blockIdx.x; r < a.R; r += gridDim.x) {
-    const int held = (int)(((int64_t)row_length(a.seq, r, a.W, a.shift) + (1 << a.shift) - 1) >> a.shift);
+    const int held = pages_held(a, r);
     for (int j = blockIdx.y * kLifeBlock + threadIdx.x; j < held; j += gridDim.y * kLifeBlock) {
       const int page = a.table[r * a.table_row + j];
       if (is_page(page, a.pages) && page >= used)
-        a.table[r * a.table_row + j] = a.out[2 * (int64_t)a.rank[page] + 1];
+        a.table[r * a.table_row + j] = a.out[2 * (int64_t)move_of(a.marks, a.before, page) + 1];
     }
   }
   const int blocks = gridDim.x * gridDim.y, block = blockIdx.y * gridDim.x + blockIdx.x;
   for (int k = block * kLifeBlock + threadIdx.x; k < moves; k += blocks * kLifeBlock) {
     const int from = a.out[2 * (int64_t)k], to = a.out[2 * (int64_t)k + 1];
+    a.shares[to] = a.shares[from];
+    a.shares[from] = 0;
+  }
+}
+
+// The same two calls by one block, with the marks in LDS: three or four launches become one where the
+// entries are few.  Entries are taken as one line, so short rows leave no thread out.
+
+constexpr int kOneBlock = 1024;  // threads, and words of marks: 65536 pages
+
+struct OneBlock {
+  Word marks[kOneBlock];
+  int before[kOneBlock], sums[kOneBlock / kWave];
+};
+
+// Sum over the block of `mine`; *before: that of the threads before this one.
+__device__ __forceinline__ int one_scan(int mine, int *sums, int *before) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(upto, o);
+    if (lane >= o) upto += x;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int all = 0;
+#pragma unroll
+  for (int k = 0; k < kOneBlock / kWave; ++k) {
+    if (k < wave) upto += sums[k];
+    all += sums[k];
+  }
+  *before = upto - mine;
+  return all;
+}
+
+// visit(page, marked, marked pages before it), a wave a word and a lane a page.
+template <class F>
+__device__ __forceinline__ void one_pages(const LifeArgs &a, const OneBlock &s, F visit) {
+  const int lane = threadIdx.x & 63;
+  for (int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); w < a.words; w += kOneBlock / kWave) {
+    const Word b = s.marks[w];
+    const int page = w * 64 + lane;
+    if (page < a.pages) visit(page, (bool)((b >> lane) & 1), s.before[w] + __popcll(b & (((Word)1 << lane) - 1)));
+  }
+}
+
+__global__ __launch_bounds__(kOneBlock) void page_free_one(LifeArgs a) {
+  __shared__ OneBlock s;
+  const int tid = threadIdx.x, entries = a.n * a.W;
+  s.marks[tid] = 0;
+  __syncthreads();
+  int given = 0;
+  for (int e = tid; e < entries; e += kOneBlock) {
+    const int i = (unsigned)e / (unsigned)a.W, r = a.rows[i], j = e - i * a.W;
+    if ((unsigned)r < (unsigned)a.R && j < pages_held(a, r))
+      given += give_up(a, r, j, [&](int page) { mark(s.marks, page); });
+  }
+  int before;
+  given = one_scan(given, s.sums, &before);  // waits for the marks too
+  const int all = one_scan(__popcll(s.marks[tid]), s.sums, &before);
+  s.before[tid] = before;
+  __syncthreads();
+  one_pages(a, s, [&](int page, bool marked, int rank) {
+    if (!marked) return;
+    a.shares[page] = 0;
+    if (rank < a.most) a.out[rank] = page;
+  });
+  for (int i = all + tid; i < a.most; i += kOneBlock) a.out[i] = -1;
+  for (int i = tid; i < a.n; i += kOneBlock)
+    if ((unsigned)a.rows[i] < (unsigned)a.R) a.seq[a.rows[i]] = 0;
+  if (tid == 0) a.counts[0] = all, a.counts[1] = given;
+}
+
+__global__ __launch_bounds__(kOneBlock) void page_compact_one(LifeArgs a) {
+  __shared__ OneBlock s;
+  const int tid = threadIdx.x, entries = a.R * a.W;
+  s.marks[tid] = 0;
+  __syncthreads();
+  for (int e = tid; e < entries; e += kOneBlock) {
+    const int r = (unsigned)e / (unsigned)a.W, j = e - r * a.W;
+    if (j >= pages_held(a, r)) continue;
+    const int page = a.table[r * a.table_row + j];
+    if (is_page(page, a.pages)) mark(s.marks, page);
+  }
+  __syncthreads();
+  int before, unused;
+  const Word bits = s.marks[tid];
+  const int used = one_scan(__popcll(bits), s.sums, &before);
+  const int left = used - tid * 64;  // of the places that stay, those from this word on
+  const Word mask = left >= 64 ? ~(Word)0 : left > 0 ? ((Word)1 << left) - 1 : 0;
+  const int stay = one_scan(__popcll(bits & mask), s.sums, &unused), moves = used - stay;
+  s.before[tid] = before - stay;
+  __syncthreads();
+  one_pages(a, s, [&](int page, bool marked, int move) {
+    if (marked && page >= used)
+      a.out[2 * move] = page;
+    else if (!marked && page < used)
+      a.out[2 * (page - stay - move) + 1] = page;
+  });
+  for (int i = 2 * moves + tid; i < 2 * a.most; i += kOneBlock) a.out[i] = -1;
+  if (tid == 0) a.counts[0] = used, a.counts[1] = moves;
+  __syncthreads();
+  for (int e = tid; e < entries; e += kOneBlock) {
+    const int r = (unsigned)e / (unsigned)a.W, j = e - r * a.W;
+    if (j >= pages_held(a, r)) continue;
+    const int page = a.table[r * a.table_row + j];
+    if (is_page(page, a.pages) && page >= used) a.table[r * a.table_row + j] = a.out[2 * move_of(s.marks, s.before, page) + 1];
+  }
+  for (int k = tid; k < moves; k += kOneBlock) {
+    const int from = a.out[2 * k], to = a.out[2 * k + 1];
     a.shares[to] = a.shares[from];
     a.shares[from] = 0;
   }

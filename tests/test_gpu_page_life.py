@@ -70,7 +70,8 @@ class Held:
             assert (self.base[:, -self.extra:] == -99).all()
 
 
-SHAPES = [(1, 1, 16, 4), (3, 5, 16, 40), (20, 7, 4, 130), (64, 40, 8, 3000), (300, 9, 1, 1500), (9, 700, 2, 5000)]
+SHAPES = [(1, 1, 16, 4), (3, 5, 16, 40), (20, 7, 4, 130), (64, 40, 8, 3000), (300, 9, 1, 1500), (9, 700, 2, 5000), (37, 30, 2, 24001),
+          (70, 64, 4, 4500), (6, 11, 16, 40000), (1, 4096, 1, 5)]
 
 
 @pytest.mark.parametrize("R,W,P,pages", SHAPES)
@@ -258,10 +259,11 @@ def test_pages_past_32_bits(gpu):
 # --------------------------------------------------------------- in a graph
 
 
-def test_a_captured_tidying_up(gpu):
+@pytest.mark.parametrize("R,W,pages", [(24, 20, 900), (60, 40, 40000)])
+def test_a_captured_tidying_up(gpu, R, W, pages):
     """Fork, free and compact with their copies, captured, replayed on other tables between eager calls."""
-    P, pages = 8, 900
-    hs = [Held(gpu, 24, 20, P, pages, 40 + i, empty=0.0, holes=False) for i in range(4)]
+    P = 8
+    hs = [Held(gpu, R, W, P, pages, 40 + i, empty=0.0, holes=False) for i in range(4)]
     table, seq, shares = hs[0].table.clone(), hs[0].seq.clone(), hs[0].shares.clone()
     parents, children = hs[0].ints([0, 1, 2]), hs[0].ints([20, 21, 22])
     rows, gone = hs[0].ints([3, 4, 20]), hs[0].ints([20, 21, 22])
