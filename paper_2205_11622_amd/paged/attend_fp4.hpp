@@ -1129,11 +1129,13 @@ __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
       const int i = wave * 32 + col;
       if (have_row) {
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
+        for (int t = 0; t < DT; ++t) {
+          if (t >= a.groups) break;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             *reinterpret_cast<f32x4 *>(dst + (int64_t)i * DP + t * 32 + j * 8 + half * 4) =
                 f32x4{o[t][4 * j], o[t][4 * j + 1], o[t][4 * j + 2], o[t][4 * j + 3]};
+        }
         if (half == 0) {
           dst[ROWS * DP + i * 2] = m;
           dst[ROWS * DP + i * 2 + 1] = l;

@@ -7,12 +7,16 @@
 namespace slnr {
 namespace paged {
 
-// A request with more rows than this goes to attend_many_fp4.
+// A request with more rows than this goes to attend_many_fp4.  Time in us of few | many, bf16, 8 query heads to each of 4
+// KV heads: 32 requests behind 8000 keys, 48 rows each: 74 | 112 at dim 64, 94 | 126 at 128, 189 | 196 at 256; 64 rows:
+// 70 | 109, 89 | 125, 232 | 199; 128 rows: 128 | 114, 172 | 135, 461 | 213.  4 requests behind 3000, 64 rows: 27 | 36,
+// 31 | 44, 32 | 58.  fp32: 83 | 169, 116 | 240 and 290 | 411 for the 32 of 64 rows.
+constexpr int kFew4MostRows = 64;
+// Waves of a block of attend_many_fp4: two to a SIMD, one where a wave takes the registers of two (O of 256 columns, the
+// three pieces of fp32 at 128).  8 | 4 waves, 500 tokens of each of 2 requests behind 6000 keys: bf16 119 | 155 us at dim 64,
+// 139 | 175 at 128; fp32 172 | 222 at 64, 429 (43 to 74 registers in memory) | 315 at 128.
 template <class T, int DP>
-constexpr int kFew4MostRows = sizeof(T) == 2 && DP > 64 ? 32 : 64;
-// Waves of a block of attend_many_fp4: two to a SIMD, one where O of 256 columns takes the registers of two.
-template <class T, int DP>
-constexpr int kMany4Waves = DP > 128 ? 4 : 8;
+constexpr int kMany4Waves = DP > 128 || (sizeof(T) == 4 && DP > 64) ? 4 : 8;
 
 template <class F>
 int launch_fp4(F *fn, dim3 grid, int block, size_t lds, const Launch &l, const AttendFp4Args &a) {
@@ -58,8 +62,8 @@ int run_attend_fp4(const Launch &l, AttendFp4Args a, int64_t max_new) {
   // rows of the longest request, as far as the host knows
   const int64_t rows = (max_new > 0 && max_new < a.T ? max_new : a.T) * a.G;
   a.few = 0x7fffffff;
-  if (rows > kFew4MostRows<T, DP>) {
-    a.few = kFew4MostRows<T, DP>;
+  if (rows > kFew4MostRows) {
+    a.few = kFew4MostRows;
     const int rc = run_many_fp4<T, DP, ONE_PAGE>(l, a);
     if (rc != SPARSELNR_OK) return rc;
   }
