@@ -482,8 +482,9 @@ SPARSELNR_API int sparselnr_paged_attention_fp4(const void *q, int64_t q_token, 
  *   - Whatever the arrays on the device hold, no call reads or writes outside them, and
  *     results do not depend on the order in which the device works.
  *   - sparselnr_page_free and sparselnr_page_compact use a workspace per (device, stream) that
- *     grows with `pages` alone (33 bits a page).  A capture of either needs one call before it
- *     with as many pages, and while the graph may be replayed no such call on that stream may have more.
+ *     grows with `pages` alone (256 KB and 12 bytes for 64 pages).  A capture of either needs one call
+ *     of the same sizes before it, and while the graph may be replayed no such call on that stream may
+ *     have more pages.
  * ---------------------------------------------------------------------- */
 
 /*

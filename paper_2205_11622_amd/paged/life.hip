@@ -26,13 +26,17 @@ int check_table(const int32_t *table, int64_t table_stride, const int32_t *seq_l
   return SPARSELNR_OK;
 }
 
-// The marks of the pages and, behind them, `more` numbers.
-int life_workspace(const Launch &l, LifeArgs &a, int64_t more, HeldWorkspace *ws, int32_t **numbers) {
+constexpr int64_t kMostRowBlocks = 8192, kMostRowParts = 8;
+
+// The marks of the pages and, behind them, a number for each word or for each block of rows.  Its size goes by
+// the pages alone: a captured graph holds its address, so a call of more rows may not have to grow it.
+int life_workspace(const Launch &l, LifeArgs &a, HeldWorkspace *ws) {
   const size_t marks = (size_t)(a.words < 1 ? 1 : a.words) * sizeof(Word);
-  const int rc = hold_workspace(l.dev, l.stream, marks + (size_t)more * sizeof(int32_t), kSlotLife, ws);
+  const int64_t numbers = a.words > kMostRowBlocks * kMostRowParts ? a.words : kMostRowBlocks * kMostRowParts;
+  const int rc = hold_workspace(l.dev, l.stream, marks + (size_t)numbers * sizeof(int32_t), kSlotLife, ws);
   if (rc != SPARSELNR_OK) return rc;
   a.marks = (Word *)ws->ptr;
-  *numbers = (int32_t *)((char *)ws->ptr + marks);
+  a.before = a.given = (int32_t *)((char *)ws->ptr + marks);
   return SPARSELNR_OK;
 }
 
@@ -47,7 +51,7 @@ bool one_block(const LifeArgs &a, int64_t rows) { return rows * a.W + a.pages / 
 
 // Rows along x, up to eight blocks to a long one.
 dim3 grid_of_rows(int64_t rows, int64_t W) {
-  return dim3((unsigned)(rows < 1 ? 1 : rows > 8192 ? 8192 : rows), blocks_for(W, 8));
+  return dim3((unsigned)(rows < 1 ? 1 : rows > kMostRowBlocks ? kMostRowBlocks : rows), blocks_for(W, kMostRowParts));
 }
 
 // Blocks that go through the marks; each of them counts all marks before its own.
@@ -108,7 +112,7 @@ int sparselnr_page_free(const int32_t *rows, int32_t *table, int64_t table_strid
   const dim3 block(kLifeBlock), rows_grid = grid_of_rows(n, W);
   const int blocks = (int)(rows_grid.x * rows_grid.y);
   HeldWorkspace ws;
-  if ((rc = life_workspace(l, a, blocks, &ws, &a.given)) != SPARSELNR_OK) return rc;
+  if ((rc = life_workspace(l, a, &ws)) != SPARSELNR_OK) return rc;
   hipLaunchKernelGGL(life_clear, dim3(blocks_for(most > a.words ? most : a.words, 1024)), block, 0, l.stream, a, most);
   if ((rc = launched()) != SPARSELNR_OK) return rc;
   hipLaunchKernelGGL(page_free_rows, rows_grid, block, 0, l.stream, a);
@@ -137,7 +141,7 @@ int sparselnr_page_compact(int32_t *table, int64_t table_stride, const int32_t *
   Launch l;
   if ((rc = current(&l, stream)) != SPARSELNR_OK) return rc;
   HeldWorkspace ws;
-  if ((rc = life_workspace(l, a, a.words, &ws, &a.before)) != SPARSELNR_OK) return rc;
+  if ((rc = life_workspace(l, a, &ws)) != SPARSELNR_OK) return rc;
   const dim3 block(kLifeBlock), rows = grid_of_rows(R, W);
   const int64_t outs = 2 * (int64_t)a.most;
   hipLaunchKernelGGL(life_clear, dim3(blocks_for(outs > a.words ? outs : a.words, 1024)), block, 0, l.stream, a, outs);
