@@ -1,14 +1,17 @@
 """A small serving loop on a paged cache: requests come, their prompts are read in
 chunks beside the running ones' single tokens, and leave when they are done.
 
-    python examples/paged_serving.py [--requests 12] [--layers 2] [--sparse 0] [--check]
+    python examples/paged_serving.py [--requests 12] [--layers 2] [--sparse 0] [--answers 1] [--four-bits] [--check]
 
 Every step is one batch: block tables and slots from the lengths, then per layer the new
 tokens' K and V into the cache and attention over it; with --sparse N each token
-attends the N pages that the 8-bit score selects.  The model is a stack of random
+attends the N pages that the 8-bit score selects.  With --answers N a prompt that has been read
+is gone on from N times: the rows of its answers share its full pages, rows that are done are given up
+by the device, and now and then the pages in use move to the front.  --four-bits keeps the cache in
+4 bits a value.  The model is a stack of random
 projections with residuals (there is nothing to say, only to compute).  --check
 compares each request's last hidden state with the same model run over its whole
-sequence at once, in fp32 on torch (dense attention only).
+sequence at once, in fp32 on torch (dense attention over a cache of the model's type only).
 """
 import argparse
 import os
@@ -26,14 +29,19 @@ import paper_2205_11622_amd as slnr  # noqa: E402
 class Cache:
     """Pages of every layer, the free list, and the requests' rows of the block table."""
 
-    def __init__(self, layers, pages, page_size, heads, dim, slots, width, device, dtype):
-        shape = (pages, page_size, heads, dim)
-        self.page_size = page_size
-        self.k = [torch.zeros(shape, dtype=dtype, device=device) for _ in range(layers)]
-        self.v = [torch.zeros(shape, dtype=dtype, device=device) for _ in range(layers)]
+    def __init__(self, layers, pages, page_size, heads, dim, slots, width, device, dtype, four_bits=False):
+        self.page_size, self.pages, self.four_bits = page_size, pages, four_bits
+
+        def rows(size, dtype):  # a head's rows of a page adjacent
+            return [torch.zeros(pages, heads, page_size, size, dtype=dtype, device=device).transpose(1, 2) for _ in range(layers)]
+
+        groups = -(-dim // 32)
+        self.k, self.v = (rows(16 * groups, torch.uint8) if four_bits else rows(dim, dtype) for _ in "kv")
+        self.k_scale, self.v_scale = (rows(groups, torch.uint8) if four_bits else [] for _ in "kv")
         self.kq = [torch.zeros(pages, heads, dim, dtype=torch.int8, device=device) for _ in range(layers)]
         self.ks = [torch.zeros(pages, heads, device=device) for _ in range(layers)]
         self.table = torch.full((slots, width), -1, dtype=torch.int32, device=device)
+        self.shares = torch.zeros(pages, dtype=torch.int32, device=device)
         self.free = list(range(pages))
         self.held = [[] for _ in range(slots)]
 
@@ -44,6 +52,32 @@ class Cache:
         self.free.extend(self.held[slot])
         self.held[slot] = []
         self.table[slot] = -1
+
+    # The same where rows share pages: what is free is what the calls say.
+
+    def copy(self, pairs):
+        """Pages of every layer, a few arrays a call."""
+        arrays = self.k + self.v + self.k_scale + self.v_scale + self.kq + self.ks
+        for i in range(0, len(arrays), 8):
+            slnr.sparselnr_page_copy(pairs, arrays[i:i + 8])
+
+    def fork(self, parents, children, seq):
+        pairs, counts = slnr.sparselnr_page_fork(*(torch.tensor(x, dtype=torch.int32, device=seq.device)
+                                                   for x in (parents, children)), self.table, seq, self.shares,
+                                                 torch.tensor(self.free, dtype=torch.int32, device=seq.device), self.page_size)
+        self.copy(pairs)
+        del self.free[:int(counts[0])]
+
+    def give_up(self, rows, seq):
+        freed, counts = slnr.sparselnr_page_free(torch.tensor(rows, dtype=torch.int32, device=seq.device), self.table, seq,
+                                                 self.shares, self.page_size)
+        self.free += freed[:int(counts[0])].tolist()
+
+    def tidy(self, seq):
+        pairs, counts = slnr.sparselnr_page_compact(self.table, seq, self.shares, self.page_size)
+        used, moved = counts.tolist()
+        self.copy(pairs[:moved])
+        self.free = list(range(used, self.pages))
 
 
 class Model:
@@ -60,8 +94,14 @@ class Model:
             qkv = (x @ w).view(x.shape[0], Hq + 2 * Hkv, self.dim)
             q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
             summaries = (cache.kq[i], cache.ks[i]) if sparse else (None, None)
-            slnr.sparselnr_cache_append(k, v, slots, cache.k[i], cache.v[i], *summaries)
-            if sparse:
+            if cache.four_bits:
+                four = (cache.k[i], cache.v[i], cache.k_scale[i], cache.v_scale[i])
+                slnr.sparselnr_cache_append_fp4(k, v, slots, *four)
+            else:
+                slnr.sparselnr_cache_append(k, v, slots, cache.k[i], cache.v[i], *summaries)
+            if cache.four_bits:
+                a = slnr.sparselnr_paged_attention_fp4(q, *four, table, seq, qptr, max_new=max_new)
+            elif sparse:
                 sel = slnr.sparselnr_block_select(q, *summaries, table, seq, qptr, cache.page_size, sparse,
                                                   first=1, local=min(2, sparse - 1))
                 a = slnr.sparselnr_block_attention(q, cache.k[i], cache.v[i], table, seq, qptr, sel)
@@ -86,22 +126,25 @@ class Model:
 
 
 def serve(requests=12, layers=2, width=256, Hq=8, Hkv=2, dim=64, page_size=16, batch=4, chunk=64, sparse=0, check=False,
-          dtype=torch.float32, device="cuda:0", seed=0):
+          dtype=torch.float32, device="cuda:0", seed=0, answers=1, four_bits=False):
     """Runs the loop; returns (tokens, steps, worst relative error or None)."""
+    if sparse and four_bits:
+        raise ValueError("pages are selected in a cache of the model's type")
     rng = random.Random(seed)
     g = torch.Generator(device=device).manual_seed(seed + 1)
     model = Model(layers, width, Hq, Hkv, dim, device, dtype)
     waiting = [(rng.randrange(1, 4 * chunk), rng.randrange(1, 24)) for _ in range(requests)]  # prompt, answer
     longest = max(p + a for p, a in waiting)
-    cache = Cache(layers, batch * -(-longest // page_size), page_size, Hkv, dim, batch, -(-longest // page_size), device,
-                  dtype)
-    running = [None] * batch
+    rows = batch * answers  # of the table; a request's answers have adjacent ones, and the first reads the prompt
+    cache = Cache(layers, rows * -(-longest // page_size), page_size, Hkv, dim, rows, -(-longest // page_size), device,
+                  dtype, four_bits)
+    running = [None] * rows
     tokens = steps = 0
     worst = 0.0 if check else None
     ints = lambda v: torch.tensor(v, dtype=torch.int32, device=device)  # noqa: E731
     while waiting or any(running):
-        for s in range(batch):
-            if running[s] is None and waiting:
+        for s in range(0, rows, answers):
+            if not any(running[s:s + answers]) and waiting:
                 p, a = waiting.pop(0)
                 running[s] = dict(ctx=0, x=torch.randn(p + a, width, device=device, generator=g).to(dtype), prompt=p)
         ctx = [r["ctx"] if r else 0 for r in running]
@@ -109,24 +152,46 @@ def serve(requests=12, layers=2, width=256, Hq=8, Hkv=2, dim=64, page_size=16, b
         T = sum(new)
         qptr, seq, slots, counts = slnr.sparselnr_page_tables(ints(ctx), ints(new), cache.table, ints(cache.free), T,
                                                               page_size)
-        for s in range(batch):  # the host's own books: what the call handed out, in its order
+        for s in range(rows):  # the host's own books: what the call handed out, in its order
             n = cache.wanted(ctx[s], new[s])
-            cache.held[s] += cache.free[:n]
+            if answers == 1:
+                cache.held[s] += cache.free[:n]
             del cache.free[:n]
         x = torch.cat([r["x"][r["ctx"]:r["ctx"] + n] for r, n in zip(running, new) if r])
         y = model.step(x, cache, qptr, seq, slots, cache.table, max(new), sparse)
         at = 0
+        done, parents, children = [], [], []
         for s, r in enumerate(running):
-            if r is None:
+            if r is None or new[s] == 0:
                 continue
             at += new[s]
             r["ctx"] += new[s]
+            if answers > 1 and r["ctx"] == r["prompt"] and s % answers == 0:
+                for c in range(s + 1, s + answers):
+                    x = torch.randn(len(r["x"]) - r["prompt"], width, device=device, generator=g).to(dtype)
+                    running[c] = dict(ctx=r["ctx"], x=torch.cat([r["x"][:r["prompt"]], x]), prompt=r["prompt"])
+                    parents.append(s)
+                    children.append(c)
             if r["ctx"] == r["x"].shape[0]:
                 if check:
                     want = model.whole(r["x"])[-1]
                     worst = max(worst, float((y[at - 1].float() - want).norm() / want.norm()))
-                cache.release(s)
-                running[s] = None
+                if answers == 1:
+                    cache.release(s)
+                done.append(s)
+        if answers > 1:
+            lengths = [r["ctx"] if r else 0 for r in running]
+            for c in children:
+                lengths[c] = 0  # until the fork
+            lengths = ints(lengths)
+            if children:
+                cache.fork(parents, children, lengths)
+            if done:
+                cache.give_up(done, lengths)
+            if steps % 8 == 7:
+                cache.tidy(lengths)
+        for s in done:
+            running[s] = None
         tokens += T
         steps += 1
     return tokens, steps, worst
@@ -137,12 +202,15 @@ def main():
     ap.add_argument("--requests", type=int, default=12)
     ap.add_argument("--layers", type=int, default=2)
     ap.add_argument("--sparse", type=int, default=0, help="pages that a token attends (0: all)")
+    ap.add_argument("--answers", type=int, default=1, help="of each request, over the same pages of its prompt")
+    ap.add_argument("--four-bits", action="store_true", help="the cache in 4 bits a value")
     ap.add_argument("--dtype", choices=["bf16", "fp16", "fp32"], default="bf16")
     ap.add_argument("--check", action="store_true")
     a = ap.parse_args()
     dtype = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}[a.dtype]
     t = time.perf_counter()
-    tokens, steps, worst = serve(a.requests, a.layers, sparse=a.sparse, check=a.check and not a.sparse, dtype=dtype)
+    tokens, steps, worst = serve(a.requests, a.layers, sparse=a.sparse, check=a.check and not a.sparse and not a.four_bits,
+                                 dtype=dtype, answers=a.answers, four_bits=a.four_bits)
     torch.cuda.synchronize()
     t = time.perf_counter() - t
     print("%d tokens in %d steps, %.2f s%s" % (tokens, steps, t, "" if worst is None else
