@@ -702,12 +702,12 @@ struct Words<16> {
   typedef u32x4 V;
 };
 
-template <class T, int DP, int NW, bool ONE_PAGE>
+template <class T, int DP, int NW, bool ONE_PAGE, int NQ>
 __global__ __launch_bounds__(NW *kWave) void attend_many_fp4(AttendFp4Args a) {
   typedef typename Four<T>::V4 V4;
   typedef typename Type<V4>::Vec Vec;
   typedef Tile<V4, DP> L;
-  constexpr int NQ = Four<T>::kQ, NP = Four<T>::kP;
+  constexpr int NP = Four<T>::kP;
   constexpr int NT = NW * kWave, ROWS = 32 * NW;
   constexpr int KS = DP / 64;               // products of the summed axis of q.k, of each piece
   constexpr int DT = DP / 32;               // tiles of output columns

@@ -40,7 +40,7 @@ int run_few_fp4(const Launch &l, AttendFp4Args a, int most_rows) {
                 kJoinBlock, 0, l, a);
 }
 
-template <class T, int DP, bool ONE_PAGE>
+template <class T, int DP, bool ONE_PAGE, int NQ>
 int run_many_fp4(const Launch &l, AttendFp4Args a) {
   constexpr int NW = kMany4Waves<T, DP>, ROWS = 32 * NW;
   a.target = l.cus * kManyPerCu;
@@ -50,7 +50,7 @@ int run_many_fp4(const Launch &l, AttendFp4Args a) {
   HeldWorkspace ws;
   int rc = partials(l, many_slots(a.target), a, &ws);
   if (rc != SPARSELNR_OK) return rc;
-  rc = launch_fp4(attend_many_fp4<T, DP, NW, ONE_PAGE>, dim3((unsigned)(pieces < most ? pieces : most)), NW * kWave,
+  rc = launch_fp4(attend_many_fp4<T, DP, NW, ONE_PAGE, NQ>, dim3((unsigned)(pieces < most ? pieces : most)), NW * kWave,
                   sizeof(Many4SharedOf<T, DP, NW>), l, a);
   if (rc != SPARSELNR_OK) return rc;
   a.scale2 = 1.0f;  // its maxima are exponents of two already
@@ -64,7 +64,10 @@ int run_attend_fp4(const Launch &l, AttendFp4Args a, int64_t max_new) {
   a.few = 0x7fffffff;
   if (rows > kFew4MostRows) {
     a.few = kFew4MostRows;
-    const int rc = run_many_fp4<T, DP, ONE_PAGE>(l, a);
+    // A fourth piece of the query, for lse: 2 of 2000 tokens behind 13000 keys 579 us, with it 642.  Few rows have
+    // it always: 96 single tokens 127.6 and 127.9 us.
+    const int rc = a.lse ? run_many_fp4<T, DP, ONE_PAGE, Four<T>::kQ>(l, a)
+                         : run_many_fp4<T, DP, ONE_PAGE, Four<T>::kQOut>(l, a);
     if (rc != SPARSELNR_OK) return rc;
   }
   return run_few_fp4<T, DP, ONE_PAGE>(l, a, rows < kFewRows ? (int)rows : kFewRows);

@@ -26,23 +26,24 @@ constexpr unsigned kNanScale = 255;  // a group with infinities or NaN: all of i
 // exactly.  kLeast, kMost: exponents of a group.  0.5 * 2^kLeast and 6 * 2^kMost are values of V4, so
 // that no group is lost or becomes infinite on its way back; only fp16's largest values
 // (above 7 * 2^13) and the last two binades of bf16 and fp32 are clipped by it.
-// kQ: pieces that a query is split into (see split_query), kP: pieces of a weight.
+// kQ: pieces that a query is split into (see split_query), kQOut: as many as out needs, which is rounded to the type
+// while lse is not; kP: pieces of a weight.
 template <class T>
 struct Four;
 template <>
 struct Four<__bf16> {
   typedef __bf16 V4;
-  static constexpr int kLeast = -125, kMost = 125, kQ = 3, kP = 1;
+  static constexpr int kLeast = -125, kMost = 125, kQ = 4, kQOut = 3, kP = 1;
 };
 template <>
 struct Four<_Float16> {
   typedef _Float16 V4;
-  static constexpr int kLeast = -23, kMost = 13, kQ = 3, kP = 1;
+  static constexpr int kLeast = -23, kMost = 13, kQ = 4, kQOut = 3, kP = 1;
 };
 template <>
 struct Four<float> {
   typedef __bf16 V4;
-  static constexpr int kLeast = -125, kMost = 125, kQ = 5, kP = 3;
+  static constexpr int kLeast = -125, kMost = 125, kQ = 5, kQOut = 5, kP = 3;
 };
 
 __device__ __forceinline__ float scale_of(unsigned byte) { return __uint_as_float(byte << 23); }
@@ -177,7 +178,8 @@ __global__ __launch_bounds__(kFp4Block) void fp4_read(Fp4Args a) {
 // with an exponent of its own per group.  A first piece leaves at most 1/4 of its unit, 4 units of a second
 // one 16 times finer; each further piece is 32 times finer.  Three pieces leave 2^-12 of the first
 // unit, which is at most the group's largest value divided by 3.75: less than half a last place of that
-// value in fp16 (and far less in bf16).  Five leave 2^-22: a last place of fp32.
+// value in fp16 (and far less in bf16), enough for out, which is rounded to the type.  lse is not: over 1000 keys at dim 96 three
+// pieces put it off by up to 1.9e-4, four, which leave 2^-17, by 4e-6.  Five leave 2^-22: a last place of fp32.
 constexpr int query_step(int piece) { return piece == 0 ? 0 : 5 * piece - 1; }
 
 template <int N>

@@ -137,10 +137,10 @@ class Batch4(pu.Batch):
                 self.ints(self.seq, device), self.ints(self.qptr, device))
 
 
-def query_error(b, scale):
-    """Bound on a score's error by the query's pieces, T x Hq: a group's rest is at most 2^-12 (16-bit
-    types) or 2^-22 of a unit, which is at most the group's largest value / 3.75; the keys' values multiply it."""
-    unit = 2.0 ** (-22 if b.dtype == torch.float32 else -12) / 3.75
+def query_error(b, scale, pieces):
+    """Bound on a score's error by the query's pieces, T x Hq: a group's rest is at most 2^-12 (three), 2^-17 or
+    2^-22 of a unit, which is at most the group's largest value / 3.75; the keys' values multiply it."""
+    unit = 2.0 ** (3 - 5 * pieces) / 3.75
     T, Hq, D = b.q.shape
     G = Hq // b.kc.shape[2]
     pad = (0, -D % 32)
@@ -159,7 +159,7 @@ def check(b, out, lse, ref, scale=None, logits=8.0):
     assert out.dtype == b.dtype
     S = max(b.seq + [1])
     vmax = float(b.vc.nan_to_num(0.0, 0.0, 0.0).abs().max()) if b.vc.numel() else 0.0
-    extra = query_error(b, scale)
+    extra = query_error(b, scale, 5 if b.dtype == torch.float32 else 3 if lse is None else 4)
     tol = pu.tolerance(b.dtype, weight, S, D, vmax, logits) + 2 * extra[..., None] * (1 + extra[..., None]) * weight
     tol = tol + 2.0 ** -25 * weight
     err = (out.double().cpu() - want).abs()
