@@ -189,11 +189,12 @@ def test_pages_that_are_not_there(gpu, new, P):
     assert (out[a:e] == 0).all() and (lse[a:e] == -math.inf).all()
 
 
-def test_a_cache_without_pages(gpu):
-    b = fu.Batch4([10], [2], 4, 2, 64, 64, BF16, seed=5)
+@pytest.mark.parametrize("dtype,D,P", [(BF16, 64, 64), (BF16, 256, 64), (torch.float32, 128, 128), (torch.float16, 256, 16)])
+def test_a_cache_without_pages(gpu, dtype, D, P):
+    b = fu.Batch4([10], [2], 4, 2, D, P, dtype, seed=5)
     q, kc, vc, ks, vs, table, seq, qptr = b.upload(gpu)
     for n in (2, 40):
-        q = torch.ones(n, 4, 64, dtype=BF16, device=gpu)
+        q = torch.ones(n, 4, D, dtype=dtype, device=gpu)
         out = slnr.sparselnr_paged_attention_fp4(q, kc[:0], vc[:0], ks[:0], vs[:0], table, b.ints([n + 10], gpu),
                                                  b.ints([0, n], gpu))
         assert (out == 0).all()

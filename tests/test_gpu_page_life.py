@@ -249,6 +249,25 @@ def test_several_arrays_at_once(gpu):
         assert torch.equal(x.contiguous().view(torch.uint8), w.contiguous().view(torch.uint8))
 
 
+@pytest.mark.parametrize("n", [70000, 70001, 131072])
+def test_long_lists_of_few_pairs(gpu, n):
+    """Pairs between many that are left out: each block looks at many steps at once."""
+    pages = 3000
+    xs = [torch.arange(pages * w, dtype=torch.int32, device=gpu).view(pages, w) for w in (5, 4096, 12)]
+    want = [x.clone() for x in xs]
+    g = torch.Generator().manual_seed(n)
+    at = torch.randperm(n - 2, generator=g)[:200].tolist() + [n - 2, n - 1]
+    order = torch.randperm(pages, generator=g)[:2 * len(at)].view(-1, 2)
+    pairs = torch.full((n, 2), -1, dtype=I32)
+    pairs[::3, 0] = 7  # only half of a pair
+    pairs[at] = order.int()
+    for w in want:
+        w[order[:, 1].to(gpu)] = w[order[:, 0].to(gpu)]
+    slnr.sparselnr_page_copy(pairs.to(gpu), xs)
+    for x, w in zip(xs, want):
+        assert torch.equal(x, w)
+
+
 def test_pages_past_32_bits(gpu):
     x = torch.empty(700, 1 << 23, dtype=torch.uint8, device=gpu)
     x[3], x[699], x[350] = 1, 2, 3
