@@ -71,7 +71,7 @@ class Held:
 
 
 SHAPES = [(1, 1, 16, 4), (3, 5, 16, 40), (20, 7, 4, 130), (64, 40, 8, 3000), (300, 9, 1, 1500), (9, 700, 2, 5000), (37, 30, 2, 24001),
-          (70, 64, 4, 4500), (6, 11, 16, 40000), (1, 4096, 1, 5)]
+          (70, 64, 4, 4500), (6, 11, 16, 40000), (1, 4096, 1, 5), (7, 3001, 2, 16000), (3, 40000, 1, 90001)]
 
 
 @pytest.mark.parametrize("R,W,P,pages", SHAPES)
