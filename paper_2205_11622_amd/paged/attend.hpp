@@ -1217,9 +1217,10 @@ __global__ __launch_bounds__(kJoinBlock) void join_few(AttendArgs a) {
 }
 
 // The same for the tiles of attend_many: many rows of few pieces, a wave per row.
-// Bound by memory and by its start: 34 us behind the 559 GFLOP above, 9 behind the
-// window's batch; one row to a block's wave at a time took 44 and 18.
-constexpr int kJoinRows = 8;  // rows of a block, two of them one after the other in each wave
+// Bound by memory and by the chain of its loads, so a wave has two rows on their way: 27 us behind the 559 GFLOP above, 7
+// behind the window's batch, 10 behind the one in 4 bits (one row after the other 34, 9 and 13; one row a wave 44, 18
+// and 13; four rows 11 for the last).
+constexpr int kJoinRows = 8;  // rows of a block, two of them side by side in each wave
 
 template <class T, int DP, int ROWS>
 __global__ __launch_bounds__(kJoinBlock) void join_many(AttendArgs a) {
@@ -1233,36 +1234,56 @@ __global__ __launch_bounds__(kJoinBlock) void join_many(AttendArgs a) {
     const int32_t *mt = a.meta + (1 + s) * kMeta;
     const int np = mt[0], rows = mt[2];
     if (np <= 1) continue;
-    for (int i = blockIdx.y * kJoinRows + wave; i < rows && i < (int)(blockIdx.y + 1) * kJoinRows;
-         i += kJoinBlock / kWave) {
-      const float *part = a.part + s * kSize + i * DP + lane * C;
-      const float *ml = a.part + s * kSize + ROWS * DP + i * 2;
-      float mx = kNegInf;
-      for (int j = lane; j < np; j += kWave) mx = fmaxf(mx, ml[j * next]);
+    constexpr int kSide = kJoinRows / (kJoinBlock / kWave);  // rows of a wave
+    const int i0 = blockIdx.y * kJoinRows + wave;
+    if (i0 >= rows) continue;
+    const float *part[kSide], *ml[kSide];
+    float mx[kSide], sum[kSide], o[kSide][C];
 #pragma unroll
-      for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
-      float sum = 0.0f, o[C];
+    for (int k = 0; k < kSide; ++k) {
+      const int i = i0 + k * (kJoinBlock / kWave) < rows ? i0 + k * (kJoinBlock / kWave) : i0;
+      part[k] = a.part + s * kSize + i * DP + lane * C;
+      ml[k] = a.part + s * kSize + ROWS * DP + i * 2;
+      mx[k] = kNegInf, sum[k] = 0.0f;
 #pragma unroll
-      for (int c = 0; c < C; ++c) o[c] = 0.0f;
-#pragma unroll 4
-      for (int j = 0; j < np; ++j) {
-        const float mj = ml[j * next], lj = ml[j * next + 1];
-        const float w = mj == kNegInf ? 0.0f : exp2_of((mj - mx) * sc);
-        float x[C];
+      for (int c = 0; c < C; ++c) o[k][c] = 0.0f;
+    }
+    for (int j = lane; j < np; j += kWave)
 #pragma unroll
-        for (int c = 0; c < C; ++c) x[c] = part[j * next + c];
+      for (int k = 0; k < kSide; ++k) mx[k] = fmaxf(mx[k], ml[k][j * next]);
+#pragma unroll
+    for (int n = 32; n; n >>= 1)
+#pragma unroll
+      for (int k = 0; k < kSide; ++k) mx[k] = fmaxf(mx[k], __shfl_xor(mx[k], n));
+#pragma unroll 2
+    for (int j = 0; j < np; ++j) {
+      float x[kSide][C], mj[kSide], lj[kSide];
+#pragma unroll
+      for (int k = 0; k < kSide; ++k) {
+        mj[k] = ml[k][j * next], lj[k] = ml[k][j * next + 1];
+#pragma unroll
+        for (int c = 0; c < C; ++c) x[k][c] = part[k][j * next + c];
+      }
+#pragma unroll
+      for (int k = 0; k < kSide; ++k) {
+        const float w = mj[k] == kNegInf ? 0.0f : exp2_of((mj[k] - mx[k]) * sc);
         if (w != 0.0f) {
-          sum += w * lj;
+          sum[k] += w * lj[k];
 #pragma unroll
-          for (int c = 0; c < C; ++c) o[c] += w * x[c];
+          for (int c = 0; c < C; ++c) o[k][c] += w * x[k][c];
         }
       }
+    }
+#pragma unroll
+    for (int k = 0; k < kSide; ++k) {
+      const int i = i0 + k * (kJoinBlock / kWave);
+      if (i >= rows) break;
       const int row = mt[1] + i, t = row / a.G, hd = mt[3] * a.G + row % a.G;
       const int64_t at = (int64_t)t * a.Hq + hd;
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        if (lane * C + c < a.D) ((T *)a.out)[at * a.D + lane * C + c] = (T)(mx == kNegInf ? 0.0f : o[c] / sum);
-      if (lane == 0 && a.lse) a.lse[at] = mx == kNegInf ? kNegInf : mx * (sc * kLn2) + __logf(sum);
+        if (lane * C + c < a.D) ((T *)a.out)[at * a.D + lane * C + c] = (T)(mx[k] == kNegInf ? 0.0f : o[k][c] / sum[k]);
+      if (lane == 0 && a.lse) a.lse[at] = mx[k] == kNegInf ? kNegInf : mx[k] * (sc * kLn2) + __logf(sum[k]);
     }
   }
 }
