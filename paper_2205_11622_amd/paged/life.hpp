@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kOneBlock) void page_compact_one(LifeArgs a) {
 // -------------------------------------------------------------------- copies
 
 constexpr int kCopyArrays = 8;
-constexpr int kCopyBytes = 16384;  // of a block's step
+constexpr int kCopyBytes = 16384;  // of a block's step: the 697 MB below 136 us; 8 KB 140, 32 KB 137
 
 struct CopyArray {
   uint8_t *data;
@@ -460,7 +460,7 @@ __device__ __forceinline__ void copy_step(const CopyArray &x, int from, int to, 
 }
 
 // A block takes 16 KB of a page of one array at a time; four 16-byte loads a thread are on their way.  Memory: 697 MB read and
-// written in 133 us, 5.2 TB/s (a torch copy of 4 GiB 4.7); 118 MB, much of it in the last cache, in 12.
+// written in 136 us, 5.1 TB/s (a torch copy of 4 GiB 4.7); 118 MB, much of it in the last cache, in 12.
 // Its lanes look at the pairs of its next 64 steps at once: a list is mostly of pairs that are left out, where a large cache
 // was compacted (100000 pages, 64 of them moved, two arrays of 128 KB a page: 16 us, with a look at each step's pair in turn 230).
 __global__ __launch_bounds__(kLifeBlock) void page_copy(CopyArgs a) {
