@@ -1,0 +1,117 @@
+"""Attention over the 4-bit cache where lse is not asked for, on the GPU against its definition in 64 bits: the
+many-row kernel with as few pieces of the query as out needs, and rows beside those of the call."""
+import math
+
+import pytest
+import torch
+
+import paper_2205_11622_amd as slnr
+from tests import fp4_util as fu
+from tests import paged_util as pu
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+PIECES = {BF16: 3, FP16: 4, FP32: 5}
+
+
+def attend(b, gpu, window=0, max_new=0, qptr=None, lse=None):
+    """out, with 8 rows of sevens before and behind it that have to stay."""
+    up = b.upload(gpu)
+    q = up[0]
+    T = q.shape[0]
+    base = torch.full((T + 16, *q.shape[1:]), 7.0, dtype=q.dtype, device=gpu)
+    at = up[-1] if qptr is None else b.ints(qptr, gpu)
+    slnr.sparselnr_paged_attention_fp4(*up[:-1], at, window=window, max_new=max_new, out=base[8:8 + T], lse=lse)
+    torch.cuda.synchronize()
+    assert (base[:8] == 7).all() and (base[8 + T:] == 7).all()
+    return base[8:8 + T].cpu()
+
+
+def check(b, out, ref, extra, logits=8.0, nan=False):
+    """out within paged_util's bound for its type, what the query's pieces leave (`extra`), and 2^-25 of fp32's
+    weights in three pieces; NaN (nan: there may be any) where the definition has it."""
+    want, _, weight = ref
+    D = b.q.shape[2]
+    vmax = float(b.vc.nan_to_num(0.0, 0.0, 0.0).abs().max())
+    tol = pu.tolerance(b.dtype, weight, max(b.seq + [1]), D, vmax, logits) + extra + 2.0 ** -25 * weight
+    assert out.dtype == b.dtype and (nan or not want.isnan().any())
+    assert torch.equal(out.isnan(), want.isnan())
+    fine = ~want.isnan()
+    err = (out.double() - want).abs()
+    bad = fine & ~(err <= tol)
+    assert not bad.any(), "%d of %d off, worst %.3g of its bound at %s" % (
+        int(bad.sum()), bad.numel(), float((err / tol)[bad].max()), bad.nonzero()[0].tolist())
+
+
+def pieces_bound(b, weight):
+    """What a type's pieces may do to out: a score off by x makes its weight, and the sum, off by x relative."""
+    x = fu.query_error(b, b.q.shape[2] ** -0.5, PIECES[b.dtype])[..., None]
+    return 2 * x * (1 + x) * weight
+
+
+def compare(b, gpu, window=0, max_new=0, nan=False):
+    ref = b.reference(window=window)
+    out = attend(b, gpu, window, max_new)
+    check(b, out, ref, pieces_bound(b, ref[2]), nan=nan)
+    return out
+
+
+# ------------------------------------------------------------ the default call of a chunk
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("D", [8, 64, 96, 128, 200, 256])
+@pytest.mark.parametrize("P", [16, 64])
+def test_widths_and_pages(gpu, dtype, D, P):
+    compare(fu.Batch4([0, 5, 130], [70, 1, 301], 4, 2, D, P, dtype, seed=D + 3), gpu)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("window", [1, 31, 64, 100])
+@pytest.mark.parametrize("D,P", [(64, 64), (128, 16), (256, 64)])
+def test_windows(gpu, dtype, window, D, P):
+    compare(fu.Batch4([0, 3, 400], [90, 90, 90], 4, 2, D, P, dtype, seed=window), gpu, window=window)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("D,P", [(64, 16), (64, 64), (128, 16), (128, 64), (256, 16), (256, 64)])
+def test_pages_that_are_not_there(gpu, dtype, D, P):
+    b = fu.Batch4([300, 64, 10], [90] * 3, 8, 2, D, P, dtype, seed=5)
+    for j in (0, 3, 4):
+        b.table[0][j] = -1
+    b.table[1] = [-1] * len(b.table[1])  # nothing left: empty rows
+    b.table[2][0] = b.kc.shape[0]        # past the cache
+    out = compare(b, gpu)
+    assert (out[b.qptr[1]:b.qptr[2]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("window", [0, 40])
+@pytest.mark.parametrize("D,P", [(64, 16), (64, 64), (128, 16), (128, 64), (256, 16), (256, 64)])
+def test_nan_groups(gpu, dtype, window, D, P):
+    """NaN in V and K of the newest tokens, and of one that only the first tokens still see."""
+    b = fu.Batch4([61, 0], [130, 80], 4, 2, D, P, dtype, seed=9)
+    S, n = b.seq[0], b.bytes["vs"].shape[3]
+
+    def at(j, *rest):
+        return (b.table[0][j // P], j % P, *rest)
+    b.bytes["vs"][at(S - 1, slice(None), n - 1)] = 255
+    b.bytes["vs"][at(S - 2, 0, 0)] = 255
+    if window:
+        b.bytes["vs"][at(30, slice(None), 0)] = 255
+    b.bytes["ks"][at(S - 1, 1, 0)] = 255
+    b.refresh()
+    compare(b, gpu, window=window, nan=True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("P", [32, 64])
+def test_long_contexts_are_cut_and_joined(gpu, dtype, D, P):
+    compare(fu.Batch4([4000], [170], 4, 2, D, P, dtype, seed=11), gpu, max_new=170)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(3, 3), (7, 1), (12, 4), (128, 1)])
+def test_head_layouts(gpu, Hq, Hkv):
+    compare(fu.Batch4([100, 0, 37], [40, 1, 90], Hq, Hkv, 128, 16, BF16, seed=Hq), gpu)
