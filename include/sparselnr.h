@@ -456,10 +456,10 @@ SPARSELNR_API int sparselnr_cache_read_fp4(const int64_t *slots, const sparselnr
 
 /*
  * As sparselnr_paged_attention, over a cache in 4 bits.  q.k is computed on its bytes: a query's
- * groups of 32 values are written as sums of 6-bit pieces, exact to 2^-13 of the group's largest
- * value for bf16 and fp16, to 2^-18 if lse is asked for, and to 2^-23 for fp32, and summed in fp32 (q * scale is
- * taken in fp32 and has to be finite there).  V is exact; the weights are
- * rounded to the type of q, in fp32 to 24 bits.
+ * groups of 32 values are written as sums of 6-bit pieces, exact to 2^-18 of the group's largest
+ * value for fp16, to 2^-13 for bf16 (2^-18 if lse is asked for, and for requests of at most 64 tokens times query
+ * heads to a KV head), to 2^-23 for fp32, and summed in fp32 (q * scale is taken in fp32 and has to be finite there).
+ * V is exact; the weights are rounded to the type of q, in fp32 to 24 bits.
  */
 SPARSELNR_API int sparselnr_paged_attention_fp4(const void *q, int64_t q_token, int64_t q_head,
                                                 int64_t Hq, const sparselnr_fp4_cache *cache,

@@ -64,8 +64,8 @@ int run_attend_fp4(const Launch &l, AttendFp4Args a, int64_t max_new) {
   a.few = 0x7fffffff;
   if (rows > kFew4MostRows) {
     a.few = kFew4MostRows;
-    // A fourth piece of the query, for lse: the chunk of 4010 tokens 579 us, with it 642.  Few rows have
-    // it always: 96 single tokens 127.6 and 127.9 us.
+    // A fourth piece of a bf16 query, for lse: the chunk of 4010 tokens 579 us, with it 642.  fp16 has it always (2 of 2000 tokens
+    // behind 9000, 32/8 heads of 128, by three 567 us, by four 619), and so have few rows: 96 single tokens 127.6 and 127.9 us.
     const int rc = a.lse ? run_many_fp4<T, DP, ONE_PAGE, Four<T>::kQ>(l, a)
                          : run_many_fp4<T, DP, ONE_PAGE, Four<T>::kQOut>(l, a);
     if (rc != SPARSELNR_OK) return rc;

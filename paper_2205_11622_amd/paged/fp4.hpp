@@ -26,7 +26,7 @@ constexpr unsigned kNanScale = 255;  // a group with infinities or NaN: all of i
 // exactly.  kLeast, kMost: exponents of a group.  0.5 * 2^kLeast and 6 * 2^kMost are values of V4, so
 // that no group is lost or becomes infinite on its way back; only fp16's largest values
 // (above 7 * 2^13) and the last two binades of bf16 and fp32 are clipped by it.
-// kQ: pieces that a query is split into (see split_query), kQOut: as many as out needs, which is rounded to the type
+// kQ: pieces that a query is split into (see split_query), kQOut: as many as out needs, which is rounded to bf16
 // while lse is not; kP: pieces of a weight.
 template <class T>
 struct Four;
@@ -38,7 +38,7 @@ struct Four<__bf16> {
 template <>
 struct Four<_Float16> {
   typedef _Float16 V4;
-  static constexpr int kLeast = -23, kMost = 13, kQ = 4, kQOut = 3, kP = 1;
+  static constexpr int kLeast = -23, kMost = 13, kQ = 4, kQOut = 4, kP = 1;
 };
 template <>
 struct Four<float> {
@@ -177,10 +177,13 @@ __global__ __launch_bounds__(kFp4Block) void fp4_read(Fp4Args a) {
 // to 2, of 1/4 up to 4, of 1/2 up to 7.5) at four times the rate of a 16-bit
 // product, so a query is written as a sum of such pieces, each the rest of those before it,
 // with an exponent of its own per group.  A first piece leaves at most 1/4 of its unit, 4 units of a second
-// one 16 times finer; each further piece is 32 times finer.  Three pieces leave 2^-12 of the first
-// unit, which is at most the group's largest value divided by 3.75: less than half a last place of that
-// value in fp16 (and far less in bf16), enough for out, which is rounded to the type.  lse is not: over 1000 keys at dim 96 three
-// pieces put it off by up to 1.9e-4, four, which leave 2^-17, by 4e-6.  Five leave 2^-22: a last place of fp32.
+// one 16 times finer; each further piece is 32 times finer.  The first unit is at most the group's largest value divided by
+// 3.75, so three pieces leave 2^-13 of that value, four 2^-18, five 2^-23.  All of this goes by the group's
+// largest value: where a channel is A times the others (A times less in K), what is left of the others counts A times as much.
+// Relative error of out over 1000 keys at dim 128 by three | four pieces, A = 1: 3.5e-5 | 1.1e-6, 30: 4.0e-4 | 1.3e-5, 100:
+// 1.4e-3 | 4.3e-5, 300: 4.2e-3 | 1.3e-4; the rounding of the result is 1.6e-3 in bf16 and 2e-4 in fp16.  So bf16's out takes three, up to
+// A = 100 no more than its rounding, and fp16's takes four.  lse is fp32: over 1000 keys at dim 96 three
+// pieces put it off by up to 1.9e-4, four by 4e-6.
 constexpr int query_step(int piece) { return piece == 0 ? 0 : 5 * piece - 1; }
 
 template <int N>

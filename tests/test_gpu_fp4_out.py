@@ -115,3 +115,61 @@ def test_long_contexts_are_cut_and_joined(gpu, dtype, D, P):
 @pytest.mark.parametrize("Hq,Hkv", [(3, 3), (7, 1), (12, 4), (128, 1)])
 def test_head_layouts(gpu, Hq, Hkv):
     compare(fu.Batch4([100, 0, 37], [40, 1, 90], Hq, Hkv, 128, 16, BF16, seed=Hq), gpu)
+
+
+# ------------------------------------------------------------ channels of very different size
+
+
+def with_outliers(b, by):
+    """A channel of each group `by` times the others in q, and the others `by` times it in K: all count alike."""
+    b.q = b.q.clone()
+    b.q[..., 5::32] *= by
+    b.kc = b.kc.to(b.dtype)
+    b.kc[..., 5::32] /= by
+    b.vc = b.vc.to(b.dtype)
+    b.requantise()
+    return b
+
+
+def first_order(b, window=0):
+    """Bound on what the query's pieces do to out, T x Hq x D.  With q off by r, scores are off by s = scale r.k and
+    out by sum_j p_j (v_j - out) s_j = scale sum_d r_d C_d, C_d = sum_j p_j (v_j - out) k_jd, and by less than 2 x^2
+    of the weighted |v| beyond that, x the largest |s_j|.  |r_d| is at most 2^(3 - 5 pieces) / 3.75 of its group's largest value."""
+    T, Hq, D = b.q.shape
+    G, P, scale = Hq // b.kc.shape[2], b.P, D ** -0.5
+    unit = 2.0 ** (3 - 5 * PIECES[b.dtype]) / 3.75
+    top = torch.nn.functional.pad(b.q.double(), (0, -D % 32)).unflatten(-1, (-1, 32)).abs().amax(-1)
+    rest = unit * top.repeat_interleave(32, -1)[..., :D]
+    bound = torch.zeros(T, Hq, D, dtype=torch.float64)
+    for r, S in enumerate(b.seq):
+        k, v, there = pu.gather(b.kc, b.vc, b.table[r], list(range(S)))
+        for t in range(b.qptr[r], b.qptr[r + 1]):
+            n = S - b.qptr[r + 1] + t + 1
+            seen = there[:n] & (torch.arange(n) >= n - window if window else True)
+            for h in range(Hq):
+                kk, vv = k[:n][seen, h // G], v[:n][seen, h // G]
+                p = torch.softmax(kk @ b.q[t, h].double() * scale, 0)
+                c = (p[:, None] * kk).t() @ (vv - p @ vv)
+                x = scale * (rest[t, h] * kk.abs()).sum(1).max()
+                bound[t, h] = scale * (rest[t, h] @ c.abs()) + 2 * x * x * (p @ vv.abs())
+    return bound
+
+
+@pytest.mark.parametrize("dtype,D,P,by", [(FP16, 64, 64, 100), (FP16, 96, 16, 100), (FP16, 128, 64, 100), (FP16, 128, 32, 200),
+                                          (FP16, 256, 64, 100), (BF16, 128, 64, 100), (BF16, 256, 16, 100),
+                                          (FP32, 128, 64, 100)])
+def test_channels_of_very_different_size(gpu, dtype, D, P, by):
+    """What the pieces leave is the type's own bound at most, by their number of pieces."""
+    b = with_outliers(fu.Batch4([0, 120], [90, 70], 4, 2, D, P, dtype, seed=31), by)
+    ref = b.reference()
+    check(b, attend(b, gpu), ref, first_order(b))
+
+
+@pytest.mark.parametrize("dtype", [FP16, FP32])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("P", [16, 64])
+def test_out_does_not_depend_on_lse(gpu, dtype, D, P):
+    """Where lse is exact enough with the pieces that out has, both calls are one."""
+    b = fu.Batch4([0, 5, 130], [70, 1, 301], 4, 2, D, P, dtype, seed=D + 1)
+    lse = torch.full(b.q.shape[:2], math.nan, device=gpu)
+    assert torch.equal(attend(b, gpu), attend(b, gpu, lse=lse)) and not lse.isnan().any()
