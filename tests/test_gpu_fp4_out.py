@@ -173,3 +173,25 @@ def test_out_does_not_depend_on_lse(gpu, dtype, D, P):
     b = fu.Batch4([0, 5, 130], [70, 1, 301], 4, 2, D, P, dtype, seed=D + 1)
     lse = torch.full(b.q.shape[:2], math.nan, device=gpu)
     assert torch.equal(attend(b, gpu), attend(b, gpu, lse=lse)) and not lse.isnan().any()
+
+
+# ------------------------------------------------------------ offsets that do not fit
+
+
+@pytest.mark.parametrize("what", ["tokens past T", "backwards", "negative"])
+@pytest.mark.parametrize("n", [3, 90])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+def test_offsets_that_do_not_fit(gpu, what, n, dtype):
+    """Offsets count as the nearest ones in [0, T], and a request that ends before it begins has no tokens: what is
+    left is attended, and other rows stay as they were."""
+    b = fu.Batch4([200, 200], [n, n], 4, 2, 64, 16, dtype, seed=7)
+    b.q = torch.cat([b.q, b.q[:n]])
+    T = 3 * n
+    qptr, held = {"tokens past T": ([0, n, 100 * n], [0, n, T]), "backwards": ([0, 2 * n, n], [0, 2 * n, 2 * n]),
+                  "negative": ([-5, n, 2 * n], [0, n, 2 * n])}[what]
+    out = attend(b, gpu, qptr=qptr)
+    assert (out[held[-1]:] == 7).all()
+    b.qptr = held
+    b.q, out = b.q[:held[-1]], out[:held[-1]]
+    ref = b.reference()
+    check(b, out, ref, pieces_bound(b, ref[2]))
