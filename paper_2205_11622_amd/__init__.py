@@ -36,6 +36,11 @@ and pages shared between requests, given back, and moved together, whatever they
     freed, counts = sparselnr_page_free(rows, table, seq, shares, P)
     pairs, counts = sparselnr_page_compact(table, seq, shares, P)
     sparselnr_page_copy(pairs, (kcache, vcache))
+
+Every call is queued on the current stream of its inputs' GPU, or on `stream` (a
+torch.cuda.Stream or a handle).  Then its inputs have to be ready there, and what it
+returns is ready there: the current stream has to wait for it (wait_stream) before
+it reads the results.
 """
 from __future__ import annotations
 
@@ -251,6 +256,25 @@ def _stream(stream, device):
 _get_device = None
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory of `device` for a result of a call on `stream`.  Where that is another stream than the current one
+    it is taken as that one's: the current one's may still be in use there, and nothing orders the two.  The
+    caller gets it on the current stream, so it is not given out again before the work that is queued there then."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    current = torch.cuda.current_stream(device)
+    if not hasattr(stream, "cuda_stream"):  # a handle
+        raw = getattr(stream, "value", stream)
+        stream = torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+    if stream.cuda_stream == current.cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        result = torch.empty(shape, dtype=dtype, device=device)
+    result.record_stream(current)
+    return result
+
+
 def _on(index, entry, *args):
     """entry(*args) with GPU `index` current: the library launches and allocates there."""
     global _get_device
@@ -299,7 +323,7 @@ def sparselnr_fused_sddmm_spmm(rowptr, colidx, vals, C, D, E, A=None, stream=Non
         raise ValueError("C and D differ in width K")
     L = _dense(E, "E", M, device)
     if A is None:
-        A = torch.empty((N, L), dtype=torch.float32, device=device)
+        A = _empty((N, L), torch.float32, device, stream)
     elif _dense(A, "A", N, device) != L:
         raise ValueError("A must be N x L")
     rc = _on(device.index, lib().sparselnr_fused_sddmm_spmm,
@@ -340,7 +364,7 @@ def sparselnr_sddmm(rowptr, colidx, vals, C, D, Y=None, stream=None):
     if _dense(D, "D", M, device) != K:
         raise ValueError("C and D differ in width K")
     if Y is None:
-        Y = torch.empty(colidx.numel(), dtype=torch.float32, device=device)
+        Y = _empty(colidx.numel(), torch.float32, device, stream)
     else:
         _check(Y, "Y", torch.float32, device, 1)
         if Y.numel() != colidx.numel():
@@ -360,7 +384,7 @@ def sparselnr_spmm(rowptr, colidx, Y, E, A=None, stream=None):
     M = E.shape[0] if isinstance(E, torch.Tensor) and E.dim() == 2 else -1
     L = _dense(E, "E", M, device)
     if A is None:
-        A = torch.empty((N, L), dtype=torch.float32, device=device)
+        A = _empty((N, L), torch.float32, device, stream)
     elif _dense(A, "A", N, device) != L:
         raise ValueError("A must be N x L")
     rc = _on(device.index, lib().sparselnr_spmm,
@@ -381,13 +405,13 @@ def sparselnr_unfused_sddmm_spmm(rowptr, colidx, vals, C, D, E, Y=None, A=None, 
         raise ValueError("C and D differ in width K")
     L = _dense(E, "E", M, device)
     if Y is None:
-        Y = torch.empty(colidx.numel(), dtype=torch.float32, device=device)
+        Y = _empty(colidx.numel(), torch.float32, device, stream)
     else:
         _check(Y, "Y", torch.float32, device, 1)
         if Y.numel() != colidx.numel():
             raise ValueError("Y must have nnz entries")
     if A is None:
-        A = torch.empty((N, L), dtype=torch.float32, device=device)
+        A = _empty((N, L), torch.float32, device, stream)
     elif _dense(A, "A", N, device) != L:
         raise ValueError("A must be N x L")
     rc = _on(device.index, lib().sparselnr_unfused_sddmm_spmm,
@@ -398,10 +422,10 @@ def sparselnr_unfused_sddmm_spmm(rowptr, colidx, vals, C, D, E, Y=None, A=None, 
     return Y, A
 
 
-def _out(A, rows, cols, device, name="A"):
+def _out(A, rows, cols, device, stream, name="A"):
     torch = _torch()
     if A is None:
-        return torch.empty((rows, cols), dtype=torch.float32, device=device)
+        return _empty((rows, cols), torch.float32, device, stream)
     if _dense(A, name, rows, device) != cols:
         raise ValueError("%s must be %d x %d" % (name, rows, cols))
     return A
@@ -418,7 +442,7 @@ def sparselnr_fused_sddmm_spmm_gemm(rowptr, colidx, vals, C, D, F, W, A=None, st
         raise ValueError("C and D differ in width K")
     L = _dense(F, "F", M, device)
     Mo = _dense(W, "W", L, device)
-    A = _out(A, N, Mo, device)
+    A = _out(A, N, Mo, device, stream)
     rc = _on(device.index, lib().sparselnr_fused_sddmm_spmm_gemm,
              _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
              _ptr(F, device), _ptr(W, device), _ptr(A, device), N, M, K, L, Mo, _stream(stream, device))
@@ -434,7 +458,7 @@ def sparselnr_spmm_gemm(rowptr, colidx, vals, C, D, A=None, stream=None):
     M = C.shape[0] if isinstance(C, torch.Tensor) and C.dim() == 2 else -1
     K = _dense(C, "C", M, device)
     L = _dense(D, "D", K, device)
-    A = _out(A, N, L, device)
+    A = _out(A, N, L, device, stream)
     rc = _on(device.index, lib().sparselnr_spmm_gemm,
              _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
              _ptr(A, device), N, M, K, L, _stream(stream, device))
@@ -452,7 +476,7 @@ def sparselnr_spmmh_gemm(rowptr, colidx, vals, C, D, E, A=None, stream=None):
     if _dense(D, "D", M, device) != J:
         raise ValueError("C and D must have the same shape")
     L = _dense(E, "E", J, device)
-    A = _out(A, N, L, device)
+    A = _out(A, N, L, device, stream)
     rc = _on(device.index, lib().sparselnr_spmmh_gemm,
              _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(D, device),
              _ptr(E, device), _ptr(A, device), N, M, J, L, _stream(stream, device))
@@ -470,7 +494,7 @@ def sparselnr_fused_sddmm_spmm_dt(rowptr, colidx, vals, C, Dt, E, A=None, stream
     if _dense(Dt, "Dt", K, device) != M:
         raise ValueError("Dt must be K x M")
     L = _dense(E, "E", M, device)
-    A = _out(A, N, L, device)
+    A = _out(A, N, L, device, stream)
     rc = _on(device.index, lib().sparselnr_fused_sddmm_spmm_dt,
              _ptr(rowptr, device), _ptr(colidx, device), _ptr(vals, device), _ptr(C, device), _ptr(Dt, device),
              _ptr(E, device), _ptr(A, device), N, M, K, L, _stream(stream, device))
@@ -617,11 +641,11 @@ def sparselnr_page_tables(ctx_len, new_len, table, free_pages, tokens, page_size
     device = ctx_len.device
     if qptr is None and seq_len is None and counts is None:
         # one allocation for the three
-        qptr, seq_len, counts = torch.empty(2 * R + 4, dtype=int32, device=device).split_with_sizes((R + 1, R, 3))
-    qptr = torch.empty(R + 1, dtype=int32, device=device) if qptr is None else qptr
-    seq_len = torch.empty(R, dtype=int32, device=device) if seq_len is None else seq_len
-    counts = torch.empty(3, dtype=int32, device=device) if counts is None else counts
-    slots = torch.empty(tokens, dtype=torch.int64, device=device) if slots is None else slots
+        qptr, seq_len, counts = _empty(2 * R + 4, int32, device, stream).split_with_sizes((R + 1, R, 3))
+    qptr = _empty(R + 1, int32, device, stream) if qptr is None else qptr
+    seq_len = _empty(R, int32, device, stream) if seq_len is None else seq_len
+    counts = _empty(3, int32, device, stream) if counts is None else counts
+    slots = _empty(tokens, torch.int64, device, stream) if slots is None else slots
     rc = _on(index, lib().sparselnr_page_tables,
              *args, _packed(qptr, "qptr", int32, index, (R + 1,)), _packed(seq_len, "seq_len", int32, index, (R,)),
              _packed(slots, "slots", torch.int64, index, (tokens,)), _packed(counts, "counts", int32, index, (3,)),
@@ -656,7 +680,7 @@ def sparselnr_cache_append(k, v, slots, kcache, vcache, kq=None, kscale=None, st
         raise SparseLNRError(rc, "sparselnr_cache_append")
 
 
-def _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse):
+def _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse, stream):
     torch = _torch()
     index, shape, cache = _cache(kcache, vcache)
     dtype = kcache.dtype
@@ -668,7 +692,7 @@ def _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse):
         raise ValueError("query heads must be a multiple of the cache's heads")
     requests = _requests(table, seq_len, qptr, T, index)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
+        out = _empty((T, Hq, D), dtype, q.device, stream)
     else:
         _packed(out, "out", dtype, index, (T, Hq, D))
     lse_at = None if lse is None else _packed(lse, "lse", torch.float32, index, (T, Hq))
@@ -682,7 +706,7 @@ def sparselnr_paged_attention(q, kcache, vcache, table, seq_len, qptr, scale=Non
     cached rows of their requests.  scale defaults to D ** -0.5; window > 0 bounds
     how far back a token sees; max_new > 0 says that no request has more new
     tokens.  lse (float32 T x Hq), if given, is filled.  Returns out (T x Hq x D)."""
-    index, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse)
+    index, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse, stream)
     rc = _on(index, lib().sparselnr_paged_attention,
              *head, scale, window, max_new, out.data_ptr(), lse, _launch_stream(stream, index))
     if rc != OK:
@@ -711,7 +735,7 @@ def sparselnr_block_select(q, kq, kscale, table, seq_len, qptr, page_size, top, 
     ks_at = _packed(kscale, "kscale", torch.float32, index, (pages, Hkv))
     requests = _requests(table, seq_len, qptr, T, index)
     if sel is None:
-        sel = torch.empty((T, Hkv, max(top, 0)), dtype=torch.int32, device=q.device)
+        sel = _empty((T, Hkv, max(top, 0)), torch.int32, q.device, stream)
     else:
         _packed(sel, "sel", torch.int32, index, (T, Hkv, top))
     rc = _on(index, lib().sparselnr_block_select,
@@ -726,7 +750,7 @@ def sparselnr_block_attention(q, kcache, vcache, table, seq_len, qptr, sel, scal
                               stream=None):
     """As sparselnr_paged_attention, over the pages sel (int32 T x Hkv x top) of each
     token and KV head only.  Returns out (T x Hq x D)."""
-    index, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse)
+    index, out, head, scale, lse = _attention(q, kcache, vcache, table, seq_len, qptr, scale, out, lse, stream)
     if not isinstance(sel, _torch().Tensor) or sel.dim() != 3:
         raise ValueError("sel must have 3 dimensions")
     top = sel.shape[2]
@@ -791,8 +815,8 @@ def sparselnr_cache_read_fp4(slots, kcache, vcache, kscale, vscale, dim, dtype, 
     index = _gpu(slots, "slots")
     T = slots.numel()
     shape = (T, kcache.shape[2] if isinstance(kcache, torch.Tensor) and kcache.dim() == 4 else 0, dim)
-    k = torch.empty(shape, dtype=dtype, device=slots.device) if k is None else k
-    v = torch.empty(shape, dtype=dtype, device=slots.device) if v is None else v
+    k = _empty(shape, dtype, slots.device, stream) if k is None else k
+    v = _empty(shape, dtype, slots.device, stream) if v is None else v
     index, _, cache = _fp4_cache(kcache, vcache, kscale, vscale, dim, k)
     rc = _on(index, lib().sparselnr_cache_read_fp4,
              _packed(slots, "slots", torch.int64, index, (T,)), cache, _packed(k, "k", dtype, index, shape),
@@ -816,7 +840,7 @@ def sparselnr_paged_attention_fp4(q, kcache, vcache, kscale, vscale, table, seq_
         raise ValueError("query heads must be a multiple of the cache's heads")
     requests = _requests(table, seq_len, qptr, T, index)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+        out = _empty((T, Hq, D), q.dtype, q.device, stream)
     else:
         _packed(out, "out", q.dtype, index, (T, Hq, D))
     lse_at = None if lse is None else _packed(lse, "lse", torch.float32, index, (T, Hq))
@@ -852,8 +876,8 @@ def sparselnr_page_fork(parents, children, table, seq_len, shares, free_pages, p
     index, stride, R, W, pages, at, seq_at, shares_at = _held(table, seq_len, shares)
     n = parents.numel() if isinstance(parents, torch.Tensor) else 0
     F = free_pages.numel() if isinstance(free_pages, torch.Tensor) else 0
-    pairs = torch.empty((n, 2), dtype=int32, device=table.device) if pairs is None else pairs
-    counts = torch.empty(2, dtype=int32, device=table.device) if counts is None else counts
+    pairs = _empty((n, 2), int32, table.device, stream) if pairs is None else pairs
+    counts = _empty(2, int32, table.device, stream) if counts is None else counts
     rc = _on(index, lib().sparselnr_page_fork,
              _packed(parents, "parents", int32, index, (n,)), _packed(children, "children", int32, index, (n,)), at,
              stride, seq_at, shares_at, _packed(free_pages, "free_pages", int32, index, (F,)),
@@ -872,8 +896,8 @@ def sparselnr_page_free(rows, table, seq_len, shares, page_size, freed=None, cou
     int32 = torch.int32
     index, stride, R, W, pages, at, seq_at, shares_at = _held(table, seq_len, shares)
     n = rows.numel() if isinstance(rows, torch.Tensor) else 0
-    freed = torch.empty(min(pages, n * W), dtype=int32, device=table.device) if freed is None else freed
-    counts = torch.empty(2, dtype=int32, device=table.device) if counts is None else counts
+    freed = _empty(min(pages, n * W), int32, table.device, stream) if freed is None else freed
+    counts = _empty(2, int32, table.device, stream) if counts is None else counts
     most = freed.numel() if isinstance(freed, torch.Tensor) else 0
     rc = _on(index, lib().sparselnr_page_free,
              _packed(rows, "rows", int32, index, (n,)), at, stride, seq_at, shares_at,
@@ -891,8 +915,8 @@ def sparselnr_page_compact(table, seq_len, shares, page_size, pairs=None, counts
     torch = _torch()
     int32 = torch.int32
     index, stride, R, W, pages, at, seq_at, shares_at = _held(table, seq_len, shares)
-    pairs = torch.empty((pages // 2, 2), dtype=int32, device=table.device) if pairs is None else pairs
-    counts = torch.empty(2, dtype=int32, device=table.device) if counts is None else counts
+    pairs = _empty((pages // 2, 2), int32, table.device, stream) if pairs is None else pairs
+    counts = _empty(2, int32, table.device, stream) if counts is None else counts
     rc = _on(index, lib().sparselnr_page_compact,
              at, stride, seq_at, shares_at, _packed(pairs, "pairs", int32, index, (pages // 2, 2)),
              _packed(counts, "counts", int32, index, (2,)), R, W, pages, page_size, _launch_stream(stream, index))
