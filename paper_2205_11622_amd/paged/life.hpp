@@ -87,9 +87,10 @@ __global__ __launch_bounds__(kLifeBlock) void page_fork(ForkArgs a, int per) {
     if (f.child < 0) continue;
     const int32_t *from = a.table + f.parent * a.table_row;
     int32_t *to = a.table + f.child * a.table_row;
-    const int full = f.length >> a.shift;
+    const unsigned full = f.length >> a.shift;
     const bool part = f.length & (P - 1);
-    for (int j = blockIdx.y * kLifeBlock + tid; j < a.W; j += gridDim.y * kLifeBlock) {
+    // without sign: a row of nearly 2^31 entries, and a step of up to 8192 behind it
+    for (unsigned j = blockIdx.y * kLifeBlock + tid; j < (unsigned)a.W; j += gridDim.y * kLifeBlock) {
       int page = -1;
       if (j < full) {
         page = from[j];
