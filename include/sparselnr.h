@@ -511,7 +511,7 @@ SPARSELNR_API int sparselnr_page_fork(const int32_t *parents, const int32_t *chi
  * Gives up the rows rows[i], i < n: their entries become -1 and their seq_len 0.  A
  * page that another row shares loses one of its shares; one that no other row holds is freed.
  *   freed (int32 [most]): the freed pages, ascending, -1 behind them
- *   counts = { pages freed, entries given up }
+ *   counts = { pages freed, entries given up (2^31 - 1 if there are more) }
  * A row that occurs twice is given up once; numbers that are no rows are left out.  Pages
  * beyond `most` are freed but not listed (counts[0] tells).  min(pages, n * W) is always enough.
  */

@@ -49,7 +49,8 @@ __device__ __forceinline__ Fork fork_of(const ForkArgs &a, int i) {
   return f;
 }
 
-__device__ __forceinline__ int block_sum(int x, int *shared) {
+template <class I>
+__device__ __forceinline__ I block_sum(I x, I *shared) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
   __syncthreads();
@@ -251,11 +252,12 @@ __global__ __launch_bounds__(kLifeBlock) void page_free_list(LifeArgs a, int blo
     if ((unsigned)r < (unsigned)a.R) a.seq[r] = 0;
   }
   if (blockIdx.x == gridDim.x - 1) {
+    __shared__ long long totals[kLifeBlock / kWave];
     const int all = marked_below(a, a.pages, sums);
-    int given = 0;
+    long long given = 0;  // tables have room for more than 2^31 entries
     for (int i = threadIdx.x; i < blocks; i += kLifeBlock) given += a.given[i];
-    given = block_sum(given, sums);
-    if (threadIdx.x == 0) a.counts[0] = all, a.counts[1] = given;
+    given = block_sum(given, totals);
+    if (threadIdx.x == 0) a.counts[0] = all, a.counts[1] = given < 0x7fffffff ? (int)given : 0x7fffffff;
   }
 }
 

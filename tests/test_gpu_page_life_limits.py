@@ -41,3 +41,15 @@ def test_the_widest_rows(gpu):
     assert counts.tolist() == [14, 4] and pairs[:5].tolist() == [[20, 10], [21, 11], [22, 12], [30, 13], [-1, -1]]
     assert table[1, :10].tolist() == list(range(10)) and table[1, -3:].tolist() == [10, 11, 12] and table[3, 0] == 13
     assert (table[1, 10:-3] == -1).all() and (table[0] == -1).all() and (table[2] == -1).all()
+
+
+def test_more_entries_than_a_count_holds(gpu):
+    """64 rows of 2^25 + 1000 entries, 2^31 + 64000 in all, over a million pages whose shares are too low by far."""
+    R, W, pages = 64, 2 ** 25 + 1000, 1 << 20
+    table = torch.arange(W, dtype=I32, device=gpu).remainder_(pages).repeat(R, 1)
+    seq = torch.full((R,), W, dtype=I32, device=gpu)
+    shares = torch.zeros(pages, dtype=I32, device=gpu)
+    freed, counts = slnr.sparselnr_page_free(torch.arange(R, dtype=I32, device=gpu), table, seq, shares, 1)
+    assert counts.tolist() == [pages, 2 ** 31 - 1]
+    assert torch.equal(freed, torch.arange(pages, dtype=I32, device=gpu))
+    assert (table == -1).all() and (seq == 0).all() and (shares == 0).all()
