@@ -406,8 +406,8 @@ SPARSELNR_API int sparselnr_block_attention(const void *q, int64_t q_token, int6
 /* ------------------------------------------------------------------------
  * A cache in 4 bits.
  *
- * The same pages, slots and block tables, with rows of a quarter of the size: a row
- * of dim values is NG = ceil(dim / 32) groups of 32, the last one filled up with
+ * The same pages, slots and block tables, with rows of 17 * NG bytes (17/64 of 16-bit rows where
+ * dim is a multiple of 32): a row of dim values is NG = ceil(dim / 32) groups of 32, the last one filled up with
  * zeros.  A group has 16 bytes, two values each, the first in the low half: a sign
  * (8) and 0..7 for 0, 0.5, 1, 1.5, 2, 3, 4, 6.  It has one more byte e + 127 elsewhere: its values are
  * multiplied by 2^e.  255 stands for a group that is NaN.  (The public formats E2M1
@@ -418,7 +418,8 @@ SPARSELNR_API int sparselnr_block_attention(const void *q, int64_t q_token, int6
  *     most 125 in bf16 and fp32, -23 and 13 in fp16, so that what a group stands for are values of
  *     the type it came from.  A value is rounded to the nearest, ties to an even code, and
  *     is off by at most 2^e (0.25, 0.5 or 1 times 2^e by its size), but for values above 7 times 2 to the
- *     largest e, which become 6 times that.  A group with an infinity or a NaN is NaN.
+ *     largest e, which become 6 times that.  So in bf16 and fp32 a group of values up to 2^-127 becomes
+ *     zeros.  A group with an infinity or a NaN is NaN.
  *   - Strides are in bytes; those of k and v keep rows at multiples of 16 bytes, those of the
  *     exponents may be any.  The 16 * NG bytes of a row, and its NG exponents, are adjacent.
  *     Heads before places in memory (a head's rows of a page adjacent) is the faster order.
@@ -458,7 +459,8 @@ SPARSELNR_API int sparselnr_cache_read_fp4(const int64_t *slots, const sparselnr
  * As sparselnr_paged_attention, over a cache in 4 bits.  q.k is computed on its bytes: a query's
  * groups of 32 values are written as sums of 6-bit pieces, exact to 2^-18 of the group's largest
  * value for fp16, to 2^-13 for bf16 (2^-18 if lse is asked for, and for requests of at most 64 tokens times query
- * heads to a KV head), to 2^-23 for fp32, and summed in fp32 (q * scale is taken in fp32 and has to be finite there).
+ * heads to a KV head), to 2^-23 for fp32 (or to 2^-128 where that is more), and summed in fp32 (q * scale is taken
+ * in fp32 and has to be finite there).  So what is left of small channels goes by the largest one of their group.
  * V is exact; the weights are rounded to the type of q, in fp32 to 24 bits.
  */
 SPARSELNR_API int sparselnr_paged_attention_fp4(const void *q, int64_t q_token, int64_t q_head,
@@ -474,7 +476,8 @@ SPARSELNR_API int sparselnr_paged_attention_fp4(const void *q, int64_t q_token, 
  * shares (int32 [pages]) counts the rows that hold a page beyond the first: 0 for a
  * page of one row and for a free one.  So a program whose rows never share anything
  * passes zeros, and sparselnr_page_tables, which hands out pages, need not know of it.
- * Only pages that are full are ever shared, so rows that share pages never write to them.
+ * Only pages that are full are ever shared, so rows that share pages never write to them (a program that makes
+ * a row shorter has to leave it its shared pages).
  *
  * Conventions as above, and:
  *   - seq_len[r] (int32 [R]) is the length of row r; its pages are the first

@@ -23,7 +23,7 @@ or, over the pages that a cheap score selects for each token and KV head,
     sel = sparselnr_block_select(q, kq, kscale, table, seq, qptr, P, top)
     out = sparselnr_block_attention(q, kcache, vcache, table, seq, qptr, sel)
 
-A cache may be kept in 4 bits, a quarter of its size (append, attention, and what it
+A cache may be kept in 4 bits, 17 bytes for 32 values (append, attention, and what it
 stands for):
 
     sparselnr_cache_append_fp4(k, v, slots, kcache, vcache, kscale, vscale)

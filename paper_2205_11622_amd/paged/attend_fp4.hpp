@@ -677,11 +677,12 @@ __global__ __launch_bounds__(kJoinBlock) void join_few_fp4(AttendArgs a) {
 //
 // attend_many_fp4: as attend_many, 32 rows to a wave over tiles of 64 keys in LDS, two
 // phases a tile.  K lies in LDS as its bytes and exponents: a product over 64 dimensions takes
-// 32 cycles, as one over 16 in 16 bits, so that three pieces of a query take three quarters
-// of the 16-bit products' time, and 1 KB of LDS serves all three of them.  In one phase the waves of a SIMD multiply, one of them
+// 32 cycles, as one over 16 in 16 bits, so that three pieces of a bf16 query take three quarters
+// of the 16-bit products' time (four all of it), and 1 KB of LDS serves all of them.  In one phase the waves of a SIMD multiply, one of them
 // the weights of the last tile with V, then the next scores; in the other they make weights of scores: two
 // waves a SIMD take turns.  The query is scaled before it is split and a product begins at the negative maximum, so that a
-// weight is one exponential of what comes out.  4010 tokens of 2 requests behind 5000 to 13000 keys, 32/8 heads of 128 in
+// weight is one exponential of what comes out.  Above 64 columns the maximum of 16-bit types may lag by 2^8, and the weights are
+// rounded to the type, both as in attend_many (see kLag): the chunk's result is off by 2.3e-3 in all, by 1.7e-3 with exact weights.  4010 tokens of 2 requests behind 5000 to 13000 keys, 32/8 heads of 128 in
 // bf16, 694 GFLOP: 573 to 614 us by card, 1.13 to 1.21 PFLOP/s, the rate of a bf16 library product.  The matrix cores are
 // busy 49% of the time at 2.0 GHz; without the exponentials it takes 8% less, without most of V's products 18%.
 template <class V4, int DP>

@@ -23,9 +23,10 @@ constexpr int kGroupBytes = 16;
 constexpr unsigned kNanScale = 255;  // a group with infinities or NaN: all of it is NaN
 
 // V4: the type that 4-bit values are taken into for products with the weights, all of them
-// exactly.  kLeast, kMost: exponents of a group.  0.5 * 2^kLeast and 6 * 2^kMost are values of V4, so
-// that no group is lost or becomes infinite on its way back; only fp16's largest values
-// (above 7 * 2^13) and the last two binades of bf16 and fp32 are clipped by it.
+// exactly.  kLeast, kMost: exponents of a group.  0.5 * 2^kLeast and 6 * 2^kMost are normal values of bf16 and values of fp16, so
+// that no code is lost or becomes infinite on its way back.  What it costs: values above 7 * 2^13 in fp16 and above
+// 7 * 2^125 in bf16 and fp32, the last quarter of their last binade, become 6 times the power, and in bf16 and fp32 groups of up to
+// 2^-127 become zeros.
 // kQ: pieces that a query is split into (see split_query), kQOut: as many as out needs, which is rounded to bf16
 // while lse is not; kP: pieces of a weight.
 template <class T>

@@ -165,6 +165,20 @@ def test_channels_of_very_different_size(gpu, dtype, D, P, by):
     check(b, attend(b, gpu), ref, first_order(b))
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("power", [100, 112, 120])
+@pytest.mark.parametrize("P", [16, 64])
+def test_very_small_queries(gpu, dtype, power, P):
+    """Queries near the least numbers and keys as large: the last piece's unit is at least 2^-125 and its steps an eighth
+    of it, so what is left is 2^-128 at most, of q by few rows and of q * scale * log2(e) by many."""
+    b = fu.Batch4([200, 90], [1, 80], 4, 2, 64, P, dtype, seed=10, amp=2.0 ** power)
+    b.q = (b.q.double() * 2.0 ** -power).to(dtype)
+    ref = b.reference()
+    k = b.kc.abs().nan_to_num(0.0, 0.0, 0.0).sum(-1).amax((0, 1)).repeat_interleave(2)  # no key has more
+    x = (fu.query_error(b, 0.125, PIECES[dtype]) + 2.0 ** -128 * k)[..., None]
+    check(b, attend(b, gpu), ref, 2 * x * (1 + x) * ref[2])
+
+
 @pytest.mark.parametrize("dtype", [FP16, FP32])
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("P", [16, 64])
