@@ -117,6 +117,44 @@ def test_head_layouts(gpu, Hq, Hkv):
     compare(fu.Batch4([100, 0, 37], [40, 1, 90], Hq, Hkv, 128, 16, BF16, seed=Hq), gpu)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("new", [1, 20, 130])
+@pytest.mark.parametrize("D,P", [(64, 64), (128, 16), (128, 64), (256, 64)])
+def test_nan_groups_that_all_tokens_see(gpu, dtype, new, D, P):
+    """In tiles that are whole: columns of V's group are NaN, and of a head whose K is, all."""
+    b = fu.Batch4([300, 70], [new, new], 4, 2, D, P, dtype, seed=19)
+    b.bytes["vs"][b.table[0][5 // P], 5 % P, 0, 1] = 255
+    b.bytes["vs"][b.table[0][130 // P], 130 % P, :, 0] = 255
+    b.bytes["ks"][b.table[1][40 // P], 40 % P, 1, 1] = 255
+    b.refresh()
+    out = compare(b, gpu, nan=True)
+    assert out[:new, :2, :64].isnan().all() and not out[:new, :2, 64:].isnan().any() and not out[:new, 2:, 32:].isnan().any()
+    assert out[new:, 2:].isnan().all() and not out[new:, :2].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("new", [1, 90])
+@pytest.mark.parametrize("D,P", [(64, 64), (128, 16), (256, 64)])
+def test_values_at_the_ends_of_the_type(gpu, dtype, new, D, P):
+    """A page a token of which nothing but one key is there: out is its value, from subnormals of fp16 to 6 * 2^125."""
+    lo, hi = fu.LIMITS[dtype]
+    b = fu.Batch4([0, 0], [new, new], 4, 2, D, P, dtype, seed=20)
+    g = torch.Generator().manual_seed(3)
+    for r in range(2):
+        for x in ("v", "vs", "k", "ks"):
+            page = b.bytes[x][b.table[r][0]]
+            page[0] = torch.randint(0, 256, page[0].shape, generator=g, dtype=torch.uint8)
+        b.bytes["ks"][b.table[r][0], 0] = 120
+        b.bytes["vs"][b.table[r][0], 0] = torch.tensor([lo + 127, hi + 127][r], dtype=torch.uint8)
+    b.seq = [1, 1]  # more tokens than positions: the last one sees the key, those before it nothing
+    b.refresh()
+    out = attend(b, gpu)
+    for r in range(2):
+        want = b.vc[b.table[r][0], 0].repeat_interleave(2, 0)
+        assert want.abs().max() == 6 * 2.0 ** [lo, hi][r]
+        assert torch.equal(out[b.qptr[r + 1] - 1].double(), want) and (out[b.qptr[r]:b.qptr[r + 1] - 1] == 0).all()
+
+
 # ------------------------------------------------------------ channels of very different size
 
 
