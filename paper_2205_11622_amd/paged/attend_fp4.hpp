@@ -683,7 +683,7 @@ __global__ __launch_bounds__(kJoinBlock) void join_few_fp4(AttendArgs a) {
 // waves a SIMD take turns.  The query is scaled before it is split and a product begins at the negative maximum, so that a
 // weight is one exponential of what comes out.  Above 64 columns the maximum of 16-bit types may lag by 2^8, and the weights are
 // rounded to the type, both as in attend_many (see kLag): the chunk's result is off by 2.3e-3 in all, by 1.7e-3 with exact weights.  4010 tokens of 2 requests behind 5000 to 13000 keys, 32/8 heads of 128 in
-// bf16, 694 GFLOP: 573 to 614 us by card, 1.13 to 1.21 PFLOP/s, the rate of a bf16 library product.  The matrix cores are
+// bf16, 694 GFLOP: 573 to 623 us by card, 1.11 to 1.21 PFLOP/s, the rate of a bf16 library product.  The matrix cores are
 // busy 49% of the time at 2.0 GHz; without the exponentials it takes 8% less, without most of V's products 18%.
 template <class V4, int DP>
 struct Many4Shared {
